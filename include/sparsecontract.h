@@ -73,7 +73,8 @@ typedef enum {
     SC_ERR_ALLOC              /* host allocation failed */
 } sc_status;
 
-typedef enum { SC_F32 = 0, SC_F64 = 1 } sc_dtype;
+/* Contractions take fp32 and fp64, attention (below) takes bf16, fp16 and fp32. */
+typedef enum { SC_F32 = 0, SC_F64 = 1, SC_BF16 = 2, SC_F16 = 3 } sc_dtype;
 
 /* Schedule classes of Section 4.2: LINEAR = the perfectly nested default nest, run
  * unfactored (every stored entry times one element of every factor for every combination
@@ -302,6 +303,117 @@ sc_status sc_stream_copy(void *dst, const void *src, size_t bytes, void *hip_str
 /* Frees the plan and its device tables (the tile tables cut from the CSF levels of Section 2.1 at
  * plan creation).  NULL is accepted.  Work queued by sc_execute must have finished. */
 sc_status sc_plan_destroy(sc_plan *plan);
+
+/* ------------------------------------------------------------------------------------------
+ * Attention over packed rows and over a paged cache.
+ *
+ * Kernel 1 of Table 2 with the sampled products of a row normalised before the second product,
+ *     A(i,l) = sum_j w(i,j) Z(j,l),   w(i,j) = exp(s(i,j)) / sum_j' exp(s(i,j')),   s(i,j) = scale * sum_k X(i,k) Y(j,k),
+ * where j runs over what row i may see: X are queries, Y keys, Z values, and the pattern is not a stored sparse matrix but
+ * follows from the lengths of the sequences (and from the table of the pages that hold a sequence's keys).  Three operators:
+ *   append   rotates the queries and keys of new rows by their positions and stores keys and values in the cache
+ *   prompt   attention of many rows per sequence, causal or not; keys packed like the queries, or in the cache
+ *   decode   attention of one row per sequence over the cache, the keys of a sequence split over the GPU and joined
+ *
+ * Conventions, besides those above
+ *   - Types: bf16, fp16, fp32, one for all of queries, keys, values, cache and output.  Products of 16-bit values are
+ *     exact, scores, the maximum and sum of a row and the output's sums are fp32.  The weights exp(s - max) are rounded to the 16-bit type
+ *     for the second product (bf16, fp16), the output once at the end.
+ *   - A row that sees no key gives +0.
+ *   - Keys and values that a row may not see do not reach it, whatever they hold (infinities and NaN too).  A NaN or
+ *     +infinity among the scores of a row makes it NaN; a score of -infinity has weight 0, and a row of such scores gives +0.  Infinite
+ *     or NaN values reach every row that sees them.
+ *   - Lengths, row starts and page numbers are device memory that may change from call to call; the kernels check what they
+ *     use of them (below) and read or write nothing out of range for wrong ones.
+ *   - No atomics: two calls on the same inputs give the same bits.
+ *   - Rows (of one head) and the cache are read 16 bytes at a time: every pointer and stride has to be a multiple of 16 bytes,
+ *     SC_ERR_SHAPE_MISMATCH otherwise.
+ * ------------------------------------------------------------------------------------------ */
+
+typedef struct sc_attention sc_attention;
+
+typedef struct {
+    sc_dtype dtype;             /* SC_BF16, SC_F16 or SC_F32 */
+    int32_t heads;              /* of queries and output */
+    int32_t kv_heads;           /* of keys and values; divides heads: query head h reads key head h / (heads / kv_heads) */
+    int32_t head_dim;           /* a multiple of 8, 8..256 */
+    int32_t page_rows;          /* rows of a page of the cache: a power of two, 16..4096 */
+    int32_t causal;             /* prompt: 1 = row at position p sees keys 0..p, 0 = every key of its sequence */
+    float scale;                /* of the scores; 0 = 1 / sqrt(head_dim); not negative */
+    int32_t rotary_dim;         /* append: leading elements of a row that are rotated; even, 0..head_dim */
+    int32_t rotary_interleaved; /* 0: element t is paired with t + rotary_dim / 2, 1: 2 t with 2 t + 1 */
+    const double *rotary_freq;  /* rotary_dim / 2 angles per position (host memory, read by sc_attention_create only) */
+} sc_attention_desc;
+
+/* Rows of heads: element (r, h, d) at data[r * row_stride + h * head_stride + d], strides in elements.  Head strides may be 0 on
+ * inputs (a head that all share). */
+typedef struct {
+    void *data;
+    int64_t row_stride, head_stride;
+} sc_rows_view;
+
+/* Cache of keys and values in pages: element (p, r, h, d) at keys[p * page_stride + r * row_stride + h * head_stride + d], and
+ * likewise in values. */
+typedef struct {
+    void *keys, *values;
+    int64_t pages;
+    int64_t page_stride, row_stride, head_stride;
+} sc_cache_view;
+
+/* The sequences of a call.  `rows` counts the rows of its queries (and of packed keys and values): sequence b has the rows
+ * [row_start[b], row_start[b + 1]), and row_start = NULL gives each sequence one row (rows = batch).  length[b] is the number of
+ * keys of the sequence, its new rows included, so that its n rows are at positions length[b] - n .. length[b] - 1.
+ * length = NULL (packed keys): as many as its rows.  Key j of sequence b is row j % page_rows of page
+ * page[b * page_ld + j / page_rows]; a sequence has page_count entries, of which those that length[b] reaches are read.
+ * Device memory all of it.  Kernels take row starts as if clamped to 0..rows; rows of no sequence are neither read nor written.  At most 2^24 - 1
+ * rows and 2^20 - 1 sequences. */
+typedef struct {
+    int32_t batch;
+    int64_t rows;
+    const int32_t *row_start;
+    const int32_t *length;
+    const int32_t *page;
+    int64_t page_ld;
+    int64_t page_count;
+} sc_sequence_view;
+
+/* Checks the description and prepares what the operators share.  Host work only, nothing is allocated on the device. */
+sc_status sc_attention_create(sc_attention **out, const sc_attention_desc *desc);
+
+/* Bytes of device workspace sc_attention_decode needs (256-byte aligned, contents arbitrary before and after): pieces of rows that
+ * are split over the GPU.  It does not depend on the sequences of a call.  Calls that share it must not overlap. */
+sc_status sc_attention_workspace_bytes(const sc_attention *attention, size_t *bytes);
+
+/* Human-readable description of the operators and of what a call reads, writes and computes.  Always NUL-terminates;
+ * truncates to n-1 characters. */
+sc_status sc_attention_describe(const sc_attention *attention, char *buf, size_t n);
+
+/* Stores `k`, rotated, and `v` (kv_heads heads each) in the pages of their positions, and writes `q` (heads heads), rotated, to
+ * `q_out`, which may be `q` itself.  `q` and `q_out` may both be NULL: keys and values alone.  The angle of pair t at position p is
+ * p * rotary_freq[t], taken in 64 bits and reduced by whole turns before its sine and cosine are taken in 32.  Needs length and
+ * page.  A row whose position is negative or not below page_count * page_rows, or whose page number is outside 0..pages-1, is not
+ * stored.  Queues one kernel on `hip_stream`; as sc_execute does, it allocates nothing and never synchronises. */
+sc_status sc_attention_append(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_rows_view *k,
+                              const sc_rows_view *v, const sc_rows_view *q_out, const sc_cache_view *cache, void *hip_stream);
+
+/* Attention of the rows of each sequence over the keys and values of the same rows, packed side by side (length must be NULL).
+ * `out` (heads heads) must not overlap the inputs. */
+sc_status sc_attention_prompt(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_rows_view *k,
+                              const sc_rows_view *v, const sc_rows_view *out, void *hip_stream);
+
+/* The same over keys and values in the cache, as many as length says: the rows are the last ones of their sequences, and a row
+ * at a negative position sees nothing.  A length that is negative or above page_count * page_rows, or a page number outside 0..pages-1 among
+ * those that a row's keys reach, makes NaN of the rows concerned. */
+sc_status sc_attention_prompt_paged(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_cache_view *cache,
+                                    const sc_rows_view *out, void *hip_stream);
+
+/* Attention of one row per sequence (row_start must be NULL) over all its keys in the cache.  Wrong lengths and page numbers as
+ * for prompts.  Queues two kernels: pieces of equal length for the whole GPU, then the join of rows that have several. */
+sc_status sc_attention_decode(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_cache_view *cache,
+                              const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Frees the handle; NULL is accepted. */
+sc_status sc_attention_destroy(sc_attention *attention);
 
 #ifdef __cplusplus
 }

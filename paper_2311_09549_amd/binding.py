@@ -20,7 +20,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsparsecontract.so")
 
-SC_F32, SC_F64 = 0, 1
+SC_F32, SC_F64, SC_BF16, SC_F16 = 0, 1, 2, 3
 SC_SCHED_LINEAR, SC_SCHED_FUSED, SC_SCHED_FISSIONED, SC_SCHED_AUTO = 0, 1, 2, 3
 
 STATUS_NAMES = [
@@ -35,6 +35,8 @@ EXPORTS = [
     "sc_plan_workspace_bytes", "sc_plan_describe", "sc_plan_model", "sc_plan_intermediate", "sc_execute",
     "sc_plan_set_profiling", "sc_plan_kernel_count", "sc_plan_kernel_time", "sc_plan_tile_count", "sc_plan_tile",
     "sc_tuning_set", "sc_stream_copy", "sc_plan_destroy", "sc_execute_static", "sc_plan_chosen",
+    "sc_attention_create", "sc_attention_workspace_bytes", "sc_attention_describe", "sc_attention_append", "sc_attention_prompt",
+    "sc_attention_prompt_paged", "sc_attention_decode", "sc_attention_destroy",
 ]
 
 _c_i32p = ctypes.POINTER(ctypes.c_int32)
@@ -63,6 +65,34 @@ _pack_csf = struct.Struct("@i4qqi4q4P4PPi0q").pack
 _pack_dense = [struct.Struct("@" + "Pqqqi" * n + "0q").pack for n in range(5)]
 assert len(_pack_csf(*[0] * 21)) == ctypes.sizeof(CsfView)
 assert all(len(pack(*[0] * (5 * n))) == n * ctypes.sizeof(DenseView) for n, pack in enumerate(_pack_dense))
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_rows", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float), ("rotary_dim", ctypes.c_int32),
+                ("rotary_interleaved", ctypes.c_int32), ("rotary_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class RowsView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class CacheView(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class SequenceView(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int64), ("row_start", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("page", ctypes.c_void_p), ("page_ld", ctypes.c_int64), ("page_count", ctypes.c_int64)]
+
+
+# Records of attention packed by one call each, like those of an execution: a decoding step of a layer is two calls of a few microseconds.
+pack_rows = struct.Struct("@Pqq").pack
+pack_cache = struct.Struct("@PPqqqq").pack
+pack_sequences = struct.Struct("@iqPPPqq").pack
+for _pack, _n, _record in ((pack_rows, 3, RowsView), (pack_cache, 6, CacheView), (pack_sequences, 7, SequenceView)):
+    assert len(_pack(*[0] * _n)) == ctypes.sizeof(_record)
 
 
 class Schedule(ctypes.Structure):
@@ -104,6 +134,10 @@ def lib():
         _sc_execute = _lib["sc_execute"]
         _sc_execute.restype = ctypes.c_int
         _sc_execute.argtypes = [ptr, ptr, ptr, ctypes.c_int32, ptr, ptr, ctypes.c_size_t, ptr]
+        for name, args in (("append", 8), ("prompt", 7), ("prompt_paged", 6)):
+            getattr(_lib, "sc_attention_" + name).argtypes = [ptr] * args
+        _lib.sc_attention_decode.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ctypes.c_size_t, ptr]
+        _lib.sc_attention_destroy.argtypes = [ptr]
     return _lib
 
 
@@ -391,3 +425,61 @@ def plan_kernel_times(plan: Plan):
                "sc_plan_kernel_time")
         res.append((name.value.decode(), float(ms.value)))
     return res
+
+
+class AttentionHandle:
+    """A handle of sc_attention_create."""
+
+    def __init__(self, handle):
+        self.handle = handle
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            try:
+                _lib.sc_attention_destroy(self.handle)
+            except Exception:  # interpreter shutdown
+                pass
+            self.handle = None
+
+
+def attention_create(dtype: int, heads: int, kv_heads: int, head_dim: int, page_rows: int, causal=True, scale=0.0, rotary_freq=None,
+                     interleaved=False, rotary_dim=None) -> AttentionHandle:
+    """`rotary_freq`: angles per position of the rotated pairs; `rotary_dim`: 2 len(rotary_freq) unless given."""
+    d = AttentionDesc(int(dtype), int(heads), int(kv_heads), int(head_dim), int(page_rows), int(causal), float(scale))
+    freq = np.ascontiguousarray(rotary_freq if rotary_freq is not None else [], dtype=np.float64)
+    d.rotary_dim = 2 * freq.size if rotary_dim is None else int(rotary_dim)
+    d.rotary_interleaved = int(interleaved)
+    if freq.size:
+        d.rotary_freq = freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+    h = ctypes.c_void_p()
+    _check(lib().sc_attention_create(ctypes.byref(h), ctypes.byref(d)), "sc_attention_create")
+    return AttentionHandle(h)
+
+
+def attention_workspace_bytes(attention: AttentionHandle) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().sc_attention_workspace_bytes(attention.handle, ctypes.byref(n)), "sc_attention_workspace_bytes")
+    return int(n.value)
+
+
+def attention_describe(attention: AttentionHandle) -> str:
+    buf = ctypes.create_string_buffer(2048)
+    _check(lib().sc_attention_describe(attention.handle, buf, ctypes.c_size_t(len(buf))), "sc_attention_describe")
+    return buf.value.decode()
+
+
+# The operators take records: bytes of pack_rows / pack_cache / pack_sequences, or None.
+def attention_append(attention: AttentionHandle, sequences, q, k, v, q_out, cache, stream=0):
+    _check(lib().sc_attention_append(attention.handle, sequences, q, k, v, q_out, cache, stream), "sc_attention_append")
+
+
+def attention_prompt(attention: AttentionHandle, sequences, q, k, v, out, stream=0):
+    _check(lib().sc_attention_prompt(attention.handle, sequences, q, k, v, out, stream), "sc_attention_prompt")
+
+
+def attention_prompt_paged(attention: AttentionHandle, sequences, q, cache, out, stream=0):
+    _check(lib().sc_attention_prompt_paged(attention.handle, sequences, q, cache, out, stream), "sc_attention_prompt_paged")
+
+
+def attention_decode(attention: AttentionHandle, sequences, q, cache, out, workspace, workspace_bytes, stream=0):
+    _check(lib().sc_attention_decode(attention.handle, sequences, q, cache, out, workspace, workspace_bytes, stream), "sc_attention_decode")

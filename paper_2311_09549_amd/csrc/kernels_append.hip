@@ -1,0 +1,116 @@
+// Append: new rows of keys and values into the pages of their sequences, queries and keys rotated by their positions on the way.
+//
+// A row is moved once, heads + 2 kv_heads heads in and as many out, and pairs / head_dim of it turned: nothing but memory traffic, or,
+// for the few rows of a decoding step, the latency of a launch and of three dependent reads (row start, length, page number).  A workgroup
+// takes one row: all its heads turn by the same angles, so it takes their sines and cosines once, into LDS.
+#include "attention.h"
+
+namespace sck {
+
+namespace {
+
+constexpr int kAppendThreads = 256;
+
+template <typename E, int N>
+struct alignas(sizeof(E) * N < 16 ? sizeof(E) * N : 16) Vec {
+    E v[N];
+};
+
+template <typename E, int N>
+__device__ __forceinline__ Vec<E, N> load(const E *p) { return *reinterpret_cast<const Vec<E, N> *>(p); }
+template <typename E, int N>
+__device__ __forceinline__ void store(E *p, const Vec<E, N> &x) { *reinterpret_cast<Vec<E, N> *>(p) = x; }
+
+// E: element, N: elements of a vector; N divides the pairs of a row where its pairs are half a rotation apart, and whatever is not rotated.
+template <typename E, int N, bool INTERLEAVED>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a)
+{
+    __shared__ float cos_s[kMaxPairs], sin_s[kMaxPairs];
+    const int32_t row = blockIdx.x, b = sequence_of(a.s, row);
+    if (b < 0) return;
+    const int32_t begin = row_begin(a.s, b), count = row_begin(a.s, b + 1) - begin;
+    const int64_t position = (int64_t)a.s.length[b] - count + (row - begin);
+    for (int t = threadIdx.x; t < a.pairs; t += kAppendThreads) {
+        const double x = (double)position * a.turns[t];
+        float c, s;
+        sincospif(2.0f * (float)(x - rint(x)), &s, &c);
+        cos_s[t] = c;
+        sin_s[t] = s;
+    }
+    // row of the cache, or none
+    int32_t page = -1;
+    if (position >= 0 && position < table_room(a.s)) page = page_of(a.s, b, (int32_t)position);
+    const int64_t at = page < 0 ? -1 : page * a.cache.page + ((int32_t)position & ((1 << a.s.page_shift) - 1)) * a.cache.row;
+    __syncthreads();
+
+    // vectors of a rotated head: pairs of vectors half a rotation apart (or vectors of pairs), then the rest of the row
+    const int turned = INTERLEAVED ? a.head_dim / N : a.pairs / N, plain = INTERLEAVED ? 0 : (a.head_dim - 2 * a.pairs) / N, per_head = turned + plain;
+    const int whole = a.head_dim / N;
+    const int n_rotated = (a.heads + a.kv_heads) * per_head, n = n_rotated + a.kv_heads * whole;
+    for (int x = threadIdx.x; x < n; x += kAppendThreads) {
+        if (x >= n_rotated) {
+            const int y = x - n_rotated, h = y / whole, e = y % whole * N;
+            const Vec<E, N> v = load<E, N>(static_cast<const E *>(a.v.data) + row * a.v.row + h * a.v.head + e);
+            if (at >= 0) store(static_cast<E *>(a.cache.values) + at + h * a.cache.head + e, v);
+            continue;
+        }
+        const int head = x / per_head, y = x % per_head, h = head - a.heads;
+        const E *src = head < a.heads ? static_cast<const E *>(a.q.data) + row * a.q.row + head * a.q.head : static_cast<const E *>(a.k.data) + row * a.k.row + h * a.k.head;
+        E *dst = head < a.heads ? static_cast<E *>(a.q_out.data) + row * a.q_out.row + head * a.q_out.head : static_cast<E *>(a.cache.keys) + at + h * a.cache.head;
+        const bool kept = head < a.heads || at >= 0;
+        if constexpr (INTERLEAVED) {
+            const int e = y * N;
+            Vec<E, N> v = load<E, N>(src + e);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const int t = e / 2 + i / 2;
+                if (t >= a.pairs) continue;
+                const float c = cos_s[t], s = sin_s[t], p = (float)v.v[i], q = (float)v.v[i + 1];
+                v.v[i] = (E)(p * c - q * s);
+                v.v[i + 1] = (E)(q * c + p * s);
+            }
+            if (kept) store(dst + e, v);
+        } else if (y < turned) {
+            const int e = y * N;
+            Vec<E, N> v = load<E, N>(src + e), w = load<E, N>(src + a.pairs + e);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float c = cos_s[e + i], s = sin_s[e + i], p = (float)v.v[i], q = (float)w.v[i];
+                v.v[i] = (E)(p * c - q * s);
+                w.v[i] = (E)(q * c + p * s);
+            }
+            if (kept) {
+                store(dst + e, v);
+                store(dst + a.pairs + e, w);
+            }
+        } else {
+            const int e = 2 * a.pairs + (y - turned) * N;
+            const Vec<E, N> v = load<E, N>(src + e);
+            if (kept) store(dst + e, v);
+        }
+    }
+}
+
+template <typename E>
+void launch_typed(const AppendArgs &a, hipStream_t stream)
+{
+    const int blocks = a.s.rows;
+    // the widest vector that halves of a rotation and the rest of a row are whole numbers of
+    if (a.interleaved) append_kernel<E, 8, true><<<blocks, kAppendThreads, 0, stream>>>(a);
+    else if (a.pairs % 8 == 0) append_kernel<E, 8, false><<<blocks, kAppendThreads, 0, stream>>>(a);
+    else if (a.pairs % 4 == 0) append_kernel<E, 4, false><<<blocks, kAppendThreads, 0, stream>>>(a);
+    else if (a.pairs % 2 == 0) append_kernel<E, 2, false><<<blocks, kAppendThreads, 0, stream>>>(a);
+    else append_kernel<E, 1, false><<<blocks, kAppendThreads, 0, stream>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendArgs &a, sc_dtype dtype, hipStream_t stream)
+{
+    if (dtype == SC_BF16) launch_typed<__bf16>(a, stream);
+    else if (dtype == SC_F16) launch_typed<_Float16>(a, stream);
+    else launch_typed<float>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace sck

@@ -1,0 +1,112 @@
+// Prompt: attention of the rows of packed sequences over their keys, packed as well or in the pages of a cache.
+//
+// One pass over the keys with the running maximum and sum of each row; scores and weights stay in registers.  A workgroup has four
+// wavefronts of 16 rows of one head; each goes through the keys that its rows see by itself.
+#include "attention_device.h"
+
+namespace sck {
+
+namespace {
+
+constexpr int kPromptRows = 64;
+
+template <typename TR, int DP, bool EXACT, bool PAGED>
+__global__ void __launch_bounds__(256) prompt_kernel(AttendArgs a)
+{
+    using W = Wave<TR, DP, EXACT>;
+    constexpr int B = TR::kBytes, TILES = W::TILES;
+    const int32_t head = blockIdx.y, kv = head / a.group;
+    const RowBlock blk = row_block<kPromptRows>(a.s, blockIdx.x);
+    if (blk.sequence < 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int32_t first = blk.first + wave * 16, end = blk.end < first + 16 ? blk.end : first + 16;   // rows of the wavefront
+    if (first >= end) return;
+    const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
+
+    W w;
+    w.init(threadIdx.x % 64, a.head_dim);
+    const int32_t row = first + w.col;
+    char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * B;
+    if (length < 0) {
+        if (row < end) w.store(out, __builtin_nanf(""));   // no sums yet: 0 * NaN
+        return;
+    }
+    w.load_q(static_cast<const char *>(a.q.data) + ((row < end ? row : first) * a.q.row + head * a.q.head) * B, row < end);
+
+    // keys that a row sees: none but those up to its own position
+    const int32_t before = length - blk.count - blk.begin + 1;
+    const auto sees = [&](int32_t r) {
+        const int32_t n = a.causal ? before + r : length;
+        return n < 0 ? 0 : n;
+    };
+    const int32_t visible = row < end ? sees(row) : 0, all = sees(first), most = sees(end - 1);
+    const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * B, v_row = (PAGED ? a.cache.row : a.v.row) * B;
+    const char *k0 = PAGED ? static_cast<const char *>(a.cache.keys) + kv * a.cache.head * B
+                           : static_cast<const char *>(a.k.data) + (blk.begin * a.k.row + kv * a.k.head) * B;
+    const char *v0 = PAGED ? static_cast<const char *>(a.cache.values) + kv * a.cache.head * B
+                           : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head) * B;
+    bool bad = false;
+    for (int32_t base = 0; base < most; base += W::KEYS) {
+        KeyTile t[TILES];
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) {
+            int32_t at = base + 16 * n;
+            if (at >= length) at = base;   // nothing of it is seen: any rows that are there
+            t[n].last = length - 1 - at;
+            if (PAGED) {
+                int32_t page = page_of(a.s, blk.sequence, at);
+                bad |= page < 0;
+                if (page < 0) page = 0;
+                const int64_t off = (page * a.cache.page + (at & ((1 << a.s.page_shift) - 1)) * a.cache.row) * B;
+                t[n].k = k0 + off;
+                t[n].v = v0 + off;
+            } else {
+                t[n].k = k0 + at * k_row;
+                t[n].v = v0 + at * v_row;
+            }
+        }
+        typename W::Keys keys;
+        typename W::Values values;
+        w.load_keys(keys, t, k_row);
+        w.load_values(values, t, v_row);
+        if (base + W::KEYS <= all) w.template step<false>(keys, values, a.scale_log2, 0);
+        else w.template step<true>(keys, values, a.scale_log2, visible - base);
+    }
+    const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
+    if (row < end) w.store(out, l == 0.0f ? 0.0f : 1.0f / l);
+}
+
+template <typename TR, int DP>
+void launch_padded(const AttendArgs &a, bool paged, hipStream_t stream)
+{
+    const dim3 grid(row_blocks<kPromptRows>(a.s.rows, a.s.batch), a.heads);
+    const bool exact = a.head_dim == DP;
+    if (paged) {
+        if (exact) prompt_kernel<TR, DP, true, true><<<grid, 256, 0, stream>>>(a);
+        else prompt_kernel<TR, DP, false, true><<<grid, 256, 0, stream>>>(a);
+    } else {
+        if (exact) prompt_kernel<TR, DP, true, false><<<grid, 256, 0, stream>>>(a);
+        else prompt_kernel<TR, DP, false, false><<<grid, 256, 0, stream>>>(a);
+    }
+}
+
+template <typename TR>
+void launch_typed(const AttendArgs &a, bool paged, hipStream_t stream)
+{
+    const int dp = padded_dim(a.head_dim);
+    if (dp == 64) launch_padded<TR, 64>(a, paged, stream);
+    else if (dp == 128) launch_padded<TR, 128>(a, paged, stream);
+    else launch_padded<TR, 256>(a, paged, stream);
+}
+
+}  // namespace
+
+hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream)
+{
+    if (dtype == SC_BF16) launch_typed<Bf16>(a, paged, stream);
+    else if (dtype == SC_F16) launch_typed<F16>(a, paged, stream);
+    else launch_typed<F32>(a, paged, stream);
+    return hipGetLastError();
+}
+
+}  // namespace sck
