@@ -26,6 +26,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kMinusInf = -__builtin_inff();
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
 struct Bf16 {
     using elem = __bf16;
     static constexpr int kBytes = 2, kTiles = 2;
@@ -40,6 +43,10 @@ struct Bf16 {
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 };
 
@@ -57,6 +64,10 @@ struct F16 {
     static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
 };
 
@@ -90,6 +101,27 @@ __device__ __forceinline__ float finite_max(float m) { return m == kMinusInf ? 0
 struct KeyTile {
     const char *k, *v;
     int last;
+};
+
+// Infinities and NaN among the elements of a word, both halves of it (16-bit types) at a time.
+template <typename TR>
+struct Special {
+    static constexpr int B = TR::kBytes;
+    static constexpr uint32_t both(uint32_t x) { return B == 2 ? x * 0x10001u : x; }
+    static constexpr int kTop = 8 * B - 1;   // sign bit of an element
+    static __device__ __forceinline__ uint32_t infinite_or_nan(uint32_t x)   // 1 in each element that is
+    {
+        constexpr uint32_t lowest = TR::kMantissa + 1;   // of the exponent's bits: all of them set carry into the sign's
+        return ((x & both(TR::kExponent)) + both(lowest)) >> kTop & both(1);
+    }
+    static __device__ __forceinline__ uint32_t indicator(uint32_t x, int kind)   // 1.0 in each element of that kind
+    {
+        const uint32_t out = infinite_or_nan(x), negative = x >> kTop & both(1);
+        uint32_t nan = ((x & both(TR::kMantissa)) + both(TR::kMantissa)) & both(TR::kMantissa + 1);   // a mantissa that is not 0 carries
+        nan = nan >> (__builtin_ctz(TR::kMantissa + 1)) & out;
+        return (kind == 0 ? out & ~nan & ~negative : kind == 1 ? out & ~nan & negative : nan) * TR::kOne;
+    }
+    static __device__ __forceinline__ uint32_t without(uint32_t x) { return x & ~(infinite_or_nan(x) * (B == 2 ? 0xffffu : 0xffffffffu)); }   // 0 in their place
 };
 
 // Wave's state for 16 query rows.  DP: head_dim padded (64, 128, 256); EXACT: head_dim == DP.
@@ -201,28 +233,13 @@ struct Wave {
 
     // Infinities and NaN among values that some query of the step does not see: the product would spread them to it (0 times infinity).
     // They are taken out of x; queries that see one get it from a product of indicators, one for each of +infinity, -infinity, NaN.
-    // Bits of both halves of a word (16-bit types) at a time.
-    static constexpr uint32_t both(uint32_t x) { return B == 2 ? x * 0x10001u : x; }
-    static constexpr int kTop = 8 * B - 1;   // sign bit of an element
-    static __device__ __forceinline__ uint32_t infinite_or_nan(uint32_t x)   // 1 in each element that is
-    {
-        constexpr uint32_t lowest = TR::kMantissa + 1;   // of the exponent's bits: all of them set carry into the sign's
-        return ((x & both(TR::kExponent)) + both(lowest)) >> kTop & both(1);
-    }
-    static __device__ __forceinline__ uint32_t indicator(uint32_t x, int kind)   // 1.0 in each element of that kind
-    {
-        const uint32_t out = infinite_or_nan(x), negative = x >> kTop & both(1);
-        uint32_t nan = ((x & both(TR::kMantissa)) + both(TR::kMantissa)) & both(TR::kMantissa + 1);   // a mantissa that is not 0 carries
-        nan = nan >> (__builtin_ctz(TR::kMantissa + 1)) & out;
-        return (kind == 0 ? out & ~nan & ~negative : kind == 1 ? out & ~nan & negative : nan) * TR::kOne;
-    }
     __device__ __forceinline__ void part_infinities(Values &x, int visible)
     {
         uint32_t any = 0;
 #pragma unroll
         for (int j = 0; j < TILES * 4; ++j)
 #pragma unroll
-            for (int w = 0; w < VW; ++w) any |= infinite_or_nan(x.v[j][w]);
+            for (int w = 0; w < VW; ++w) any |= Special<TR>::infinite_or_nan(x.v[j][w]);
         if (!__any(any != 0)) return;
         const f32x4 none = {0, 0, 0, 0};
         uint32_t one[TILES * 4];
@@ -243,7 +260,7 @@ struct Wave {
                 f32x4 n = none;
                 u32x4 is;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) is[h] = indicator(y[h], kind);
+                for (int h = 0; h < 4; ++h) is[h] = Special<TR>::indicator(y[h], kind);
                 if constexpr (B == 2) {
                     n = TR::mfma(is, u32x4{one[0] | one[1] << 16, one[2] | one[3] << 16, one[4] | one[5] << 16, one[6] | one[7] << 16}, none);
                 } else {
@@ -260,7 +277,7 @@ struct Wave {
 #pragma unroll
         for (int j = 0; j < TILES * 4; ++j)
 #pragma unroll
-            for (int w = 0; w < VW; ++w) x.v[j][w] &= ~(infinite_or_nan(x.v[j][w]) * (B == 2 ? 0xffffu : 0xffffffffu));
+            for (int w = 0; w < VW; ++w) x.v[j][w] = Special<TR>::without(x.v[j][w]);
     }
     // What was computed from x before is not kept for later.
     static __device__ __forceinline__ void fresh(Values &x)

@@ -2,7 +2,9 @@
 //
 // One pass over the keys with the running maximum and sum of each row; scores and weights stay in registers.  A workgroup has four
 // wavefronts of 16 rows of one head; each goes through the keys that its rows see by itself.
-#include "attention_device.h"
+#include <type_traits>
+
+#include "prompt_tile.h"
 
 namespace sck {
 
@@ -76,27 +78,38 @@ __global__ void __launch_bounds__(256) prompt_kernel(AttendArgs a)
     if (row < end) w.store(out, l == 0.0f ? 0.0f : 1.0f / l);
 }
 
-template <typename TR, int DP>
-void launch_padded(const AttendArgs &a, bool paged, hipStream_t stream)
+template <typename TR, int DP, bool PAGED>
+void launch_padded(const AttendArgs &a, hipStream_t stream)
 {
-    const dim3 grid(row_blocks<kPromptRows>(a.s.rows, a.s.batch), a.heads);
-    const bool exact = a.head_dim == DP;
-    if (paged) {
-        if (exact) prompt_kernel<TR, DP, true, true><<<grid, 256, 0, stream>>>(a);
-        else prompt_kernel<TR, DP, false, true><<<grid, 256, 0, stream>>>(a);
+    if constexpr (TR::kBytes == 2) {
+        constexpr int NW = DP == 256 ? 4 : 8, KT = DP == 256 ? 32 : 64;
+        int heads_log2 = 0;
+        while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
+        const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch;
+        const uint32_t grid = (uint32_t)(blocks * (a.heads >> heads_log2));
+        if (a.scale_log2 > 1.0f) prompt_tile_kernel<TR, DP, PAGED, true, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
+        else prompt_tile_kernel<TR, DP, PAGED, false, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
     } else {
-        if (exact) prompt_kernel<TR, DP, true, false><<<grid, 256, 0, stream>>>(a);
-        else prompt_kernel<TR, DP, false, false><<<grid, 256, 0, stream>>>(a);
+        const dim3 grid(row_blocks<kPromptRows>(a.s.rows, a.s.batch), a.heads);
+        if (a.head_dim == DP) prompt_kernel<TR, DP, true, PAGED><<<grid, 256, 0, stream>>>(a);
+        else prompt_kernel<TR, DP, false, PAGED><<<grid, 256, 0, stream>>>(a);
     }
+}
+
+template <typename TR, bool PAGED>
+void launch_typed(const AttendArgs &a, hipStream_t stream)
+{
+    const int dp = padded_dim(a.head_dim);
+    if (dp == 64) launch_padded<TR, 64, PAGED>(a, stream);
+    else if (dp == 128) launch_padded<TR, 128, PAGED>(a, stream);
+    else launch_padded<TR, 256, PAGED>(a, stream);
 }
 
 template <typename TR>
 void launch_typed(const AttendArgs &a, bool paged, hipStream_t stream)
 {
-    const int dp = padded_dim(a.head_dim);
-    if (dp == 64) launch_padded<TR, 64>(a, paged, stream);
-    else if (dp == 128) launch_padded<TR, 128>(a, paged, stream);
-    else launch_padded<TR, 256>(a, paged, stream);
+    if (paged) launch_typed<TR, true>(a, stream);
+    else launch_typed<TR, false>(a, stream);
 }
 
 }  // namespace

@@ -1,0 +1,283 @@
+// Prompt attention of 16-bit types: tiles of keys and values in LDS, shared by the wavefronts of a workgroup.
+//
+// A wavefront has 32 query rows of one head; a workgroup NW of them, which share the keys of one key head: as many of the
+// heads of that key head as there are (1, 2, 4 or 8), and rows of them one behind the other.  Both products are transposed as in
+// attention_device.h, on v_mfma 32x32x16: S^T = K Q^T, O^T = V^T P^T.  A lane (q = lane % 32, half = lane / 32) holds of query q the scores
+// with keys 8 (r / 4) + 4 half + r % 4 of each 32, r = 0..15, and eight of them in a row, as they are, are its operand of a step of the
+// second product, whose 16 keys are then taken in the order 4 half + 0..3, 8 + 4 half + 0..3.  Values are read from LDS in that order by
+// transposing reads (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 elements and get 4 rows of one element each).
+//
+// Rows of a tile are whole rows of the head; their 16-byte pieces are exchanged within a row (exclusive or with bits of the
+// row number), so that the 32 rows that a read of keys touches, and the 4 of a transposing read, lie in different banks.
+//
+// The maximum that weights are taken against is raised only where a score passes it by more than 2^8: sums are rescaled a few times a row instead of at
+// every new maximum, and weights up to 2^8 lose nothing.
+#pragma once
+
+#include "attention_device.h"
+
+namespace sck {
+
+template <typename TR, int DP, int NW, int KT>
+struct PromptTile {
+    static constexpr int THREADS = 64 * NW, CHUNKS = DP / 8, DT = DP / 32, NT = KT / 32;   // pieces of a row, tiles of the head, tiles of keys
+    static constexpr int LOADS = KT * CHUNKS / THREADS, ROWS_PER_LOAD = THREADS / CHUNKS;
+    static constexpr int ROW_BYTES = DP * 2, TILE_BYTES = KT * ROW_BYTES, LDS_BYTES = 4 * TILE_BYTES;
+    static constexpr float kRaise = 8.0f;
+    static constexpr float kLift = TR::kLift > 0.0f ? TR::kLift - kRaise + 1.0f : 0.0f;   // fp16: weights up to 2^15
+    static_assert(KT * CHUNKS % THREADS == 0 && ROWS_PER_LOAD * CHUNKS == THREADS, "whole rows per load");
+
+    // Place of piece c of row r.
+    static __device__ __forceinline__ int key_piece(int r, int c)
+    {
+        if constexpr (CHUNKS >= 16) return c ^ (r & 15);
+        else return c ^ ((r & 7) ^ (r >> 3 & 1));
+    }
+    static __device__ __forceinline__ int value_piece(int r, int c)
+    {
+        if constexpr (CHUNKS >= 16) return c ^ ((r & 1) << 1 | (r & 2) << 1 | (r & 1) << 3);
+        else return c ^ ((r & 2) << 1 | (r & 1) << 1);
+    }
+};
+
+// FAR: the maximum times scale_log2 may be beyond fp32 (a scale above ln 2), so that differences are taken before they are scaled.
+template <typename TR, int DP, bool PAGED, bool FAR, int NW, int KT>
+__global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
+{
+    using P = PromptTile<TR, DP, NW, KT>;
+    constexpr int CHUNKS = P::CHUNKS, DT = P::DT, NT = P::NT, LOADS = P::LOADS;
+    __shared__ __attribute__((aligned(16))) char tile_s[P::LDS_BYTES];   // [buffer][keys, values]
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), q = lane % 32, half = lane / 32;
+
+    // Blocks of a key head follow each other at a distance that is a multiple of the number of its XCD, where that is one, and share that
+    // one's L2; the last rows of a sequence, which see most keys, come first.
+    const int32_t head_groups = a.heads >> heads_log2;
+    const int32_t head0 = blockIdx.x % head_groups << heads_log2, kv = head0 / a.group;
+    const int32_t blocks = gridDim.x / head_groups, number = blocks - 1 - blockIdx.x / head_groups;
+    constexpr int R = 32 * NW;
+    const RowBlock blk = heads_log2 == 0 ? row_block<R>(a.s, number) : heads_log2 == 1 ? row_block<R / 2>(a.s, number) : heads_log2 == 2 ? row_block<R / 4>(a.s, number) : row_block<R / 8>(a.s, number);
+    if (blk.sequence < 0) return;
+    const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
+    const int32_t head = head0 + (wave & ((1 << heads_log2) - 1)), first = blk.first + 32 * (wave >> heads_log2), row = first + q;
+    const bool mine = row < blk.end;
+    char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
+    if (length < 0) {
+        if (mine)
+            for (int d = 8 * half; d < a.head_dim; d += 16) *reinterpret_cast<u32x4 *>(out + 2 * d) = u32x4{0, 0, 0, 0} + TR::kExponent * 0x10001u + 0x00010001u;
+        return;
+    }
+
+    // keys that a row sees: none but those up to its own position
+    const int32_t before = length - blk.count - blk.begin + 1;
+    const auto sees = [&](int32_t r) {
+        const int32_t n = a.causal ? before + r : length;
+        return n < 0 ? 0 : n;
+    };
+    const int32_t block_most = sees(blk.end - 1);
+    const int32_t visible = mine ? sees(row) : 0;
+    const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
+
+    u32x4 qf[DP / 16];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        qf[c] = u32x4{0, 0, 0, 0};
+        const int e = (2 * c + half) * 8;
+        if (mine && e < a.head_dim) qf[c] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q.data) + (row * a.q.row + head * a.q.head + e) * 2);
+    }
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    float m = kMinusInf, l = 0.0f, from = 0.0f;   // from: what weights are taken against, the maximum (FAR) or its product with scale_log2
+
+    // this thread's pieces of a tile
+    const int piece = threadIdx.x % CHUNKS, row0 = threadIdx.x / CHUNKS;
+    const bool held = piece * 8 < a.head_dim;
+    const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * 2, v_row = (PAGED ? a.cache.row : a.v.row) * 2;
+    const char *k0 = PAGED ? static_cast<const char *>(a.cache.keys) + (kv * a.cache.head + piece * 8) * 2
+                           : static_cast<const char *>(a.k.data) + (blk.begin * a.k.row + kv * a.k.head + piece * 8) * 2;
+    const char *v0 = PAGED ? static_cast<const char *>(a.cache.values) + (kv * a.cache.head + piece * 8) * 2
+                           : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head + piece * 8) * 2;
+    bool bad = false;
+    u32x4 ks[LOADS], vs[LOADS];
+    const auto fetch = [&](int32_t base) {
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) {
+            int32_t key = base + row0 + n * P::ROWS_PER_LOAD;
+            key = key < length ? key : length - 1;   // rows behind the last key are seen by none: any that are there
+            int64_t k_at = key * k_row, v_at = key * v_row;
+            if (PAGED) {
+                int32_t page = page_of(a.s, blk.sequence, key);
+                bad |= page < 0;
+                if (page < 0) page = 0;
+                k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
+            }
+            ks[n] = vs[n] = u32x4{0, 0, 0, 0};
+            if (held) {
+                ks[n] = *reinterpret_cast<const u32x4 *>(k0 + k_at);
+                vs[n] = *reinterpret_cast<const u32x4 *>(v0 + v_at);
+            }
+        }
+    };
+    // Tiles that some rows see in part are stored without infinities and NaN among the values, which the product would spread to rows that do not see them
+    // (0 times infinity); the answer is whether there were any.
+    const auto put = [&](char *buffer, bool part) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) {
+            const int r = row0 + n * P::ROWS_PER_LOAD;
+            if (part) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    any |= Special<TR>::infinite_or_nan(vs[n][i]);
+                    vs[n][i] = Special<TR>::without(vs[n][i]);
+                }
+            }
+            *reinterpret_cast<u32x4 *>(buffer + r * P::ROW_BYTES + 16 * P::key_piece(r, piece)) = ks[n];
+            *reinterpret_cast<u32x4 *>(buffer + P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, piece)) = vs[n];
+        }
+        return any != 0;
+    };
+    // They are added to the rows that see them, from memory.
+    const auto add_special = [&](int32_t base) {
+#pragma unroll 1
+        for (int32_t key = base; key < base + KT && key < most; ++key) {
+            const char *p = static_cast<const char *>(PAGED ? a.cache.values : a.v.data);
+            if (PAGED) {
+                const int32_t page = page_of(a.s, blk.sequence, key);
+                p += ((page < 0 ? 0 : page) * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + kv * a.cache.head) * 2;
+            } else {
+                p += ((blk.begin + key) * a.v.row + kv * a.v.head) * 2;
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+                    if (key >= visible || e >= a.head_dim) continue;
+                    const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(p)[e];
+                    if ((__builtin_bit_cast(uint16_t, x) & TR::kExponent) == TR::kExponent) o[d][r] += (float)x;
+                }
+        }
+    };
+
+    // Where the lane reads, of the first buffer: pieces of the keys of its query's number, and its part of a transposing read.  The other rows of a tile are
+    // at constant distances, which are multiples of what the exchange of pieces goes by.
+    int k_at[DP / 16], v_at[DT];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) k_at[c] = q * P::ROW_BYTES + 16 * P::key_piece(q, 2 * c + half);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        const int r = 4 * half + lane % 16 / 4, c = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
+        v_at[d] = P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, c) + lane % 2 * 8;
+    }
+    typedef __attribute__((address_space(3))) char *Lds;
+    const auto tile = [&](Lds buffer, int32_t base, auto masked) {
+        constexpr bool MASK = decltype(masked)::value;
+        f32x16 s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                s[t] = TR::mfma32(*(__attribute__((address_space(3))) u32x4 *)(buffer + k_at[c] + 32 * t * P::ROW_BYTES), qf[c], s[t]);
+            }
+        }
+        float top = kMinusInf;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (MASK) s[t][r] = 32 * t + 8 * (r / 4) + 4 * half + r % 4 < visible - base ? s[t][r] : kMinusInf;
+                top = fmaxf(top, s[t][r]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any((top - m) * a.scale_log2 > P::kRaise)) {
+            const float next = fmaxf(m, top), base_next = finite_max(next);
+            const float shrink = __builtin_amdgcn_exp2f((m - base_next) * a.scale_log2);
+            m = next;
+            from = FAR ? base_next : base_next * a.scale_log2;
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+        }
+        const float minus = P::kLift - from;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = __builtin_amdgcn_exp2f(FAR ? __builtin_fmaf(s[t][r] - from, a.scale_log2, P::kLift) : __builtin_fmaf(s[t][r], a.scale_log2, minus));
+        u32x4 w[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                l += s[t][r] + s[t][r + 1];
+                w[t][r / 8][r / 2 % 4] = TR::pack(s[t][r], s[t][r + 1]);
+            }
+
+        // operand of tile d of the head and keys 32 t + 16 n + ..
+        const auto values = [&](int d, int t, int n) {
+            u32x4 y;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Lds p = buffer + v_at[d] + (32 * t + 16 * n + 8 * h) * P::ROW_BYTES;
+                const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p));
+                y[2 * h] = z.x;
+                y[2 * h + 1] = z.y;
+            }
+            return y;
+        };
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = TR::mfma32(values(d, t, n), w[t][n], o[d]);
+    };
+
+    if (block_most > 0) {
+        const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
+        fetch(0);
+        bool special = __syncthreads_or(put(tile_s, KT > block_all));
+        int buffer = 0;
+        int32_t base = 0;
+        const auto pass = [&](auto masked) {
+            constexpr bool MASK = decltype(masked)::value;
+            const bool more = base + KT < block_most, part = MASK || base + 2 * KT > block_all;
+            if (more) fetch(base + KT);
+            if (!MASK || base < most) {
+                tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked);
+                if (MASK && special) add_special(base);
+            }
+            buffer ^= 1;
+            bool any = false;
+            if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
+            if (part) special = __syncthreads_or(any);
+            else __syncthreads();
+            base += KT;
+        };
+        // tiles that every row of the block sees whole, then the others
+        while (base + KT <= block_all) pass(std::false_type());
+        while (base < block_most) pass(std::true_type());
+    }
+    if (PAGED) bad = __syncthreads_or(bad);
+    l += __shfl_xor(l, 32);
+    const float factor = PAGED && bad ? __builtin_nanf("") : l == 0.0f ? 0.0f : 1.0f / l;
+    if (mine) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int e = 32 * d + 2 * r + 4 * half;
+                if (e < a.head_dim)
+                    *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[d][r] * factor, o[d][r + 1] * factor), TR::pack(o[d][r + 2] * factor, o[d][r + 3] * factor)};
+            }
+    }
+}
+
+}  // namespace sck
