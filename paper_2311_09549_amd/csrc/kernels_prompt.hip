@@ -82,7 +82,7 @@ template <typename TR, int DP, bool PAGED>
 void launch_padded(const AttendArgs &a, hipStream_t stream)
 {
     if constexpr (TR::kBytes == 2) {
-        constexpr int NW = DP == 256 ? 4 : 8, KT = DP == 256 ? 32 : 64;
+        constexpr int NW = DP == 256 ? 4 : 8, KT = DP == 256 ? 32 : 128;
         int heads_log2 = 0;
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch;
