@@ -366,7 +366,7 @@ typedef struct {
  * length = NULL (packed keys): as many as its rows.  Key j of sequence b is row j % page_rows of page
  * page[b * page_ld + j / page_rows]; a sequence has page_count entries, of which those that length[b] reaches are read.
  * Device memory all of it.  Kernels take row starts as if clamped to 0..rows; rows of no sequence are neither read nor written.  At most 2^24 - 1
- * rows and 2^20 - 1 sequences. */
+ * rows, 2^20 - 1 sequences and 2^30 keys of one (more are a wrong length). */
 typedef struct {
     int32_t batch;
     int64_t rows;

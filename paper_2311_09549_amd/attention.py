@@ -18,6 +18,8 @@ from . import binding as sc
 
 _DTYPES = {torch.bfloat16: sc.SC_BF16, torch.float16: sc.SC_F16, torch.float32: sc.SC_F32}
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 
 class Attention:
     """The operators for one head layout.  Holds the workspace of `decode`: calls of one Attention are to be queued on one stream, or
@@ -38,11 +40,14 @@ class Attention:
         if rotary_dim and 2 * len(rotary_freq) != rotary_dim and rotary_dim % 2 == 0:
             raise ValueError("rotary_freq has one angle for each pair of rotary_dim")
         self.heads, self.kv_heads, self.head_dim, self.page_rows, self.dtype = heads, kv_heads, head_dim, page_rows, dtype
+        self._page = (page_rows, kv_heads, head_dim)
         self.handle = sc.attention_create(_DTYPES[dtype], heads, kv_heads, head_dim, page_rows, causal, 0.0 if scale is None else scale,
                                           rotary_freq, interleaved, rotary_dim)
         self.ws_bytes = sc.attention_workspace_bytes(self.handle)
         self.device = torch.device(device)
         self.workspace = None   # made by the first decode
+        self._h = self.handle.handle
+        self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
 
     def describe(self) -> str:
         return sc.attention_describe(self.handle)
@@ -50,80 +55,104 @@ class Attention:
     # -- operators ---------------------------------------------------------------------------------------------------------
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
         """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None."""
-        rows = k.shape[0]
+        rows = len(k)
         sequences, cache = self._sequences(rows, row_start, lengths, pages), self._cache(keys, values)
+        key, value = self._rows(k, rows, self.kv_heads), self._rows(v, rows, self.kv_heads)
+        query = result = None
         if q is not None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-            query, result = self._rows(q, rows, self.heads), self._rows(out, rows, self.heads)
-        else:
-            query = result = None
-        sc.attention_append(self.handle, sequences, query, self._rows(k, rows, self.kv_heads), self._rows(v, rows, self.kv_heads), result, cache,
-                            self._stream() if stream is None else stream)
+            query = self._rows(q, rows, self.heads)
+            out, result = self._out(q, out, rows)
+        self._append(self._h, sequences, query, key, value, result, cache, self._stream() if stream is None else stream)
         return out
 
     def prompt(self, q, k, v, row_start, out=None, stream=None):
         """Attention of the rows of each sequence over the keys and values of the same rows."""
-        rows = q.shape[0]
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        sc.attention_prompt(self.handle, self._sequences(rows, row_start), self._rows(q, rows, self.heads), self._rows(k, rows, self.kv_heads),
-                            self._rows(v, rows, self.kv_heads), self._rows(out, rows, self.heads), self._stream() if stream is None else stream)
+        rows = len(q)
+        query, key, value = self._rows(q, rows, self.heads), self._rows(k, rows, self.kv_heads), self._rows(v, rows, self.kv_heads)
+        out, result = self._out(q, out, rows)
+        self._prompt(self._h, self._sequences(rows, row_start), query, key, value, result, self._stream() if stream is None else stream)
         return out
 
     def prompt_paged(self, q, keys, values, pages, lengths, row_start, out=None, stream=None):
         """Attention of the last rows of each sequence over its keys in the cache."""
-        rows = q.shape[0]
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        sc.attention_prompt_paged(self.handle, self._sequences(rows, row_start, lengths, pages), self._rows(q, rows, self.heads),
-                                  self._cache(keys, values), self._rows(out, rows, self.heads), self._stream() if stream is None else stream)
+        rows = len(q)
+        query = self._rows(q, rows, self.heads)
+        out, result = self._out(q, out, rows)
+        self._prompt_paged(self._h, self._sequences(rows, row_start, lengths, pages), query, self._cache(keys, values), result,
+                           self._stream() if stream is None else stream)
         return out
 
     def decode(self, q, keys, values, pages, lengths, out=None, workspace=None, stream=None):
         """Attention of one row per sequence over all its keys in the cache.  `workspace`: device bytes of the caller's, `ws_bytes` of them."""
-        rows = q.shape[0]
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        if workspace is None:
+        rows = len(q)
+        query = self._rows(q, rows, self.heads)
+        out, result = self._out(q, out, rows)
+        if workspace is not None:
+            address, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        else:
             if self.workspace is None:
                 self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-            workspace = self.workspace
-        sc.attention_decode(self.handle, self._sequences(rows, None, lengths, pages), self._rows(q, rows, self.heads), self._cache(keys, values),
-                            self._rows(out, rows, self.heads), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                            self._stream() if stream is None else stream)
+            address, size = self.workspace.data_ptr(), self.ws_bytes
+        self._decode(self._h, self._sequences(rows, None, lengths, pages), query, self._cache(keys, values), result, address, size,
+                     self._stream() if stream is None else stream)
         return out
 
     # -- records -----------------------------------------------------------------------------------------------------------
+    # The host side of a call is most of the time of a short one: each attribute of a tensor is read once, and the messages are made apart.
     def _rows(self, x, rows, heads):
+        stride = x.stride()
+        if x.dtype is not self.dtype or not x.is_cuda or x.shape != (rows, heads, self.head_dim) or stride[2] != 1:
+            self._refuse_rows(x, rows, heads)
+        return sc.pack_rows(x.data_ptr(), stride[0], stride[1])
+
+    def _refuse_rows(self, x, rows, heads):
         if x.dtype is not self.dtype or not x.is_cuda:
             raise TypeError(f"rows have to be {self.dtype} on the GPU, not {x.dtype} on {x.device}")
-        row, head, element = x.stride()
-        if x.shape != (rows, heads, self.head_dim) or element != 1:
-            raise ValueError(f"rows have to be ({rows}, {heads}, {self.head_dim}) with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
-        return sc.pack_rows(x.data_ptr(), row, head)
+        raise ValueError(f"rows have to be ({rows}, {heads}, {self.head_dim}) with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
+
+    def _out(self, q, out, rows):
+        if out is not None:
+            return out, self._rows(out, rows, self.heads)
+        out = torch.empty_like(q)
+        stride = out.stride()
+        if stride[2] != 1 or 0 in stride:   # of heads that share their memory, or a single one
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            stride = out.stride()
+        return out, sc.pack_rows(out.data_ptr(), stride[0], stride[1])
 
     def _cache(self, keys, values):
+        shape, stride = keys.shape, keys.stride()
+        if (keys.dtype is not self.dtype or values.dtype is not self.dtype or not keys.is_cuda or not values.is_cuda or shape[1:] != self._page or stride[3] != 1
+                or values.shape != shape or values.stride() != stride):
+            self._refuse_cache(keys, values)
+        return sc.pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], stride[0], stride[1], stride[2])
+
+    def _refuse_cache(self, keys, values):
         if keys.dtype is not self.dtype or values.dtype is not self.dtype or not keys.is_cuda or not values.is_cuda:
             raise TypeError(f"the cache has to be {self.dtype} on the GPU, not {keys.dtype} and {values.dtype}")
-        shape, (page, row, head, element) = keys.shape, keys.stride()
-        if shape[1:] != (self.page_rows, self.kv_heads, self.head_dim) or element != 1 or values.shape != shape or values.stride() != keys.stride():
-            raise ValueError(f"keys and values have to be (pages, {self.page_rows}, {self.kv_heads}, {self.head_dim}) alike, with the last "
-                             f"dimension contiguous, not {tuple(shape)} and {tuple(values.shape)} with strides {keys.stride()} and {values.stride()}")
-        return sc.pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], page, row, head)
+        raise ValueError(f"keys and values have to be (pages, {self.page_rows}, {self.kv_heads}, {self.head_dim}) alike, with the last "
+                         f"dimension contiguous, not {tuple(keys.shape)} and {tuple(values.shape)} with strides {keys.stride()} and {values.stride()}")
 
     def _sequences(self, rows, row_start=None, lengths=None, pages=None):
-        batch = rows if row_start is None else row_start.shape[0] - 1
-        page_ld = columns = 0
-        for x, n in ((row_start, batch + 1), (lengths, batch)):
-            if x is not None and (x.dtype is not torch.int32 or not x.is_cuda or x.shape != (n,) or not x.is_contiguous()):
-                raise ValueError(f"row_start and lengths have to be contiguous int32 on the GPU, one length and row start per sequence ({batch}): got {x.dtype} {tuple(x.shape)}")
+        batch, starts, length, page, page_ld, columns = rows, 0, 0, 0, 0, 0
+        if row_start is not None:
+            batch = len(row_start) - 1
+            if row_start.dtype is not torch.int32 or not row_start.is_cuda or row_start.dim() != 1 or not row_start.is_contiguous() or batch < 0:
+                raise ValueError(f"row_start has to be contiguous int32 on the GPU, one number more than sequences: got {row_start.dtype} {tuple(row_start.shape)}")
+            starts = row_start.data_ptr()
+        if lengths is not None:
+            if lengths.dtype is not torch.int32 or not lengths.is_cuda or lengths.shape != (batch,) or not lengths.is_contiguous():
+                raise ValueError(f"lengths have to be contiguous int32 on the GPU, one for each of {batch} sequences: got {lengths.dtype} {tuple(lengths.shape)}")
+            length = lengths.data_ptr()
         if pages is not None:
-            if pages.dtype is not torch.int32 or not pages.is_cuda or pages.dim() != 2 or pages.shape[0] != batch or (pages.shape[1] > 1 and pages.stride(1) != 1):
-                raise ValueError(f"pages have to be int32 on the GPU, a row per sequence ({batch}): got {pages.dtype} {tuple(pages.shape)}")
-            page_ld, columns = pages.stride(0), pages.shape[1]
-        return sc.pack_sequences(batch, rows, 0 if row_start is None else row_start.data_ptr(), 0 if lengths is None else lengths.data_ptr(),
-                                 0 if pages is None else pages.data_ptr(), page_ld, columns)
+            shape, stride = pages.shape, pages.stride()
+            if pages.dtype is not torch.int32 or not pages.is_cuda or len(shape) != 2 or shape[0] != batch or (shape[1] > 1 and stride[1] != 1):
+                raise ValueError(f"pages have to be int32 on the GPU, a row for each of {batch} sequences: got {pages.dtype} {tuple(shape)}")
+            page, page_ld, columns = pages.data_ptr(), stride[0], shape[1]
+        return sc.pack_sequences(batch, rows, starts, length, page, page_ld, columns)
 
     def _stream(self):
         # torch's own accessor of the address alone: the stream object around it takes 2 us to make
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is None or self.device.index is None:
+        if _raw_stream is None or self.device.index is None:
             return torch.cuda.current_stream(self.device).cuda_stream
-        return raw(self.device.index)
+        return _raw_stream(self.device.index)

@@ -483,3 +483,20 @@ def attention_prompt_paged(attention: AttentionHandle, sequences, q, cache, out,
 
 def attention_decode(attention: AttentionHandle, sequences, q, cache, out, workspace, workspace_bytes, stream=0):
     _check(lib().sc_attention_decode(attention.handle, sequences, q, cache, out, workspace, workspace_bytes, stream), "sc_attention_decode")
+
+
+def attention_calls():
+    """The four operators above as functions of the same arguments (a handle's address first) that raise ScError by themselves: one call
+    less on the way of a step that is made for every layer and token."""
+    def of(name):
+        call = getattr(lib(), name)
+
+        def checked(status, _, __):
+            if status:
+                _check(status, name)
+            return status
+        prototype = ctypes.CFUNCTYPE(ctypes.c_int, *call.argtypes)
+        call = prototype((name, _lib))
+        call.errcheck = checked
+        return call
+    return tuple(of("sc_attention_" + name) for name in ("append", "prompt", "prompt_paged", "decode"))

@@ -14,9 +14,6 @@ using namespace sck;
 
 namespace {
 
-// Workgroups of decode per compute unit: see kernels_decode.hip.
-constexpr int kDecodePerCu = 3;
-
 int elem_size(sc_dtype t) { return t == SC_F32 ? 4 : 2; }
 
 bool aligned(const sc_attention *at, const void *p, int64_t s0, int64_t s1, int64_t s2 = 0)
@@ -146,8 +143,9 @@ extern "C" sc_status sc_attention_create(sc_attention **out, const sc_attention_
     } else {
         (void)hipGetLastError();
     }
-    at->decode_groups = at->n_cu * kDecodePerCu;
-    at->ws_bytes = sizeof(float) * 2 * (size_t)at->decode_groups * piece_floats(padded_dim(at->head_dim));
+    // workgroups of decode: the power of two from two a compute unit on (two wavefronts a SIMD are what its registers allow)
+    while (at->groups_log2 < kMaxGroupsLog2 && (1 << at->groups_log2) < 2 * at->n_cu) ++at->groups_log2;
+    at->ws_bytes = sizeof(float) * 2 * ((size_t)1 << at->groups_log2) * piece_floats(padded_dim(at->head_dim));
     *out = at;
     return SC_OK;
 }
@@ -173,7 +171,7 @@ extern "C" sc_status sc_attention_describe(const sc_attention *at, char *buf, si
              at->dtype == SC_F32 ? "f32" : at->dtype == SC_F16 ? "f16" : "bf16", at->heads, at->kv_heads, d, padded_dim(d), at->page_rows,
              at->causal ? "causal" : "not causal", at->scale_log2 * 0.6931471805599453, 2 * at->pairs, d,
              at->interleaved ? "adjacent pairs" : "pairs of halves", 2 * (at->heads + 2 * at->kv_heads) * d * e, 4 * at->heads * d, 2 * at->heads * d * e,
-             2 * at->kv_heads * d * e, 4 * at->heads * d, 2 * at->kv_heads * d * e, at->decode_groups, at->ws_bytes);
+             2 * at->kv_heads * d * e, 4 * at->heads * d, 2 * at->kv_heads * d * e, 1 << at->groups_log2, at->ws_bytes);
     return SC_OK;
 }
 
@@ -250,8 +248,9 @@ extern "C" sc_status sc_attention_decode(const sc_attention *at, const sc_sequen
     if (!workspace) return SC_ERR_NULL;
     if ((uintptr_t)workspace % 256) return SC_ERR_SHAPE_MISMATCH;
     if (!at->has_device) return SC_ERR_DEVICE;
-    a.groups = at->decode_groups;
+    a.groups_log2 = at->groups_log2;
     a.head_tiles = (a.group + kHeadTile - 1) / kHeadTile;
+    if (units_of((int32_t)std::min<int64_t>(table_room(a.s), INT32_MAX)) * (int64_t)a.s.batch >= kMaxUnits / ((int64_t)a.kv_heads * a.head_tiles)) return SC_ERR_BAD_DIMS;
     a.pieces = static_cast<float *>(workspace);
     return launched(launch_decode(a, at->dtype, (hipStream_t)hip_stream));
 }

@@ -17,7 +17,10 @@ constexpr int kMaxPairs = kMaxHeadDim / 2;
 constexpr int kHeadTile = 16;      // query heads of one key head that a wavefront of decode works on
 constexpr int kDecodeUnit = 128;   // keys: the grain of the split of decode
 constexpr int64_t kMaxRows = (1 << 24) - 1;
+constexpr int64_t kMaxUnits = (int64_t)1 << 52;   // of decode: 2^10 times as many fit what quotient() takes
+constexpr int32_t kMaxKeys = 1 << 30;   // of a sequence: a tile beyond the last one fits 32 bits
 constexpr int32_t kMaxBatch = (1 << 20) - 1;
+constexpr int32_t kMaxGroupsLog2 = 10;   // 2^n workgroups of decode at most
 
 // ------------------------------------------------------------------------------------------
 // sequences
@@ -47,7 +50,7 @@ ATTN_HD int64_t table_room(const Sequences &s) { return s.page_count << s.page_s
 ATTN_HD int32_t paged_length(const Sequences &s, int32_t b)
 {
     const int32_t n = s.length[b];
-    return n < 0 || n > table_room(s) ? -1 : n;
+    return n < 0 || n > table_room(s) || n > kMaxKeys ? -1 : n;
 }
 
 // Page of key j of sequence b, -1 for a number that is no page of the cache.  0 <= j < table_room.
@@ -108,21 +111,23 @@ ATTN_HD RowBlock row_block(const Sequences &s, int32_t number)
 // split of decode: the units of all segments (a segment is a sequence and a tile of the heads of one key head) in one
 // line, a workgroup takes an equal share of it
 // ------------------------------------------------------------------------------------------
-ATTN_HD int32_t units_of(int32_t length) { return length <= 0 ? 0 : (length + kDecodeUnit - 1) / kDecodeUnit; }
+ATTN_HD int32_t units_of(int32_t length) { return length <= 0 ? 0 : (length - 1) / kDecodeUnit + 1; }
 
-// First unit of workgroup w of `groups`.
-ATTN_HD int64_t share_begin(int64_t units, int32_t w, int32_t groups) { return units / groups * w + units % groups * w / groups; }
-
-// The workgroup that has unit u (0 <= u < units).
-ATTN_HD int32_t share_of(int64_t units, int64_t u, int32_t groups)
+// x / y, rounded down, for 0 <= x < 2^62, 0 < y and a quotient below 2^50.  A division of 64-bit integers is some hundred instructions on a GPU, and every workgroup makes a few
+// before its first load; one in fp64, corrected, is thirty.
+ATTN_HD int64_t quotient(int64_t x, int64_t y)
 {
-    int32_t lo = 0, hi = groups;   // share_begin(lo) <= u < share_begin(hi)
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (share_begin(units, mid, groups) <= u) lo = mid; else hi = mid;
-    }
-    return lo;
+    int64_t q = (int64_t)((double)x / (double)y);   // off by one at most
+    if (q * y > x) --q;
+    if ((q + 1) * y <= x) ++q;
+    return q;
 }
+
+// First unit of workgroup w of 2^groups_log2: the w-th part of the line, rounded down.
+ATTN_HD int64_t share_begin(int64_t units, int32_t w, int32_t groups_log2) { return (units * w) >> groups_log2; }
+
+// The workgroup that has unit u (0 <= u < units): the last w with share_begin(w) < u + 1.
+ATTN_HD int32_t share_of(int64_t units, int64_t u, int32_t groups_log2) { return (int32_t)quotient(((u + 1) << groups_log2) - 1, units); }
 
 // A workgroup has at most two segments that others have parts of: the one its share begins in and the one it ends in.  The piece of the
 // first goes to slot 2 w, that of another one to 2 w + 1.
@@ -155,7 +160,7 @@ struct AttendArgs {
     Cache cache;                // keys in pages
     int32_t heads, kv_heads, group, head_dim, causal;
     float scale_log2;           // scale / ln 2: weights are powers of two
-    int32_t groups;             // decode: workgroups
+    int32_t groups_log2;        // decode: workgroups
     int32_t head_tiles;         // decode: tiles of kHeadTile heads of one key head
     float *pieces;              // decode: per slot 16 rows of padded head_dim sums, 16 maxima, 16 sums of weights
 };
@@ -178,6 +183,6 @@ struct sc_attention {
     double turns[sck::kMaxPairs];
     bool has_device;
     int32_t n_cu;
-    int32_t decode_groups;
+    int32_t groups_log2;
     size_t ws_bytes;
 };

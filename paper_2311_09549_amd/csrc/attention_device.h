@@ -298,24 +298,40 @@ struct Wave {
             for (int w = 0; w < VW; ++w) asm volatile("" : "+v"(x.v[j][w]));
     }
 
-    // One step: scores of the tile's keys, of which the lane's query sees the first `visible` (MASK), running maximum and sum, second product.
-    template <bool MASK>
-    __device__ __forceinline__ void step(const Keys &k, Values &v, float scale_log2, int visible)
+    // Values of keys that no query of the step sees, all of which see the first `visible`, become 0.
+    __device__ __forceinline__ void hide(Values &x, int visible) const
     {
-        f32x4 s[TILES];
+#pragma unroll
+        for (int j = 0; j < TILES * 4; ++j)
+#pragma unroll
+            for (int w = 0; w < VW; ++w) x.v[j][w] = j / 4 * 16 + 4 * g + j % 4 < visible ? x.v[j][w] : 0u;
+    }
+
+    struct Scores { f32x4 s[TILES]; };
+
+    __device__ __forceinline__ void scores(Scores &x, const Keys &k) const
+    {
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
-            s[n] = f32x4{0, 0, 0, 0};
+            x.s[n] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < QC; ++c) {
                 if constexpr (B == 2) {
-                    s[n] = TR::mfma(k.k[n][c], q[c], s[n]);
+                    x.s[n] = TR::mfma(k.k[n][c], q[c], x.s[n]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[n] = TR::mfma(k.k[n][c][e], q[c][e], s[n]);
+                    for (int e = 0; e < 4; ++e) x.s[n] = TR::mfma(k.k[n][c][e], q[c][e], x.s[n]);
                 }
             }
         }
+    }
+
+    // The rest of a step: scores of keys of which the lane's query sees the first `visible` (MASK; ALIKE: as every query does), running maximum and sum,
+    // second product.
+    template <bool MASK, bool ALIKE = false>
+    __device__ __forceinline__ void add(const Scores &x, Values &v, float scale_log2, int visible)
+    {
+        const f32x4(&s)[TILES] = x.s;
         float p[TILES * 4], top = kMinusInf;
 #pragma unroll
         for (int j = 0; j < TILES * 4; ++j) {
@@ -336,8 +352,17 @@ struct Wave {
         l = l * shrink + sum;
 #pragma unroll
         for (int u = 0; u < EPL; ++u) o[u] *= shrink;
-        if (MASK) part_infinities(v, visible);
+        if (MASK && ALIKE) hide(v, visible);
+        else if (MASK) part_infinities(v, visible);
         add_values(v, p);
+    }
+
+    template <bool MASK>
+    __device__ __forceinline__ void step(const Keys &k, Values &v, float scale_log2, int visible)
+    {
+        Scores x;
+        scores(x, k);
+        add<MASK>(x, v, scale_log2, visible);
     }
 
     // The lane's sums are elements 4 g EPL + [0, 4 EPL) of query `col`, in the order o[0][0], o[1][0], .., o[0][1], ..

@@ -5,6 +5,8 @@
 // one line of units of 128 keys, and every workgroup takes an equal share of the line, by arithmetic on the lengths that are in device memory
 // (nobody on the host knows them).  A share that ends inside a segment (one sequence, one tile of 16 heads of a key head) leaves its
 // sums with their maximum and weight in the workspace, and a second kernel joins the pieces in order.
+#include <type_traits>
+
 #include "attention_device.h"
 
 namespace sck {
@@ -12,14 +14,7 @@ namespace sck {
 namespace {
 
 constexpr int kWaves = 4;
-
-// Sums over the wavefront's lanes of per-lane values, and places in the line; wave-uniform results.
-__device__ __forceinline__ int64_t wave_sum(int64_t x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
-}
+constexpr int64_t kWholeKeys = 512;
 
 // A value that all lanes hold alike, in scalar registers: what follows from it is scalar too.
 __device__ __forceinline__ int64_t uniform(int64_t x)
@@ -28,45 +23,63 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-__device__ __forceinline__ int64_t units_in_all(const Sequences &s, int lane)
-{
-    int64_t n = 0;
-    for (int32_t b = lane; b < s.batch; b += 64) n += units_of(paged_length(s, b));
-    return uniform(wave_sum(n));
-}
+// The line of units of the sequences, as a wavefront finds it: 64 sequences at a time, a lane each.  Units of 64 sequences are less than 2^31.
+struct Line {
+    const Sequences &s;
+    int lane;
+    int32_t mine, upto;    // units of sequence 64 chunk + lane, of it and those before it in the chunk
+    int32_t chunk;
+    int64_t before;        // units of the chunks before
 
-// Units of the sequences before b.
-__device__ __forceinline__ int64_t units_before(const Sequences &s, int32_t b, int lane)
-{
-    int64_t n = 0;
-    for (int32_t x = lane; x < b; x += 64) n += units_of(paged_length(s, x));
-    return uniform(wave_sum(n));
-}
-
-// The sequence that has unit u of the line of sequences (0 <= u < all of them), and the units before it.
-__device__ __forceinline__ int32_t sequence_at(const Sequences &s, int64_t u, int lane, int64_t &before)
-{
-    before = 0;
-    for (int32_t b0 = 0; b0 < s.batch; b0 += 64) {
-        const int64_t mine = b0 + lane < s.batch ? units_of(paged_length(s, b0 + lane)) : 0;
-        int64_t upto = mine;
+    __device__ __forceinline__ void load(int32_t c)
+    {
+        chunk = c;
+        const int32_t b = 64 * c + lane;
+        mine = b < s.batch ? units_of(paged_length(s, b)) : 0;
+        upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int64_t y = __shfl_up(upto, d);
-            if (lane >= d) upto += y;
+            const int32_t y = __shfl_up(upto, d);
+            upto += lane >= d ? y : 0;
         }
-        const uint64_t past = __ballot(before + upto > u);
-        if (past) {
-            const int at = __ffsll((unsigned long long)past) - 1;
-            before += uniform(__shfl(upto - mine, at));
-            return b0 + __builtin_amdgcn_readfirstlane(at);
-        }
-        before += uniform(__shfl(upto, 63));
     }
-    return s.batch;
-}
+    __device__ __forceinline__ int32_t chunk_units() const { return __builtin_amdgcn_readlane(upto, 63); }
+    // Units of all sequences.  One chunk stays loaded.
+    __device__ __forceinline__ int64_t all()
+    {
+        int64_t n = 0;
+        for (int32_t c = 0; 64 * c < s.batch; ++c) {
+            load(c);
+            n += chunk_units();
+        }
+        before = 0;
+        if (s.batch > 64) load(0);
+        return n;
+    }
+    // The sequence that has unit u (below all()), and the units before it.
+    __device__ __forceinline__ int32_t find(int64_t u, int64_t &ahead)
+    {
+        while (before + chunk_units() <= u) {
+            before += chunk_units();
+            load(chunk + 1);
+        }
+        const int at = __ffsll((unsigned long long)__ballot(before + upto > u)) - 1;
+        ahead = before + __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at);
+        return 64 * chunk + at;
+    }
+    // Units of the sequences before b.
+    __device__ __forceinline__ int64_t until(int32_t b)
+    {
+        while (chunk < b / 64) {
+            before += chunk_units();
+            load(chunk + 1);
+        }
+        return before + __builtin_amdgcn_readlane(upto, b % 64) - __builtin_amdgcn_readlane(mine, b % 64);
+    }
+};
 
-template <typename TR, int DP, bool EXACT>
+// WHOLE: a workgroup for each segment, and nothing to join.
+template <typename TR, int DP, bool EXACT, bool WHOLE>
 __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
 {
     using W = Wave<TR, DP, EXACT>;
@@ -75,21 +88,29 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
     __shared__ float top_s[kWaves][16], sum_s[kWaves][16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int32_t segments = a.kv_heads * a.head_tiles;   // of a sequence
-    const int64_t units = units_in_all(a.s, lane) * segments;
-    const int64_t share0 = share_begin(units, blockIdx.x, a.groups), share1 = share_begin(units, blockIdx.x + 1, a.groups);
-    if (share0 >= share1) return;
-    int64_t before;
-    int32_t b = sequence_at(a.s, share0 / segments, lane, before);
-    int64_t at = share0;   // place in the line
-    before *= segments;    // of the first unit of sequence b
+    int64_t share0 = 0, share1 = 0, before = 0, at = 0;   // places in the line: of the share, of the first unit of sequence b, and the present one
+    int32_t b, length, n_units, segment, u0 = 0;
+    if constexpr (WHOLE) {
+        b = blockIdx.x / segments;
+        segment = blockIdx.x % segments;
+        length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b));
+        share1 = n_units = units_of(length);
+    } else {
+        Line line = {a.s, lane};
+        const int64_t units = line.all() * segments;
+        share0 = share_begin(units, blockIdx.x, a.groups_log2);
+        share1 = share_begin(units, blockIdx.x + 1, a.groups_log2);
+        if (share0 >= share1) return;
+        b = line.find(quotient(share0, segments), before);
+        at = share0;
+        before *= segments;
+        length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b));
+        n_units = units_of(length);
+        segment = (int32_t)quotient(at - before, n_units);
+        u0 = (int32_t)(at - before - (int64_t)segment * n_units);
+    }
     W w;
-    while (at < share1 && b < a.s.batch) {
-        const int32_t length = paged_length(a.s, b), n_units = units_of(length);
-        if (n_units == 0) {
-            ++b;
-            continue;
-        }
-        const int32_t segment = (int32_t)((at - before) / n_units), u0 = (int32_t)((at - before) % n_units);
+    while (true) {
         const int32_t u1 = (int32_t)(share1 - at < n_units - u0 ? u0 + (share1 - at) : n_units);
         const int32_t kv = segment / a.head_tiles, head0 = segment % a.head_tiles * kHeadTile, heads = a.group - head0 < kHeadTile ? a.group - head0 : kHeadTile;
         w.init(lane, a.head_dim);
@@ -97,10 +118,14 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
         w.load_q(static_cast<const char *>(a.q.data) + (b * a.q.row + head * a.q.head) * B, w.col < heads);
         const char *k0 = static_cast<const char *>(a.cache.keys) + kv * a.cache.head * B, *v0 = static_cast<const char *>(a.cache.values) + kv * a.cache.head * B;
         const int64_t row_bytes = a.cache.row * B;
-        const int32_t end = u1 * kDecodeUnit < length ? u1 * kDecodeUnit : length;
+        const int32_t end = u1 == n_units ? length : u1 * kDecodeUnit;
         bool bad = false;
-        for (int32_t base = u0 * kDecodeUnit + wave * W::KEYS; base < end; base += kWaves * W::KEYS) {
-            KeyTile t[TILES];
+        // Keys of the next step are asked for when the scores have used this step's, values when the second product has: one of the two is always on its way.
+        // Every step masks: the vector ALUs have time, and a second form of it would be as much code again, which a short call waits for.
+        typename W::Keys keys;
+        typename W::Values values;
+        KeyTile t[TILES];
+        const auto find = [&](int32_t base) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < TILES; ++n) {
                 int32_t key = base + 16 * n;
@@ -113,12 +138,24 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
                 t[n].k = k0 + off;
                 t[n].v = v0 + off;
             }
-            typename W::Keys keys;
-            typename W::Values values;
+        };
+        constexpr int32_t STEP = kWaves * W::KEYS;
+        int32_t base = u0 * kDecodeUnit + wave * W::KEYS;
+        if (base < end) {
+            find(base);
             w.load_keys(keys, t, row_bytes);
             w.load_values(values, t, row_bytes);
-            if (base + W::KEYS <= length) w.template step<false>(keys, values, a.scale_log2, 0);
-            else w.template step<true>(keys, values, a.scale_log2, length - base);
+        }
+        for (; base < end; base += STEP) {
+            const bool more = base + STEP < end;
+            typename W::Scores scores;
+            w.scores(scores, keys);
+            if (more) {
+                find(base + STEP);
+                w.load_keys(keys, t, row_bytes);
+            }
+            w.template add<true, true>(scores, values, a.scale_log2, length - base);
+            if (more) w.load_values(values, t, row_bytes);
         }
 
         // join the wavefronts: each sums the elements (4 g + wave) EPL + [0, EPL) of every row
@@ -151,8 +188,8 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
 #pragma unroll
             for (int u = 0; u < EPL; ++u) r[u] += part_s[wave][n][lane][u];
         const int e0 = (4 * w.g + wave) * EPL;
-        if (u0 == 0 && u1 == n_units) {
-            const float factor = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (WHOLE || (u0 == 0 && u1 == n_units)) {
+            const float factor = WHOLE && length < 0 ? __builtin_nanf("") : sum == 0.0f ? 0.0f : 1.0f / sum;
             char *out = static_cast<char *>(a.out.data) + (b * a.out.row + head * a.out.head + e0) * B;
             if (w.col < heads) {
 #pragma unroll
@@ -173,10 +210,15 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
                 }
             }
         }
+        if (WHOLE) break;
         at += u1 - u0;
-        if (segment == segments - 1 && u1 == n_units) {
-            before += (int64_t)segments * n_units;
-            ++b;
+        if (at >= share1) break;
+        u0 = 0;
+        if (++segment == segments) {
+            segment = 0;
+            before = at;
+            do length = __builtin_amdgcn_readfirstlane(paged_length(a.s, ++b)); while (units_of(length) == 0);   // share1 is not behind the last unit
+            n_units = units_of(length);
         }
     }
 }
@@ -187,7 +229,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
 {
     constexpr int B = TR::kBytes, LANES = DP / 4, PARTS = 256 / LANES;
     __shared__ f32x4 sum_s[PARTS][LANES];
-    __shared__ float weight_s[PARTS];
+    __shared__ float weight_s[PARTS], top_s[4], factor_s[1 << kMaxGroupsLog2], total_s[1 << kMaxGroupsLog2];
     const int32_t b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x % 64;
     const int part = threadIdx.x / LANES, e = threadIdx.x % LANES * 4;
     const int32_t length = paged_length(a.s, b), n_units = units_of(length);
@@ -197,23 +239,33 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
     if (n_units) {
         const int32_t segments = a.kv_heads * a.head_tiles, tile = head % a.group / kHeadTile, col = head % a.group % kHeadTile;
         const int32_t segment = head / a.group * a.head_tiles + tile;
-        const int64_t units = units_in_all(a.s, lane) * segments, first = units_before(a.s, b, lane) * segments + (int64_t)segment * n_units;
-        const int32_t w0 = share_of(units, first, a.groups), w1 = share_of(units, first + n_units - 1, a.groups);
+        Line line = {a.s, lane};
+        const int64_t units = line.all() * segments, first = line.until(b) * segments + (int64_t)segment * n_units;
+        const int32_t w0 = share_of(units, first, a.groups_log2), w1 = share_of(units, first + n_units - 1, a.groups_log2);
         if (w0 == w1) return;   // whole in one workgroup, which has stored it
         float top = kMinusInf;
-        for (int32_t w = w0 + lane; w <= w1; w += 64) {
-            // a workgroup that has no units has no piece
-            if (share_begin(units, w, a.groups) == share_begin(units, w + 1, a.groups)) continue;
-            top = fmaxf(top, a.pieces[(int64_t)piece_slot(first, share_begin(units, w, a.groups), w) * piece_floats(DP) + kHeadTile * DP + col]);
+        // several workgroups have no units where there are fewer of those: they have no piece either
+        for (int32_t w = w0 + threadIdx.x; w <= w1; w += 256) {
+            const int64_t share0 = share_begin(units, w, a.groups_log2);
+            const bool none = share0 == share_begin(units, w + 1, a.groups_log2);
+            const int64_t at = (int64_t)piece_slot(first, share0, w) * piece_floats(DP) + kHeadTile * DP + col;
+            const float m = none ? kMinusInf : a.pieces[at];
+            factor_s[w - w0] = m;
+            total_s[w - w0] = none ? 0.0f : a.pieces[at + kHeadTile];
+            top = fmaxf(top, m);
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        if (lane == 0) top_s[threadIdx.x / 64] = top;
+        __syncthreads();
+        top = finite_max(fmaxf(fmaxf(top_s[0], top_s[1]), fmaxf(top_s[2], top_s[3])));
+#pragma unroll 4
         for (int32_t w = w0 + part; w <= w1; w += PARTS) {
-            if (share_begin(units, w, a.groups) == share_begin(units, w + 1, a.groups)) continue;
-            const float *piece = a.pieces + (int64_t)piece_slot(first, share_begin(units, w, a.groups), w) * piece_floats(DP);
-            const float factor = __builtin_amdgcn_exp2f((piece[kHeadTile * DP + col] - finite_max(top)) * a.scale_log2);
+            const float factor = __builtin_amdgcn_exp2f((factor_s[w - w0] - top) * a.scale_log2), total = total_s[w - w0];
+            if (factor_s[w - w0] == kMinusInf && total == 0.0f) continue;   // no piece, or one of weights 0
+            const float *piece = a.pieces + (int64_t)piece_slot(first, share_begin(units, w, a.groups_log2), w) * piece_floats(DP);
             sum += *reinterpret_cast<const f32x4 *>(piece + col * DP + e) * factor;
-            weight += piece[kHeadTile * (DP + 1) + col] * factor;
+            weight += total * factor;
         }
         sum_s[part][threadIdx.x % LANES] = sum;
         if (e == 0) weight_s[part] = weight;
@@ -235,12 +287,23 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
     }
 }
 
+template <typename TR, int DP, bool EXACT>
+void launch_exact(const AttendArgs &a, hipStream_t stream)
+{
+    // Few keys: a workgroup for each segment does with them before shares are found and pieces joined.
+    if (table_room(a.s) <= kWholeKeys && (int64_t)a.s.batch * a.kv_heads * a.head_tiles < 1 << 24) {
+        decode_kernel<TR, DP, EXACT, true><<<a.s.batch * a.kv_heads * a.head_tiles, 64 * kWaves, 0, stream>>>(a);
+        return;
+    }
+    decode_kernel<TR, DP, EXACT, false><<<1 << a.groups_log2, 64 * kWaves, 0, stream>>>(a);
+    decode_join_kernel<TR, DP><<<dim3(a.s.batch, a.heads), 256, 0, stream>>>(a);
+}
+
 template <typename TR, int DP>
 void launch_padded(const AttendArgs &a, hipStream_t stream)
 {
-    if (a.head_dim == DP) decode_kernel<TR, DP, true><<<a.groups, 64 * kWaves, 0, stream>>>(a);
-    else decode_kernel<TR, DP, false><<<a.groups, 64 * kWaves, 0, stream>>>(a);
-    decode_join_kernel<TR, DP><<<dim3(a.s.batch, a.heads), 256, 0, stream>>>(a);
+    if (a.head_dim == DP) launch_exact<TR, DP, true>(a, stream);
+    else launch_exact<TR, DP, false>(a, stream);
 }
 
 template <typename TR>

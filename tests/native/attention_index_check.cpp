@@ -44,11 +44,14 @@ static void blocks_cover(const std::vector<int32_t> &start, int32_t rows, bool i
     }
 }
 
-static void split_covers(const std::vector<int32_t> &length, int32_t segments, int32_t groups)
+static void split_covers(const std::vector<int32_t> &length, int32_t segments, int32_t groups_log2)
 {
     int64_t units = 0;
     for (const int32_t n : length) units += units_of(n);
     units *= segments;
+    const int32_t groups = 1 << groups_log2;
+    const auto share_begin = [&](int64_t all, int32_t w, int32_t) { return sck::share_begin(all, w, groups_log2); };
+    const auto share_of = [&](int64_t all, int64_t u, int32_t) { return sck::share_of(all, u, groups_log2); };
     CHECK(share_begin(units, 0, groups) == 0 && share_begin(units, groups, groups) == units);
     std::vector<int> slot(2 * groups, 0);
     int64_t first = 0;
@@ -89,9 +92,15 @@ int main()
     for (int round = 0; round < 400; ++round) {
         std::vector<int32_t> length;
         for (int b = below(40); b >= 0; --b) length.push_back(below(4) ? below(round % 5 ? 1000 : 100000) : 0);
-        split_covers(length, 1 + below(9), 1 + below(round % 2 ? 2000 : 7));
+        split_covers(length, 1 + below(9), below(round % 2 ? 11 : 4));
     }
-    split_covers(std::vector<int32_t>(3, 2147483647), 64, 768);
+    split_covers(std::vector<int32_t>(3, 2147483647), 64, 10);
+    for (int round = 0; round < 200000; ++round) {   // quotients below 2^50 of numbers below 2^62
+        const auto any = [&](int bits) { return (int64_t)(((uint64_t)rng() << 32 | rng()) >> (64 - bits)); };
+        const int64_t y = 1 + any(1 + below(40)), q = any(1 + below(50));
+        for (const int64_t r : {(int64_t)0, y - 1, any(62) % y})
+            if (q <= (((int64_t)1 << 62) - 1 - r) / y) CHECK(quotient(q * y + r, y) == q);
+    }
 
     const int32_t table[6] = {0, 4, -1, 5, 2147483647, 3}, lengths[4] = {-1, 33, 48, 49};
     Sequences s = {};

@@ -242,6 +242,32 @@ def test_decode(dtype, heads, kv_heads, head_dim, page_rows, lengths, heads_firs
             assert bool((got[b] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("heads,kv_heads,head_dim,lengths", [
+    (1, 1, 64, [1]),
+    (4, 2, 128, [1, 0, 15, 16, 17, 33, 127, 128, 129, 0, 255, 256, 257]),
+    (20, 1, 128, [300, 40]),
+    (35, 1, 72, [150, 0, 513]),
+    (6, 2, 256, [130, 1000]),
+    (2, 2, 136, [90, 640]),
+])
+def test_decode_with_room_for_more(dtype, heads, kv_heads, head_dim, lengths):
+    """Tables with room for many more keys than there are: the line of units, shares and pieces whatever the lengths."""
+    gen = torch.Generator().manual_seed(sum(lengths) + heads)
+    keys, values = ([normal(gen, n, kv_heads, head_dim, dtype=dtype) for n in lengths] for _ in range(2))
+    q = normal(gen, len(lengths), heads, head_dim, dtype=dtype)
+    kc, vc, table = cache_of(keys, values, 16, 2000, gen)
+    attention = Attention(heads, kv_heads, head_dim, dtype, 16)
+    workspace = torch.full((attention.ws_bytes // 4,), NAN, device="cuda")
+    got = attention.decode(q.cuda(), kc, vc, table, int32(lengths), workspace=workspace).cpu()
+    for b, n in enumerate(lengths):
+        want, bound = attend(q[b:b + 1], keys[b], values[b], torch.tensor([n]), 1 / math.sqrt(head_dim), dtype)
+        assert_within(got[b:b + 1], want, bound, f"length {n}")
+    table[0, 0] = -1
+    wrong = attention.decode(q.cuda(), kc, vc, table, int32([lengths[0]] + [-n - 1 for n in lengths[1:]])).cpu()
+    assert bool(torch.isnan(wrong).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_decode_many_sequences(dtype):
     """More sequences than a wavefront has lanes, and more units than workgroups: shares that begin and end anywhere."""
