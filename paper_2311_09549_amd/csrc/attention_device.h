@@ -357,14 +357,6 @@ struct Wave {
         add_values(v, p);
     }
 
-    template <bool MASK>
-    __device__ __forceinline__ void step(const Keys &k, Values &v, float scale_log2, int visible)
-    {
-        Scores x;
-        scores(x, k);
-        add<MASK>(x, v, scale_log2, visible);
-    }
-
     // The lane's sums are elements 4 g EPL + [0, 4 EPL) of query `col`, in the order o[0][0], o[1][0], .., o[0][1], ..
     __device__ __forceinline__ float sum_at(int e) const { return o[e % EPL][e / EPL]; }
 
@@ -383,6 +375,63 @@ struct Wave {
                 for (int w = 0; w < 4; ++w) y[w] = __builtin_bit_cast(uint32_t, sum_at(e + w) * factor);
             }
             if (EXACT || at < head_dim) *reinterpret_cast<u32x4 *>(static_cast<char *>(row) + at * B) = y;
+        }
+    }
+};
+
+// Join of four wavefronts that have had different keys of the same queries: each is left with the sums of a quarter of every row, elements
+// (4 g + wave) EPL + [0, EPL) of query `col`, and with the maximum and sum of weights of the whole.
+template <typename W>
+struct Join {
+    static constexpr int WAVES = 4, EPL = W::EPL;
+    struct Space {
+        alignas(16) float part[WAVES][WAVES - 1][64][EPL];   // [quarter][other wavefronts][lane]
+        float top[WAVES][16], sum[WAVES][16];
+    };
+
+    // l: sum of weights of the wavefront, over its lanes.  Space may be used again after the next barrier.
+    static __device__ __forceinline__ void run(const W &w, Space &space, int wave, int lane, float l, float scale_log2, float (&r)[EPL], float &top, float &sum)
+    {
+        if (w.g == 0) {
+            space.top[wave][w.col] = w.m;
+            space.sum[wave][w.col] = l;
+        }
+        __syncthreads();
+        top = kMinusInf;
+        sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) top = fmaxf(top, space.top[n][w.col]);
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) sum += space.sum[n][w.col] * __builtin_amdgcn_exp2f((space.top[n][w.col] - finite_max(top)) * scale_log2);
+        const float mine = __builtin_amdgcn_exp2f((w.m - finite_max(top)) * scale_log2);
+        // (r apart from the stores: one store to either place would keep it out of registers)
+#pragma unroll
+        for (int u = 0; u < EPL; ++u) r[u] = (wave == 0 ? w.o[u][0] : wave == 1 ? w.o[u][1] : wave == 2 ? w.o[u][2] : w.o[u][3]) * mine;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i)
+            if (i != wave) {
+#pragma unroll
+                for (int u = 0; u < EPL; u += 4)
+                    *reinterpret_cast<f32x4 *>(&space.part[i][wave - (wave > i)][lane][u]) = f32x4{w.o[u][i], w.o[u + 1][i], w.o[u + 2][i], w.o[u + 3][i]} * mine;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < WAVES - 1; ++n)
+#pragma unroll
+            for (int u = 0; u < EPL; ++u) r[u] += space.part[wave][n][lane][u];
+    }
+
+    // Stores the quarter in the row `out`, times `factor`.
+    template <typename TR, bool EXACT>
+    static __device__ __forceinline__ void store(const W &w, const float (&r)[EPL], int wave, char *out, float factor)
+    {
+        const int e0 = (4 * w.g + wave) * EPL;
+#pragma unroll
+        for (int u = 0; u < EPL; u += 4) {
+            if (!EXACT && e0 + u >= w.head_dim) break;
+            char *at = out + (e0 + u) * TR::kBytes;
+            if constexpr (TR::kBytes == 2) *reinterpret_cast<u32x2 *>(at) = u32x2{TR::pack(r[u] * factor, r[u + 1] * factor), TR::pack(r[u + 2] * factor, r[u + 3] * factor)};
+            else *reinterpret_cast<f32x4 *>(at) = f32x4{r[u], r[u + 1], r[u + 2], r[u + 3]} * factor;
         }
     }
 };

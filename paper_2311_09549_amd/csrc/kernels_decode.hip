@@ -13,7 +13,7 @@ namespace sck {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;   // that join() takes
 constexpr int64_t kWholeKeys = 512;
 
 // A value that all lanes hold alike, in scalar registers: what follows from it is scalar too.
@@ -80,12 +80,11 @@ struct Line {
 
 // WHOLE: a workgroup for each segment, and nothing to join.
 template <typename TR, int DP, bool EXACT, bool WHOLE>
-__global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
+__global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(AttendArgs a)
 {
     using W = Wave<TR, DP, EXACT>;
     constexpr int B = TR::kBytes, TILES = W::TILES, EPL = W::EPL;
-    __shared__ float part_s[kWaves][kWaves - 1][64][EPL];   // [quarter of the rows][other wavefronts][lane]
-    __shared__ float top_s[kWaves][16], sum_s[kWaves][16];
+    __shared__ typename Join<W>::Space join_s;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int32_t segments = a.kv_heads * a.head_tiles;   // of a sequence
     int64_t share0 = 0, share1 = 0, before = 0, at = 0;   // places in the line: of the share, of the first unit of sequence b, and the present one
@@ -158,50 +157,16 @@ __global__ void __launch_bounds__(64 * kWaves) decode_kernel(AttendArgs a)
             if (more) w.load_values(values, t, row_bytes);
         }
 
-        // join the wavefronts: each sums the elements (4 g + wave) EPL + [0, EPL) of every row
         const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
-        if (w.g == 0) {
-            top_s[wave][w.col] = w.m;
-            sum_s[wave][w.col] = l;
-        }
-        __syncthreads();
-        float top = kMinusInf, sum = 0.0f;
-#pragma unroll
-        for (int n = 0; n < kWaves; ++n) top = fmaxf(top, top_s[n][w.col]);
-#pragma unroll
-        for (int n = 0; n < kWaves; ++n) sum += sum_s[n][w.col] * __builtin_amdgcn_exp2f((top_s[n][w.col] - finite_max(top)) * a.scale_log2);
-        const float mine = __builtin_amdgcn_exp2f((w.m - finite_max(top)) * a.scale_log2);
-        float r[EPL];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i == wave) {
-#pragma unroll
-                for (int u = 0; u < EPL; ++u) r[u] = w.o[u][i] * mine;
-            } else {
-#pragma unroll
-                for (int u = 0; u < EPL; ++u) part_s[i][wave - (wave > i)][lane][u] = w.o[u][i] * mine;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < kWaves - 1; ++n)
-#pragma unroll
-            for (int u = 0; u < EPL; ++u) r[u] += part_s[wave][n][lane][u];
-        const int e0 = (4 * w.g + wave) * EPL;
+        float r[EPL], top, sum;
+        Join<W>::run(w, join_s, wave, lane, l, a.scale_log2, r, top, sum);
         if (WHOLE || (u0 == 0 && u1 == n_units)) {
             const float factor = WHOLE && length < 0 ? __builtin_nanf("") : sum == 0.0f ? 0.0f : 1.0f / sum;
-            char *out = static_cast<char *>(a.out.data) + (b * a.out.row + head * a.out.head + e0) * B;
-            if (w.col < heads) {
-#pragma unroll
-                for (int u = 0; u < EPL; u += 4) {
-                    if (!EXACT && e0 + u >= a.head_dim) break;
-                    if constexpr (B == 2) *reinterpret_cast<u32x2 *>(out + u * B) = u32x2{TR::pack(r[u] * factor, r[u + 1] * factor), TR::pack(r[u + 2] * factor, r[u + 3] * factor)};
-                    else *reinterpret_cast<f32x4 *>(out + u * B) = f32x4{r[u], r[u + 1], r[u + 2], r[u + 3]} * factor;
-                }
-            }
+            if (w.col < heads) Join<W>::template store<TR, EXACT>(w, r, wave, static_cast<char *>(a.out.data) + (b * a.out.row + head * a.out.head) * B, factor);
         } else {
             float *piece = a.pieces + (int64_t)piece_slot(before + (int64_t)segment * n_units, share0, blockIdx.x) * piece_floats(DP);
             if (w.col < heads) {
+                const int e0 = (4 * w.g + wave) * EPL;
 #pragma unroll
                 for (int u = 0; u < EPL; u += 4) *reinterpret_cast<f32x4 *>(piece + w.col * DP + e0 + u) = f32x4{r[u], r[u + 1], r[u + 2], r[u + 3]};
                 if (wave == 0 && w.g == 0) {

@@ -1,7 +1,9 @@
-// Prompt: attention of the rows of packed sequences over their keys, packed as well or in the pages of a cache.
+// Prompt: attention of the rows of packed sequences over their keys, packed as well or in the pages of a cache.  One pass over the keys with the running
+// maximum and sum of each row; scores and weights stay in registers.
 //
-// One pass over the keys with the running maximum and sum of each row; scores and weights stay in registers.  A workgroup has four
-// wavefronts of 16 rows of one head; each goes through the keys that its rows see by itself.
+// 16-bit types: prompt_tile.h.  fp32, here: the matrix cores have a sixteenth of the rate for it, so that keys and values straight from L2, for 16 rows of a
+// wavefront, keep up with them.  SPLIT: the four wavefronts of a workgroup have the same 16 rows and every fourth step of their keys; otherwise 16 rows
+// each and all keys.
 #include <type_traits>
 
 #include "prompt_tile.h"
@@ -10,23 +12,25 @@ namespace sck {
 
 namespace {
 
-constexpr int kPromptRows = 64;
+// fp32: below so many workgroups of 64 rows the keys are split too.
+constexpr int64_t kSplitBlocks = 1024;
 
-template <typename TR, int DP, bool EXACT, bool PAGED>
-__global__ void __launch_bounds__(256) prompt_kernel(AttendArgs a)
+template <typename TR, int DP, bool EXACT, bool PAGED, bool SPLIT>
+__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendArgs a)
 {
     using W = Wave<TR, DP, EXACT>;
-    constexpr int B = TR::kBytes, TILES = W::TILES;
+    constexpr int B = TR::kBytes, TILES = W::TILES, STEP = SPLIT ? 4 * W::KEYS : W::KEYS;
+    __shared__ typename std::conditional<SPLIT, typename Join<W>::Space, char>::type join_s;
     const int32_t head = blockIdx.y, kv = head / a.group;
-    const RowBlock blk = row_block<kPromptRows>(a.s, blockIdx.x);
+    const RowBlock blk = row_block<SPLIT ? 16 : 64>(a.s, blockIdx.x);
     if (blk.sequence < 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int32_t first = blk.first + wave * 16, end = blk.end < first + 16 ? blk.end : first + 16;   // rows of the wavefront
-    if (first >= end) return;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int32_t first = SPLIT ? blk.first : blk.first + wave * 16, end = blk.end < first + 16 ? blk.end : first + 16;   // rows of the wavefront
+    if (first >= end) return;   // never with SPLIT, whose wavefronts meet
     const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
 
     W w;
-    w.init(threadIdx.x % 64, a.head_dim);
+    w.init(lane, a.head_dim);
     const int32_t row = first + w.col;
     char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * B;
     if (length < 0) {
@@ -48,8 +52,10 @@ __global__ void __launch_bounds__(256) prompt_kernel(AttendArgs a)
     const char *v0 = PAGED ? static_cast<const char *>(a.cache.values) + kv * a.cache.head * B
                            : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head) * B;
     bool bad = false;
-    for (int32_t base = 0; base < most; base += W::KEYS) {
-        KeyTile t[TILES];
+    typename W::Keys keys;
+    typename W::Values values;
+    KeyTile t[TILES];
+    const auto find = [&](int32_t base) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
             int32_t at = base + 16 * n;
@@ -67,15 +73,34 @@ __global__ void __launch_bounds__(256) prompt_kernel(AttendArgs a)
                 t[n].v = v0 + at * v_row;
             }
         }
-        typename W::Keys keys;
-        typename W::Values values;
+    };
+    // keys of the next step are asked for when the scores have used this step's, values when the second product has
+    int32_t base = SPLIT ? wave * W::KEYS : 0;
+    if (base < most) {
+        find(base);
         w.load_keys(keys, t, k_row);
         w.load_values(values, t, v_row);
-        if (base + W::KEYS <= all) w.template step<false>(keys, values, a.scale_log2, 0);
-        else w.template step<true>(keys, values, a.scale_log2, visible - base);
+    }
+    for (; base < most; base += STEP) {
+        const bool more = base + STEP < most;
+        typename W::Scores scores;
+        w.scores(scores, keys);
+        if (more) {
+            find(base + STEP);
+            w.load_keys(keys, t, k_row);
+        }
+        if (base + W::KEYS <= all) w.template add<false>(scores, values, a.scale_log2, 0);
+        else w.template add<true>(scores, values, a.scale_log2, visible - base);
+        if (more) w.load_values(values, t, v_row);
     }
     const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
-    if (row < end) w.store(out, l == 0.0f ? 0.0f : 1.0f / l);
+    if constexpr (SPLIT) {
+        float r[W::EPL], top, sum;
+        Join<W>::run(w, join_s, wave, lane, l, a.scale_log2, r, top, sum);
+        if (row < end) Join<W>::template store<TR, EXACT>(w, r, wave, out, sum == 0.0f ? 0.0f : 1.0f / sum);
+    } else {
+        if (row < end) w.store(out, l == 0.0f ? 0.0f : 1.0f / l);
+    }
 }
 
 template <typename TR, int DP, bool PAGED>
@@ -90,9 +115,11 @@ void launch_padded(const AttendArgs &a, hipStream_t stream)
         if (a.scale_log2 > 1.0f) prompt_tile_kernel<TR, DP, PAGED, true, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
         else prompt_tile_kernel<TR, DP, PAGED, false, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
     } else {
-        const dim3 grid(row_blocks<kPromptRows>(a.s.rows, a.s.batch), a.heads);
-        if (a.head_dim == DP) prompt_kernel<TR, DP, true, PAGED><<<grid, 256, 0, stream>>>(a);
-        else prompt_kernel<TR, DP, false, PAGED><<<grid, 256, 0, stream>>>(a);
+        const bool split = (int64_t)row_blocks<64>(a.s.rows, a.s.batch) * a.heads < kSplitBlocks;
+        const dim3 grid(split ? row_blocks<16>(a.s.rows, a.s.batch) : row_blocks<64>(a.s.rows, a.s.batch), a.heads);
+        const auto kernel = a.head_dim == DP ? (split ? prompt_kernel<TR, DP, true, PAGED, true> : prompt_kernel<TR, DP, true, PAGED, false>)
+                                             : (split ? prompt_kernel<TR, DP, false, PAGED, true> : prompt_kernel<TR, DP, false, PAGED, false>);
+        kernel<<<grid, 256, 0, stream>>>(a);
     }
 }
 
