@@ -18,7 +18,11 @@ from . import binding as sc
 
 _DTYPES = {torch.bfloat16: sc.SC_BF16, torch.float16: sc.SC_F16, torch.float32: sc.SC_F32}
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_INT32, _empty_like = torch.int32, torch.empty_like
+_pack_rows, _pack_cache, _pack_sequences = sc.pack_rows, sc.pack_cache, sc.pack_sequences
+
+# torch's own accessor of a stream's address alone: the stream object around it takes 2 us to make
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class Attention:
@@ -45,7 +49,11 @@ class Attention:
                                           rotary_freq, interleaved, rotary_dim)
         self.ws_bytes = sc.attention_workspace_bytes(self.handle)
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"attention runs on a GPU, not on {self.device}")
+        self._index = torch.cuda.current_device() if self.device.index is None else self.device.index
         self.workspace = None   # made by the first decode
+        self._ws_streams = set()
         self._h = self.handle.handle
         self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
 
@@ -53,106 +61,119 @@ class Attention:
         return sc.attention_describe(self.handle)
 
     # -- operators ---------------------------------------------------------------------------------------------------------
+    # `stream`: the address of a HIP stream, torch's current one unless given.  Results that are made here belong to the current one.
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
         """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None."""
-        rows = len(k)
-        sequences, cache = self._sequences(rows, row_start, lengths, pages), self._cache(keys, values)
-        key, value = self._rows(k, rows, self.kv_heads), self._rows(v, rows, self.kv_heads)
+        shape = (k.shape[0], self.kv_heads, self.head_dim)
+        sequences, cache = self._sequences(shape[0], row_start, lengths, pages), self._cache(keys, values)
+        key, value = self._rows(k, shape), self._rows(v, shape)
         query = result = None
         if q is not None:
-            query = self._rows(q, rows, self.heads)
-            out, result = self._out(q, out, rows)
-        self._append(self._h, sequences, query, key, value, result, cache, self._stream() if stream is None else stream)
+            shape = (shape[0], self.heads, self.head_dim)
+            query = self._rows(q, shape)
+            out, result = self._out(q, out, shape)
+        status = self._append(self._h, sequences, query, key, value, result, cache, _raw_stream(self._index) if stream is None else stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_append")
         return out
 
     def prompt(self, q, k, v, row_start, out=None, stream=None):
         """Attention of the rows of each sequence over the keys and values of the same rows."""
-        rows = len(q)
-        query, key, value = self._rows(q, rows, self.heads), self._rows(k, rows, self.kv_heads), self._rows(v, rows, self.kv_heads)
-        out, result = self._out(q, out, rows)
-        self._prompt(self._h, self._sequences(rows, row_start), query, key, value, result, self._stream() if stream is None else stream)
+        rows = q.shape[0]
+        shape, kv_shape = (rows, self.heads, self.head_dim), (rows, self.kv_heads, self.head_dim)
+        query, key, value = self._rows(q, shape), self._rows(k, kv_shape), self._rows(v, kv_shape)
+        out, result = self._out(q, out, shape)
+        status = self._prompt(self._h, self._sequences(rows, row_start, None, None), query, key, value, result, _raw_stream(self._index) if stream is None else stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_prompt")
         return out
 
     def prompt_paged(self, q, keys, values, pages, lengths, row_start, out=None, stream=None):
         """Attention of the last rows of each sequence over its keys in the cache."""
-        rows = len(q)
-        query = self._rows(q, rows, self.heads)
-        out, result = self._out(q, out, rows)
-        self._prompt_paged(self._h, self._sequences(rows, row_start, lengths, pages), query, self._cache(keys, values), result,
-                           self._stream() if stream is None else stream)
+        shape = (q.shape[0], self.heads, self.head_dim)
+        query = self._rows(q, shape)
+        out, result = self._out(q, out, shape)
+        status = self._prompt_paged(self._h, self._sequences(shape[0], row_start, lengths, pages), query, self._cache(keys, values), result,
+                                     _raw_stream(self._index) if stream is None else stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_prompt_paged")
         return out
 
     def decode(self, q, keys, values, pages, lengths, out=None, workspace=None, stream=None):
         """Attention of one row per sequence over all its keys in the cache.  `workspace`: device bytes of the caller's, `ws_bytes` of them."""
-        rows = len(q)
-        query = self._rows(q, rows, self.heads)
-        out, result = self._out(q, out, rows)
-        if workspace is not None:
-            address, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        else:
-            if self.workspace is None:
-                self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-            address, size = self.workspace.data_ptr(), self.ws_bytes
-        self._decode(self._h, self._sequences(rows, None, lengths, pages), query, self._cache(keys, values), result, address, size,
-                     self._stream() if stream is None else stream)
+        shape = (q.shape[0], self.heads, self.head_dim)
+        query = self._rows(q, shape)
+        out, result = self._out(q, out, shape)
+        if stream is None:
+            stream = _raw_stream(self._index)
+        address, size = self._own_workspace(stream) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        status = self._decode(self._h, self._sequences(shape[0], None, lengths, pages), query, self._cache(keys, values), result, address, size, stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_decode")
         return out
 
     # -- records -----------------------------------------------------------------------------------------------------------
     # The host side of a call is most of the time of a short one: each attribute of a tensor is read once, and the messages are made apart.
-    def _rows(self, x, rows, heads):
+    def _rows(self, x, shape):
         stride = x.stride()
-        if x.dtype is not self.dtype or not x.is_cuda or x.shape != (rows, heads, self.head_dim) or stride[2] != 1:
-            self._refuse_rows(x, rows, heads)
-        return sc.pack_rows(x.data_ptr(), stride[0], stride[1])
+        if x.dtype is not self.dtype or x.get_device() != self._index or x.shape != shape or stride[2] != 1:
+            self._refuse_rows(x, shape)
+        return _pack_rows(x.data_ptr(), stride[0], stride[1])
 
-    def _refuse_rows(self, x, rows, heads):
-        if x.dtype is not self.dtype or not x.is_cuda:
-            raise TypeError(f"rows have to be {self.dtype} on the GPU, not {x.dtype} on {x.device}")
-        raise ValueError(f"rows have to be ({rows}, {heads}, {self.head_dim}) with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
+    def _refuse_rows(self, x, shape):
+        if x.dtype is not self.dtype or x.get_device() != self._index:
+            raise TypeError(f"rows have to be {self.dtype} on {self.device}, not {x.dtype} on {x.device}")
+        raise ValueError(f"rows have to be {shape} with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
 
-    def _out(self, q, out, rows):
+    def _out(self, q, out, shape):
         if out is not None:
-            return out, self._rows(out, rows, self.heads)
-        out = torch.empty_like(q)
+            return out, self._rows(out, shape)
+        out = _empty_like(q)
         stride = out.stride()
         if stride[2] != 1 or 0 in stride:   # of heads that share their memory, or a single one
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             stride = out.stride()
-        return out, sc.pack_rows(out.data_ptr(), stride[0], stride[1])
+        return out, _pack_rows(out.data_ptr(), stride[0], stride[1])
 
     def _cache(self, keys, values):
-        shape, stride = keys.shape, keys.stride()
-        if (keys.dtype is not self.dtype or values.dtype is not self.dtype or not keys.is_cuda or not values.is_cuda or shape[1:] != self._page or stride[3] != 1
-                or values.shape != shape or values.stride() != stride):
+        shape, stride, dtype = keys.shape, keys.stride(), self.dtype
+        if (keys.dtype is not dtype or values.dtype is not dtype or keys.get_device() != self._index or values.get_device() != self._index
+                or shape[1:] != self._page or stride[3] != 1 or values.shape != shape or values.stride() != stride):
             self._refuse_cache(keys, values)
-        return sc.pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], stride[0], stride[1], stride[2])
+        return _pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], stride[0], stride[1], stride[2])
 
     def _refuse_cache(self, keys, values):
-        if keys.dtype is not self.dtype or values.dtype is not self.dtype or not keys.is_cuda or not values.is_cuda:
-            raise TypeError(f"the cache has to be {self.dtype} on the GPU, not {keys.dtype} and {values.dtype}")
+        if any(x.dtype is not self.dtype or x.get_device() != self._index for x in (keys, values)):
+            raise TypeError(f"the cache has to be {self.dtype} on {self.device}, not {keys.dtype} on {keys.device} and {values.dtype} on {values.device}")
         raise ValueError(f"keys and values have to be (pages, {self.page_rows}, {self.kv_heads}, {self.head_dim}) alike, with the last "
                          f"dimension contiguous, not {tuple(keys.shape)} and {tuple(values.shape)} with strides {keys.stride()} and {values.stride()}")
 
-    def _sequences(self, rows, row_start=None, lengths=None, pages=None):
+    def _sequences(self, rows, row_start, lengths, pages):
         batch, starts, length, page, page_ld, columns = rows, 0, 0, 0, 0, 0
         if row_start is not None:
-            batch = len(row_start) - 1
-            if row_start.dtype is not torch.int32 or not row_start.is_cuda or row_start.dim() != 1 or not row_start.is_contiguous() or batch < 0:
-                raise ValueError(f"row_start has to be contiguous int32 on the GPU, one number more than sequences: got {row_start.dtype} {tuple(row_start.shape)}")
-            starts = row_start.data_ptr()
+            shape = row_start.shape
+            if row_start.dtype is not _INT32 or row_start.get_device() != self._index or len(shape) != 1 or not shape[0] or not row_start.is_contiguous():
+                self._refuse_table("row_start", "one number more than sequences", row_start)
+            batch, starts = shape[0] - 1, row_start.data_ptr()
         if lengths is not None:
-            if lengths.dtype is not torch.int32 or not lengths.is_cuda or lengths.shape != (batch,) or not lengths.is_contiguous():
-                raise ValueError(f"lengths have to be contiguous int32 on the GPU, one for each of {batch} sequences: got {lengths.dtype} {tuple(lengths.shape)}")
+            if lengths.dtype is not _INT32 or lengths.get_device() != self._index or lengths.shape != (batch,) or not lengths.is_contiguous():
+                self._refuse_table("lengths", f"one for each of {batch} sequences", lengths)
             length = lengths.data_ptr()
         if pages is not None:
             shape, stride = pages.shape, pages.stride()
-            if pages.dtype is not torch.int32 or not pages.is_cuda or len(shape) != 2 or shape[0] != batch or (shape[1] > 1 and stride[1] != 1):
-                raise ValueError(f"pages have to be int32 on the GPU, a row for each of {batch} sequences: got {pages.dtype} {tuple(shape)}")
+            if pages.dtype is not _INT32 or pages.get_device() != self._index or len(shape) != 2 or shape[0] != batch or (shape[1] > 1 and stride[1] != 1):
+                self._refuse_table("pages", f"a row for each of {batch} sequences", pages)
             page, page_ld, columns = pages.data_ptr(), stride[0], shape[1]
-        return sc.pack_sequences(batch, rows, starts, length, page, page_ld, columns)
+        return _pack_sequences(batch, rows, starts, length, page, page_ld, columns)
 
-    def _stream(self):
-        # torch's own accessor of the address alone: the stream object around it takes 2 us to make
-        if _raw_stream is None or self.device.index is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
-        return _raw_stream(self.device.index)
+    def _refuse_table(self, name, what, x):
+        raise ValueError(f"{name}: contiguous int32 on {self.device}, {what}; got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
+
+    def _own_workspace(self, stream):
+        if self.workspace is None:
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+            self._ws_streams = {_raw_stream(self._index)}
+        if stream not in self._ws_streams:   # not given away before this stream is done with it either
+            self._ws_streams.add(stream)
+            self.workspace.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
+        return self.workspace.data_ptr(), self.ws_bytes

@@ -486,17 +486,8 @@ def attention_decode(attention: AttentionHandle, sequences, q, cache, out, works
 
 
 def attention_calls():
-    """The four operators above as functions of the same arguments (a handle's address first) that raise ScError by themselves: one call
+    """The four operators above as functions of the same arguments (a handle's address first) that return the status: two calls
     less on the way of a step that is made for every layer and token."""
     def of(name):
-        call = getattr(lib(), name)
-
-        def checked(status, _, __):
-            if status:
-                _check(status, name)
-            return status
-        prototype = ctypes.CFUNCTYPE(ctypes.c_int, *call.argtypes)
-        call = prototype((name, _lib))
-        call.errcheck = checked
-        return call
+        return ctypes.CFUNCTYPE(ctypes.c_int, *getattr(lib(), name).argtypes)((name, _lib))
     return tuple(of("sc_attention_" + name) for name in ("append", "prompt", "prompt_paged", "decode"))
