@@ -60,17 +60,38 @@ ATTN_HD int32_t page_of(const Sequences &s, int32_t b, int32_t j)
     return (uint32_t)p < (uint32_t)s.pages ? p : -1;
 }
 
-// Sequence of row r: the last b whose first row is not after r.  Rows before the first sequence or after the last give
-// -1.  For a table that is not in order the answer is some sequence; the caller checks the range it then reads.
+// Of 64 places base + n * step, n = 0..63, a bit for each that is below `end` and a sequence that begins at row r or before.  On the GPU every lane of
+// a wavefront looks at one: a table of 64 is searched in one read's time.
+ATTN_HD uint64_t begun(const Sequences &s, int32_t r, int32_t base, int32_t step, int32_t end)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    const int64_t b = base + (int64_t)(threadIdx.x % 64) * step;
+    return __ballot(b < end && row_begin(s, (int32_t)b) <= r);
+#else
+    uint64_t bits = 0;
+    for (int n = 0; n < 64; ++n) {
+        const int64_t b = base + (int64_t)n * step;
+        if (b < end && row_begin(s, (int32_t)b) <= r) bits |= (uint64_t)1 << n;
+    }
+    return bits;
+#endif
+}
+
+// Sequence of row r, which all lanes ask for: the last b whose first row is not after r.  Rows before the first sequence or after the last give
+// -1.  For a table that is not in order the answer is some sequence that has the row.
 ATTN_HD int32_t sequence_of(const Sequences &s, int32_t r)
 {
     if (!s.row_start) return r;
-    int32_t lo = -1, hi = s.batch;   // row_begin(lo) <= r, row_begin(hi) > r
-    while (hi - lo > 1) {
-        const int32_t mid = lo + ((hi - lo) >> 1);
-        if (row_begin(s, mid) <= r) lo = mid; else hi = mid;
+    int32_t base = 0, end = s.batch;
+    while (true) {
+        const int32_t step = (end - base + 63) / 64;
+        const uint64_t bits = begun(s, r, base, step, end);
+        if (bits == 0) return -1;
+        base += (63 - __builtin_clzll(bits)) * step;
+        if (step == 1) break;
+        end = end - base < step ? end : base + step;
     }
-    return lo >= 0 && r < row_begin(s, lo + 1) ? lo : -1;
+    return r < row_begin(s, base + 1) ? base : -1;
 }
 
 // Blocks of ROWS rows, none across sequences, without a table of them: sequence b is given the numbers from row_begin(b) / ROWS + b
