@@ -5,8 +5,6 @@
 // one line of units of 128 keys, and every workgroup takes an equal share of the line, by arithmetic on the lengths that are in device memory
 // (nobody on the host knows them).  A share that ends inside a segment (one sequence, one tile of 16 heads of a key head) leaves its
 // sums with their maximum and weight in the workspace, and a second kernel joins the pieces in order.
-#include <type_traits>
-
 #include "attention_device.h"
 
 namespace sck {
@@ -78,8 +76,7 @@ struct Line {
     }
 };
 
-// WHOLE: a workgroup for each segment, and nothing to join.
-template <typename TR, int DP, bool EXACT, bool WHOLE>
+template <typename TR, int DP, bool EXACT>
 __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(AttendArgs a)
 {
     using W = Wave<TR, DP, EXACT>;
@@ -87,27 +84,15 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
     __shared__ typename Join<W>::Space join_s;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int32_t segments = a.kv_heads * a.head_tiles;   // of a sequence
-    int64_t share0 = 0, share1 = 0, before = 0, at = 0;   // places in the line: of the share, of the first unit of sequence b, and the present one
-    int32_t b, length, n_units, segment, u0 = 0;
-    if constexpr (WHOLE) {
-        b = blockIdx.x / segments;
-        segment = blockIdx.x % segments;
-        length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b));
-        share1 = n_units = units_of(length);
-    } else {
-        Line line = {a.s, lane};
-        const int64_t units = line.all() * segments;
-        share0 = share_begin(units, blockIdx.x, a.groups_log2);
-        share1 = share_begin(units, blockIdx.x + 1, a.groups_log2);
-        if (share0 >= share1) return;
-        b = line.find(quotient(share0, segments), before);
-        at = share0;
-        before *= segments;
-        length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b));
-        n_units = units_of(length);
-        segment = (int32_t)quotient(at - before, n_units);
-        u0 = (int32_t)(at - before - (int64_t)segment * n_units);
-    }
+    Line line = {a.s, lane};
+    const int64_t units = line.all() * segments;
+    const int64_t share0 = share_begin(units, blockIdx.x, a.groups_log2), share1 = share_begin(units, blockIdx.x + 1, a.groups_log2);
+    if (share0 >= share1) return;
+    int64_t before = 0, at = share0;   // places in the line: of the first unit of sequence b, and the present one
+    int32_t b = line.find(quotient(share0, segments), before);
+    before *= segments;
+    int32_t length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b)), n_units = units_of(length), segment = (int32_t)quotient(at - before, n_units);
+    int32_t u0 = (int32_t)(at - before - (int64_t)segment * n_units);
     W w;
     while (true) {
         const int32_t u1 = (int32_t)(share1 - at < n_units - u0 ? u0 + (share1 - at) : n_units);
@@ -160,8 +145,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
         const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
         float r[EPL], top, sum;
         Join<W>::run(w, join_s, wave, lane, l, a.scale_log2, r, top, sum);
-        if (WHOLE || (u0 == 0 && u1 == n_units)) {
-            const float factor = WHOLE && length < 0 ? __builtin_nanf("") : sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (u0 == 0 && u1 == n_units) {
+            const float factor = sum == 0.0f ? 0.0f : 1.0f / sum;
             if (w.col < heads) Join<W>::template store<TR, EXACT>(w, r, wave, static_cast<char *>(a.out.data) + (b * a.out.row + head * a.out.head) * B, factor);
         } else {
             float *piece = a.pieces + (int64_t)piece_slot(before + (int64_t)segment * n_units, share0, blockIdx.x) * piece_floats(DP);
@@ -175,7 +160,6 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
                 }
             }
         }
-        if (WHOLE) break;
         at += u1 - u0;
         if (at >= share1) break;
         u0 = 0;
@@ -185,6 +169,98 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
             do length = __builtin_amdgcn_readfirstlane(paged_length(a.s, ++b)); while (units_of(length) == 0);   // share1 is not behind the last unit
             n_units = units_of(length);
         }
+    }
+}
+
+// Few keys: a workgroup for each segment with as many wavefronts as LDS holds the sums of, so that most take one step.  What such a call waits for
+// is a chain of reads, length and page number, then keys and values, and the page numbers of a wavefront's first step do not wait for the length.
+template <int DP>
+constexpr int kWholeWaves = DP == 256 ? 8 : 16;
+
+template <typename TR, int DP, bool EXACT>
+__global__ void __launch_bounds__(64 * kWholeWaves<DP>, kWholeWaves<DP> / 4) decode_whole_kernel(AttendArgs a)
+{
+    using W = Wave<TR, DP, EXACT>;
+    constexpr int B = TR::kBytes, TILES = W::TILES, EPL = W::EPL, WAVES = kWholeWaves<DP>, LD = DP + 4;   // rows of sums begin in different banks
+    __shared__ __attribute__((aligned(16))) float sum_s[WAVES][kHeadTile][LD];
+    __shared__ float top_s[WAVES][kHeadTile], weight_s[WAVES][kHeadTile];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int32_t segments = a.kv_heads * a.head_tiles, b = blockIdx.x / segments, segment = blockIdx.x % segments;
+    const int32_t kv = segment / a.head_tiles, head0 = segment % a.head_tiles * kHeadTile, heads = a.group - head0 < kHeadTile ? a.group - head0 : kHeadTile;
+    const int64_t room = table_room(a.s);   // at most kWholeKeys
+    constexpr int32_t STEP = WAVES * W::KEYS;
+    int32_t base = wave * W::KEYS, page[TILES];
+#pragma unroll
+    for (int n = 0; n < TILES; ++n) page[n] = base + 16 * n < room ? page_of(a.s, b, base + 16 * n) : -1;
+    const int32_t length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b));
+    W w;
+    w.init(lane, a.head_dim);
+    const int32_t head = kv * a.group + head0 + (w.col < heads ? w.col : 0);
+    w.load_q(static_cast<const char *>(a.q.data) + (b * a.q.row + head * a.q.head) * B, w.col < heads);
+    const char *k0 = static_cast<const char *>(a.cache.keys) + kv * a.cache.head * B, *v0 = static_cast<const char *>(a.cache.values) + kv * a.cache.head * B;
+    const int64_t row_bytes = a.cache.row * B;
+    bool bad = false;
+    for (; base < length; base += STEP) {
+        typename W::Keys keys;
+        typename W::Values values;
+        typename W::Scores scores;
+        KeyTile t[TILES];
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) {
+            int32_t key = base + 16 * n, p = page[n];
+            if (key >= length) {   // nothing of it is seen: any rows that are there
+                key = base;
+                p = page[0];
+            }
+            t[n].last = length - 1 - key;
+            bad |= p < 0;
+            if (p < 0) p = 0;
+            const int64_t off = (p * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * B;
+            t[n].k = k0 + off;
+            t[n].v = v0 + off;
+        }
+        w.load_keys(keys, t, row_bytes);
+        w.load_values(values, t, row_bytes);
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) page[n] = base + STEP + 16 * n < length ? page_of(a.s, b, base + STEP + 16 * n) : -1;
+        w.scores(scores, keys);
+        w.template add<true, true>(scores, values, a.scale_log2, length - base);
+    }
+    const int parts = length <= 0 ? 0 : length > STEP - W::KEYS ? WAVES : (length - 1) / W::KEYS + 1;   // wavefronts that have had keys
+    const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
+    if (wave < parts && w.col < heads) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int u = 0; u < EPL; u += 4)
+                *reinterpret_cast<f32x4 *>(&sum_s[wave][w.col][(4 * w.g + i) * EPL + u]) = f32x4{w.o[u][i], w.o[u + 1][i], w.o[u + 2][i], w.o[u + 3][i]};
+        if (w.g == 0) {
+            top_s[wave][w.col] = w.m;
+            weight_s[wave][w.col] = l;
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < heads * (DP / 4); x += 64 * WAVES) {
+        const int c = x / (DP / 4), e = x % (DP / 4) * 4;
+        if (!EXACT && e >= a.head_dim) continue;
+        float m[WAVES], top = kMinusInf, weight = 0.0f;
+        f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) {
+            m[n] = n < parts ? top_s[n][c] : kMinusInf;
+            top = fmaxf(top, m[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) {
+            if (n >= parts) continue;
+            const float factor = __builtin_amdgcn_exp2f((m[n] - finite_max(top)) * a.scale_log2);
+            sum += *reinterpret_cast<const f32x4 *>(&sum_s[n][c][e]) * factor;
+            weight += weight_s[n][c] * factor;
+        }
+        sum *= length < 0 ? __builtin_nanf("") : weight == 0.0f ? 0.0f : 1.0f / weight;
+        char *out = static_cast<char *>(a.out.data) + (b * a.out.row + (kv * a.group + head0 + c) * a.out.head + e) * B;
+        if constexpr (B == 2) *reinterpret_cast<u32x2 *>(out) = u32x2{TR::pack(sum.x, sum.y), TR::pack(sum.z, sum.w)};
+        else *reinterpret_cast<f32x4 *>(out) = sum;
     }
 }
 
@@ -256,11 +332,11 @@ template <typename TR, int DP, bool EXACT>
 void launch_exact(const AttendArgs &a, hipStream_t stream)
 {
     // Few keys: a workgroup for each segment does with them before shares are found and pieces joined.
-    if (table_room(a.s) <= kWholeKeys && (int64_t)a.s.batch * a.kv_heads * a.head_tiles < 1 << 24) {
-        decode_kernel<TR, DP, EXACT, true><<<a.s.batch * a.kv_heads * a.head_tiles, 64 * kWaves, 0, stream>>>(a);
+    if (table_room(a.s) <= kWholeKeys && (int64_t)a.s.batch * a.kv_heads * a.head_tiles < 1 << 22) {
+        decode_whole_kernel<TR, DP, EXACT><<<a.s.batch * a.kv_heads * a.head_tiles, 64 * kWholeWaves<DP>, 0, stream>>>(a);
         return;
     }
-    decode_kernel<TR, DP, EXACT, false><<<1 << a.groups_log2, 64 * kWaves, 0, stream>>>(a);
+    decode_kernel<TR, DP, EXACT><<<1 << a.groups_log2, 64 * kWaves, 0, stream>>>(a);
     decode_join_kernel<TR, DP><<<dim3(a.s.batch, a.heads), 256, 0, stream>>>(a);
 }
 
