@@ -384,6 +384,9 @@ sc_status sc_attention_create(sc_attention **out, const sc_attention_desc *desc)
  * are split over the GPU.  It does not depend on the sequences of a call.  Calls that share it must not overlap. */
 sc_status sc_attention_workspace_bytes(const sc_attention *attention, size_t *bytes);
 
+/* Bytes of device workspace that the two prompt operators can use (256-byte aligned, contents arbitrary), 0 where they use none. */
+sc_status sc_attention_prompt_workspace_bytes(const sc_attention *attention, size_t *bytes);
+
 /* Human-readable description of the operators and of what a call reads, writes and computes.  Always NUL-terminates;
  * truncates to n-1 characters. */
 sc_status sc_attention_describe(const sc_attention *attention, char *buf, size_t n);
@@ -397,15 +400,16 @@ sc_status sc_attention_append(const sc_attention *attention, const sc_sequence_v
                               const sc_rows_view *v, const sc_rows_view *q_out, const sc_cache_view *cache, void *hip_stream);
 
 /* Attention of the rows of each sequence over the keys and values of the same rows, packed side by side (length must be NULL).
- * `out` (heads heads) must not overlap the inputs. */
+ * `out` (heads heads) must not overlap the inputs.  `workspace` may be NULL; with one, few long sequences are split over the whole GPU along
+ * their keys (a second kernel joins the pieces). */
 sc_status sc_attention_prompt(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_rows_view *k,
-                              const sc_rows_view *v, const sc_rows_view *out, void *hip_stream);
+                              const sc_rows_view *v, const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* The same over keys and values in the cache, as many as length says: the rows are the last ones of their sequences, and a row
- * at a negative position sees nothing.  A length that is negative or above page_count * page_rows, or a page number outside 0..pages-1 among
- * those that a row's keys reach, makes NaN of the rows concerned. */
+ * at a negative position sees nothing.  A length that is negative or above page_count * page_rows makes NaN of the rows of its sequence; a
+ * page number outside 0..pages-1 makes NaN of the rows whose keys reach it, and may make NaN of other rows of the sequence. */
 sc_status sc_attention_prompt_paged(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_cache_view *cache,
-                                    const sc_rows_view *out, void *hip_stream);
+                                    const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Attention of one row per sequence (row_start must be NULL) over all its keys in the cache.  Wrong lengths and page numbers as
  * for prompts.  Queues two kernels: pieces of equal length for the whole GPU, then the join of rows that have several. */

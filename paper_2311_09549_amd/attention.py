@@ -18,6 +18,8 @@ from . import binding as sc
 
 _DTYPES = {torch.bfloat16: sc.SC_BF16, torch.float16: sc.SC_F16, torch.float32: sc.SC_F32}
 
+_FEW_ROWS = 512   # packed prompts of no more are never split along their keys
+
 _INT32, _empty_like = torch.int32, torch.empty_like
 _pack_rows, _pack_cache, _pack_sequences = sc.pack_rows, sc.pack_cache, sc.pack_sequences
 
@@ -26,7 +28,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 
 
 class Attention:
-    """The operators for one head layout.  Holds the workspace of `decode`: calls of one Attention are to be queued on one stream, or
+    """The operators for one head layout.  Holds the workspace of its calls: those of one Attention are to be queued on one stream, or
     ordered by the caller; more streams at once take an Attention each."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
@@ -52,7 +54,8 @@ class Attention:
         if self.device.type != "cuda":
             raise ValueError(f"attention runs on a GPU, not on {self.device}")
         self._index = torch.cuda.current_device() if self.device.index is None else self.device.index
-        self.workspace = None   # made by the first decode
+        self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
+        self.workspace = None   # made, or made larger, by the first calls that need it
         self._ws_streams = set()
         self._h = self.handle.handle
         self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
@@ -77,24 +80,29 @@ class Attention:
             raise sc.ScError(status, "sc_attention_append")
         return out
 
-    def prompt(self, q, k, v, row_start, out=None, stream=None):
+    def prompt(self, q, k, v, row_start, out=None, workspace=None, stream=None):
         """Attention of the rows of each sequence over the keys and values of the same rows."""
         rows = q.shape[0]
         shape, kv_shape = (rows, self.heads, self.head_dim), (rows, self.kv_heads, self.head_dim)
         query, key, value = self._rows(q, shape), self._rows(k, kv_shape), self._rows(v, kv_shape)
         out, result = self._out(q, out, shape)
-        status = self._prompt(self._h, self._sequences(rows, row_start, None, None), query, key, value, result, _raw_stream(self._index) if stream is None else stream)
+        if stream is None:
+            stream = _raw_stream(self._index)
+        address, size = self._workspace_of(stream, workspace, self.prompt_ws_bytes if rows >= _FEW_ROWS else 0)
+        status = self._prompt(self._h, self._sequences(rows, row_start, None, None), query, key, value, result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_prompt")
         return out
 
-    def prompt_paged(self, q, keys, values, pages, lengths, row_start, out=None, stream=None):
+    def prompt_paged(self, q, keys, values, pages, lengths, row_start, out=None, workspace=None, stream=None):
         """Attention of the last rows of each sequence over its keys in the cache."""
         shape = (q.shape[0], self.heads, self.head_dim)
         query = self._rows(q, shape)
         out, result = self._out(q, out, shape)
-        status = self._prompt_paged(self._h, self._sequences(shape[0], row_start, lengths, pages), query, self._cache(keys, values), result,
-                                     _raw_stream(self._index) if stream is None else stream)
+        if stream is None:
+            stream = _raw_stream(self._index)
+        address, size = self._workspace_of(stream, workspace, self.prompt_ws_bytes)
+        status = self._prompt_paged(self._h, self._sequences(shape[0], row_start, lengths, pages), query, self._cache(keys, values), result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_prompt_paged")
         return out
@@ -106,7 +114,7 @@ class Attention:
         out, result = self._out(q, out, shape)
         if stream is None:
             stream = _raw_stream(self._index)
-        address, size = self._own_workspace(stream) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        address, size = self._workspace_of(stream, workspace, self.ws_bytes)
         status = self._decode(self._h, self._sequences(shape[0], None, lengths, pages), query, self._cache(keys, values), result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_decode")
@@ -169,11 +177,16 @@ class Attention:
     def _refuse_table(self, name, what, x):
         raise ValueError(f"{name}: contiguous int32 on {self.device}, {what}; got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
 
-    def _own_workspace(self, stream):
-        if self.workspace is None:
-            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+    def _workspace_of(self, stream, given, size):
+        if given is not None:
+            return given.data_ptr(), given.numel() * given.element_size()
+        if size == 0:
+            return None, 0
+        own = self.workspace
+        if own is None or own.numel() < size:
+            own = self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
             self._ws_streams = {_raw_stream(self._index)}
         if stream not in self._ws_streams:   # not given away before this stream is done with it either
             self._ws_streams.add(stream)
-            self.workspace.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
-        return self.workspace.data_ptr(), self.ws_bytes
+            own.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
+        return own.data_ptr(), own.numel()

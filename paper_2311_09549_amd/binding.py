@@ -35,7 +35,7 @@ EXPORTS = [
     "sc_plan_workspace_bytes", "sc_plan_describe", "sc_plan_model", "sc_plan_intermediate", "sc_execute",
     "sc_plan_set_profiling", "sc_plan_kernel_count", "sc_plan_kernel_time", "sc_plan_tile_count", "sc_plan_tile",
     "sc_tuning_set", "sc_stream_copy", "sc_plan_destroy", "sc_execute_static", "sc_plan_chosen",
-    "sc_attention_create", "sc_attention_workspace_bytes", "sc_attention_describe", "sc_attention_append", "sc_attention_prompt",
+    "sc_attention_create", "sc_attention_workspace_bytes", "sc_attention_prompt_workspace_bytes", "sc_attention_describe", "sc_attention_append", "sc_attention_prompt",
     "sc_attention_prompt_paged", "sc_attention_decode", "sc_attention_destroy",
 ]
 
@@ -134,9 +134,9 @@ def lib():
         _sc_execute = _lib["sc_execute"]
         _sc_execute.restype = ctypes.c_int
         _sc_execute.argtypes = [ptr, ptr, ptr, ctypes.c_int32, ptr, ptr, ctypes.c_size_t, ptr]
-        for name, args in (("append", 8), ("prompt", 7), ("prompt_paged", 6)):
-            getattr(_lib, "sc_attention_" + name).argtypes = [ptr] * args
-        _lib.sc_attention_decode.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ctypes.c_size_t, ptr]
+        _lib.sc_attention_append.argtypes = [ptr] * 8
+        for name, records in (("prompt", 6), ("prompt_paged", 5), ("decode", 5)):
+            getattr(_lib, "sc_attention_" + name).argtypes = [ptr] * (records + 1) + [ctypes.c_size_t, ptr]
         _lib.sc_attention_destroy.argtypes = [ptr]
     return _lib
 
@@ -462,6 +462,12 @@ def attention_workspace_bytes(attention: AttentionHandle) -> int:
     return int(n.value)
 
 
+def attention_prompt_workspace_bytes(attention: AttentionHandle) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().sc_attention_prompt_workspace_bytes(attention.handle, ctypes.byref(n)), "sc_attention_prompt_workspace_bytes")
+    return int(n.value)
+
+
 def attention_describe(attention: AttentionHandle) -> str:
     buf = ctypes.create_string_buffer(2048)
     _check(lib().sc_attention_describe(attention.handle, buf, ctypes.c_size_t(len(buf))), "sc_attention_describe")
@@ -473,12 +479,12 @@ def attention_append(attention: AttentionHandle, sequences, q, k, v, q_out, cach
     _check(lib().sc_attention_append(attention.handle, sequences, q, k, v, q_out, cache, stream), "sc_attention_append")
 
 
-def attention_prompt(attention: AttentionHandle, sequences, q, k, v, out, stream=0):
-    _check(lib().sc_attention_prompt(attention.handle, sequences, q, k, v, out, stream), "sc_attention_prompt")
+def attention_prompt(attention: AttentionHandle, sequences, q, k, v, out, workspace=None, workspace_bytes=0, stream=0):
+    _check(lib().sc_attention_prompt(attention.handle, sequences, q, k, v, out, workspace, workspace_bytes, stream), "sc_attention_prompt")
 
 
-def attention_prompt_paged(attention: AttentionHandle, sequences, q, cache, out, stream=0):
-    _check(lib().sc_attention_prompt_paged(attention.handle, sequences, q, cache, out, stream), "sc_attention_prompt_paged")
+def attention_prompt_paged(attention: AttentionHandle, sequences, q, cache, out, workspace=None, workspace_bytes=0, stream=0):
+    _check(lib().sc_attention_prompt_paged(attention.handle, sequences, q, cache, out, workspace, workspace_bytes, stream), "sc_attention_prompt_paged")
 
 
 def attention_decode(attention: AttentionHandle, sequences, q, cache, out, workspace, workspace_bytes, stream=0):

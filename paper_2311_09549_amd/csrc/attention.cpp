@@ -105,6 +105,17 @@ AttendArgs attend_args(const sc_attention *at)
     return a;
 }
 
+sc_status prompt_workspace_of(const sc_attention *at, void *workspace, size_t bytes, AttendArgs &a)
+{
+    a.n_cu = at->n_cu;
+    if (!workspace || !at->prompt_ws_bytes) return SC_OK;
+    if (bytes < at->prompt_ws_bytes) return SC_ERR_WORKSPACE_SMALL;
+    if ((uintptr_t)workspace % 256) return SC_ERR_SHAPE_MISMATCH;
+    a.pieces = static_cast<float *>(workspace);
+    a.cut = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + at->prompt_ws_bytes - 2 * prompt_shares(at->n_cu) * sizeof(int32_t));
+    return SC_OK;
+}
+
 }  // namespace
 
 extern "C" sc_status sc_attention_create(sc_attention **out, const sc_attention_desc *d)
@@ -146,6 +157,7 @@ extern "C" sc_status sc_attention_create(sc_attention **out, const sc_attention_
     // workgroups of decode: the power of two from two a compute unit on (two wavefronts a SIMD are what its registers allow)
     while (at->groups_log2 < kMaxGroupsLog2 && (1 << at->groups_log2) < 2 * at->n_cu) ++at->groups_log2;
     at->ws_bytes = sizeof(float) * 2 * ((size_t)1 << at->groups_log2) * piece_floats(padded_dim(at->head_dim));
+    at->prompt_ws_bytes = prompt_workspace(at->dtype, at->head_dim, at->n_cu);
     *out = at;
     return SC_OK;
 }
@@ -154,6 +166,13 @@ extern "C" sc_status sc_attention_workspace_bytes(const sc_attention *at, size_t
 {
     if (!at || !bytes) return SC_ERR_NULL;
     *bytes = at->ws_bytes;
+    return SC_OK;
+}
+
+extern "C" sc_status sc_attention_prompt_workspace_bytes(const sc_attention *at, size_t *bytes)
+{
+    if (!at || !bytes) return SC_ERR_NULL;
+    *bytes = at->prompt_ws_bytes;
     return SC_OK;
 }
 
@@ -202,7 +221,7 @@ extern "C" sc_status sc_attention_append(const sc_attention *at, const sc_sequen
 }
 
 extern "C" sc_status sc_attention_prompt(const sc_attention *at, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_rows_view *k,
-                                         const sc_rows_view *v, const sc_rows_view *out, void *hip_stream)
+                                         const sc_rows_view *v, const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!at || !sequences || !q || !k || !v || !out) return SC_ERR_NULL;
     AttendArgs a = attend_args(at);
@@ -213,12 +232,13 @@ extern "C" sc_status sc_attention_prompt(const sc_attention *at, const sc_sequen
     SC_TRY(check_rows(at, v, a.v));
     SC_TRY(check_rows(at, out, a.out));
     if (!written_ok(a.out, a.s.rows, at->heads, at->head_dim)) return SC_ERR_SHAPE_MISMATCH;
+    SC_TRY(prompt_workspace_of(at, workspace, workspace_bytes, a));
     if (!at->has_device) return SC_ERR_DEVICE;
     return launched(launch_prompt(a, at->dtype, false, (hipStream_t)hip_stream));
 }
 
 extern "C" sc_status sc_attention_prompt_paged(const sc_attention *at, const sc_sequence_view *sequences, const sc_rows_view *q,
-                                               const sc_cache_view *cache, const sc_rows_view *out, void *hip_stream)
+                                               const sc_cache_view *cache, const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!at || !sequences || !q || !cache || !out) return SC_ERR_NULL;
     AttendArgs a = attend_args(at);
@@ -228,6 +248,7 @@ extern "C" sc_status sc_attention_prompt_paged(const sc_attention *at, const sc_
     SC_TRY(check_rows(at, q, a.q));
     SC_TRY(check_rows(at, out, a.out));
     if (!written_ok(a.out, a.s.rows, at->heads, at->head_dim)) return SC_ERR_SHAPE_MISMATCH;
+    SC_TRY(prompt_workspace_of(at, workspace, workspace_bytes, a));
     if (!at->has_device) return SC_ERR_DEVICE;
     return launched(launch_prompt(a, at->dtype, true, (hipStream_t)hip_stream));
 }

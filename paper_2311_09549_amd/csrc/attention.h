@@ -20,6 +20,7 @@ constexpr int64_t kMaxRows = (1 << 24) - 1;
 constexpr int64_t kMaxUnits = (int64_t)1 << 52;   // of decode: 2^10 times as many fit what quotient() takes
 constexpr int32_t kMaxKeys = 1 << 30;   // of a sequence: a tile beyond the last one fits 32 bits
 constexpr int32_t kMaxBatch = (1 << 20) - 1;
+constexpr int kSplitBlocks = 1024;   // of rows of a prompt whose keys are split
 constexpr int32_t kMaxGroupsLog2 = 10;   // 2^n workgroups of decode at most
 
 // ------------------------------------------------------------------------------------------
@@ -183,12 +184,19 @@ struct AttendArgs {
     float scale_log2;           // scale / ln 2: weights are powers of two
     int32_t groups_log2;        // decode: workgroups
     int32_t head_tiles;         // decode: tiles of kHeadTile heads of one key head
-    float *pieces;              // decode: per slot 16 rows of padded head_dim sums, 16 maxima, 16 sums of weights
+    float *pieces;              // decode: per slot 16 rows of padded head_dim sums, 16 maxima, 16 sums of weights; prompt: null, or room for prompt_tile.h's
+    int32_t *cut;               // prompt: blocks that each share has pieces of
+    int32_t blocks;             // prompt: numbers of blocks of rows
+    int32_t n_cu;
 };
 
 // Padded head_dim of the kernels.
 ATTN_HD int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 ATTN_HD int piece_floats(int padded) { return kHeadTile * (padded + 2); }
+
+// Workgroups that a split prompt has, and the bytes of its pieces and of its table (0: a type that is not split).
+int prompt_shares(int n_cu);
+size_t prompt_workspace(sc_dtype dtype, int head_dim, int n_cu);
 
 hipError_t launch_append(const AppendArgs &a, sc_dtype dtype, hipStream_t stream);
 hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream);
@@ -205,5 +213,5 @@ struct sc_attention {
     bool has_device;
     int32_t n_cu;
     int32_t groups_log2;
-    size_t ws_bytes;
+    size_t ws_bytes, prompt_ws_bytes;
 };

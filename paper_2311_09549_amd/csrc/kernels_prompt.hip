@@ -13,7 +13,7 @@ namespace sck {
 namespace {
 
 // fp32: below so many workgroups of 64 rows the keys are split too.
-constexpr int64_t kSplitBlocks = 1024;
+constexpr int64_t kSplitBlocks32 = 1024;
 
 template <typename TR, int DP, bool EXACT, bool PAGED, bool SPLIT>
 __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendArgs a)
@@ -21,8 +21,26 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendAr
     using W = Wave<TR, DP, EXACT>;
     constexpr int B = TR::kBytes, TILES = W::TILES, STEP = SPLIT ? 4 * W::KEYS : W::KEYS;
     __shared__ typename std::conditional<SPLIT, typename Join<W>::Space, char>::type join_s;
-    const int32_t head = blockIdx.y, kv = head / a.group;
-    const RowBlock blk = row_block<SPLIT ? 16 : 64>(a.s, blockIdx.x);
+    const int32_t head = blockIdx.x % a.heads, kv = head / a.group, place = blockIdx.x / a.heads;
+    RowBlock blk;
+    if (SPLIT && a.blocks <= 256 && a.s.batch > 1) {
+        // The block with the place-th most keys: each thread has one and counts those before it.
+        __shared__ int32_t keys_s[256];
+        __shared__ RowBlock blk_s;
+        blk = (int32_t)threadIdx.x < a.blocks ? row_block<16>(a.s, threadIdx.x) : RowBlock{-1, 0, 0, 0, 0};
+        const int32_t mine = blk.sequence < 0 ? -1 : keys_seen(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, blk.end - 1);
+        keys_s[threadIdx.x] = mine;
+        __syncthreads();
+        int32_t ahead = 0;
+#pragma unroll 8
+        for (int32_t n = 0; n < a.blocks; ++n) ahead += keys_s[n] > mine || (keys_s[n] == mine && n < (int32_t)threadIdx.x);
+        if (ahead == place && (int32_t)threadIdx.x < a.blocks) blk_s = blk;
+        __syncthreads();
+        const auto same = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };
+        blk = {same(blk_s.sequence), same(blk_s.first), same(blk_s.end), same(blk_s.begin), same(blk_s.count)};
+    } else {
+        blk = row_block<SPLIT ? 16 : 64>(a.s, a.blocks - 1 - place);
+    }
     if (blk.sequence < 0) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int32_t first = SPLIT ? blk.first : blk.first + wave * 16, end = blk.end < first + 16 ? blk.end : first + 16;   // rows of the wavefront
@@ -103,23 +121,48 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendAr
     }
 }
 
+// 16-bit types: wavefronts of a workgroup, and how many blocks a share's worth of them is at most
+// where keys are split.
+template <int DP>
+constexpr int kPromptWaves = DP == 256 ? 4 : 8;
+constexpr int64_t kSplitBelow = 2;
+
 template <typename TR, int DP, bool PAGED>
-void launch_padded(const AttendArgs &a, hipStream_t stream)
+void launch_padded(AttendArgs a, hipStream_t stream)
 {
     if constexpr (TR::kBytes == 2) {
-        constexpr int NW = DP == 256 ? 4 : 8, KT = DP == 256 ? 32 : 128;
+        constexpr int NW = kPromptWaves<DP>, KT = DP == 256 ? 32 : 128;
         int heads_log2 = 0;
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
-        const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch;
-        const uint32_t grid = (uint32_t)(blocks * (a.heads >> heads_log2));
-        if (a.scale_log2 > 1.0f) prompt_tile_kernel<TR, DP, PAGED, true, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
-        else prompt_tile_kernel<TR, DP, PAGED, false, NW, KT><<<grid, 64 * NW, 0, stream>>>(a, heads_log2);
+        const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;
+        const bool far = a.scale_log2 > 1.0f;
+        // Keys are split where a block may have more than a few tiles of them, and there are too few blocks to come out even without.
+        const int64_t most = PAGED ? table_room(a.s) : a.s.rows;
+        const int shares = prompt_shares(a.n_cu);
+        if (a.pieces && !far && blocks <= kSplitBlocks && blocks * groups <= kSplitBelow * shares && most > 4 * KT) {
+            a.blocks = (int32_t)blocks;
+            prompt_tile_kernel<TR, DP, PAGED, false, true, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
+            prompt_join_kernel<TR, DP, NW><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
+            return;
+        }
+        const auto kernel = far ? prompt_tile_kernel<TR, DP, PAGED, true, false, NW, KT> : prompt_tile_kernel<TR, DP, PAGED, false, false, NW, KT>;
+        // a grid has fewer than 2^32 threads
+        const int64_t each = (((int64_t)1 << 32) / (64 * NW) - 1) / groups;
+        for (int64_t end = blocks; end > 0; end -= each) {
+            a.blocks = (int32_t)end;
+            kernel<<<(uint32_t)((end < each ? end : each) * groups), 64 * NW, 0, stream>>>(a, heads_log2);
+        }
     } else {
-        const bool split = (int64_t)row_blocks<64>(a.s.rows, a.s.batch) * a.heads < kSplitBlocks;
-        const dim3 grid(split ? row_blocks<16>(a.s.rows, a.s.batch) : row_blocks<64>(a.s.rows, a.s.batch), a.heads);
+        const bool split = (int64_t)row_blocks<64>(a.s.rows, a.s.batch) * a.heads < kSplitBlocks32;
+        a.blocks = split ? row_blocks<16>(a.s.rows, a.s.batch) : row_blocks<64>(a.s.rows, a.s.batch);
         const auto kernel = a.head_dim == DP ? (split ? prompt_kernel<TR, DP, true, PAGED, true> : prompt_kernel<TR, DP, true, PAGED, false>)
                                              : (split ? prompt_kernel<TR, DP, false, PAGED, true> : prompt_kernel<TR, DP, false, PAGED, false>);
-        kernel<<<grid, 256, 0, stream>>>(a);
+        // a grid has fewer than 2^32 threads
+        const int32_t each = (int32_t)(((int64_t)1 << 24) - 1) / a.heads;
+        for (int32_t end = a.blocks; end > 0; end -= each) {
+            a.blocks = end;
+            kernel<<<(end < each ? end : each) * a.heads, 256, 0, stream>>>(a);
+        }
     }
 }
 
@@ -140,6 +183,16 @@ void launch_typed(const AttendArgs &a, bool paged, hipStream_t stream)
 }
 
 }  // namespace
+
+int prompt_shares(int n_cu) { return n_cu; }   // the registers of a workgroup are a compute unit's
+
+size_t prompt_workspace(sc_dtype dtype, int head_dim, int n_cu)
+{
+    if (dtype == SC_F32) return 0;
+    const int dp = padded_dim(head_dim), n = prompt_shares(n_cu);
+    const size_t piece = dp == 64 ? kPromptWaves<64> * kPromptPiece<64> : dp == 128 ? kPromptWaves<128> * kPromptPiece<128> : kPromptWaves<256> * kPromptPiece<256>;
+    return 2 * n * (piece * sizeof(float) + sizeof(int32_t));
+}
 
 hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream)
 {

@@ -40,23 +40,42 @@ struct PromptTile {
     }
 };
 
+// What a piece of a wavefront's 32 rows takes in the workspace: per lane its sums, its maximum and its sum of weights.
+template <int DP>
+constexpr int kPromptPiece = 64 * (DP / 2 + 2);   // floats
+
+template <int R>
+__device__ __forceinline__ RowBlock row_block_of(const Sequences &s, int32_t number, int heads_log2)
+{
+    return heads_log2 == 0 ? row_block<R>(s, number) : heads_log2 == 1 ? row_block<R / 2>(s, number) : heads_log2 == 2 ? row_block<R / 4>(s, number) : row_block<R / 8>(s, number);
+}
+
+// Keys that row r of a block sees: none but those up to its own position.
+__device__ __forceinline__ int32_t keys_seen(const AttendArgs &a, const RowBlock &blk, int32_t length, int32_t r)
+{
+    const int32_t n = a.causal ? length - blk.count - blk.begin + 1 + r : length;
+    return n < 0 ? 0 : n;
+}
+
 // FAR: the maximum times scale_log2 may be beyond fp32 (a scale above ln 2), so that differences are taken before they are scaled.
-template <typename TR, int DP, bool PAGED, bool FAR, int NW, int KT>
+//
+// SPLIT: as in decode, the tiles of keys of all blocks are put in one line, block after block, one group of heads after the other, and every workgroup takes an
+// equal share of it; blocks that shares cut leave pieces, which prompt_join_kernel joins.  Without it a workgroup has one block, and a call takes as long as
+// the longest of them, or as the compute unit that was given most.
+template <typename TR, int DP, bool PAGED, bool FAR, bool SPLIT, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
 {
     using P = PromptTile<TR, DP, NW, KT>;
-    constexpr int CHUNKS = P::CHUNKS, DT = P::DT, NT = P::NT, LOADS = P::LOADS;
+    constexpr int CHUNKS = P::CHUNKS, DT = P::DT, NT = P::NT, LOADS = P::LOADS, R = 32 * NW;
     __shared__ __attribute__((aligned(16))) char tile_s[P::LDS_BYTES];   // [buffer][keys, values]
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), q = lane % 32, half = lane / 32;
-
-    // Blocks of a key head follow each other at a distance that is a multiple of the number of its XCD, where that is one, and share that
-    // one's L2; the last rows of a sequence, which see most keys, come first.
     const int32_t head_groups = a.heads >> heads_log2;
-    const int32_t head0 = blockIdx.x % head_groups << heads_log2, kv = head0 / a.group;
-    const int32_t blocks = gridDim.x / head_groups, number = blocks - 1 - blockIdx.x / head_groups;
-    constexpr int R = 32 * NW;
-    const RowBlock blk = heads_log2 == 0 ? row_block<R>(a.s, number) : heads_log2 == 1 ? row_block<R / 2>(a.s, number) : heads_log2 == 2 ? row_block<R / 4>(a.s, number) : row_block<R / 8>(a.s, number);
-    if (blk.sequence < 0) return;
+
+    // Keys of tiles first_tile .. last_tile - 1 for a block of rows and a group of heads; sums: where the sums go if those are not all tiles that it sees.
+    const auto work = [&](const RowBlock &blk, int32_t head_group, int32_t first_tile, int32_t last_tile, float *sums) __attribute__((always_inline)) {
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));   // what follows from it is made again for each block, instead of taking the registers of the main loop
+    const int lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64), q = lane % 32, half = lane / 32;
+    const int32_t head0 = head_group << heads_log2, kv = head0 / a.group;
     const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
     const int32_t head = head0 + (wave & ((1 << heads_log2) - 1)), first = blk.first + 32 * (wave >> heads_log2), row = first + q;
     const bool mine = row < blk.end;
@@ -67,13 +86,9 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         return;
     }
 
-    // keys that a row sees: none but those up to its own position
-    const int32_t before = length - blk.count - blk.begin + 1;
-    const auto sees = [&](int32_t r) {
-        const int32_t n = a.causal ? before + r : length;
-        return n < 0 ? 0 : n;
-    };
-    const int32_t block_most = sees(blk.end - 1);
+    const auto sees = [&](int32_t r) { return keys_seen(a, blk, length, r); };
+    int32_t block_most = sees(blk.end - 1);
+    if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
     const int32_t visible = mine ? sees(row) : 0;
     const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
 
@@ -92,7 +107,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
     float m = kMinusInf, l = 0.0f, from = 0.0f;   // from: what weights are taken against, the maximum (FAR) or its product with scale_log2
 
     // this thread's pieces of a tile
-    const int piece = threadIdx.x % CHUNKS, row0 = threadIdx.x / CHUNKS;
+    const int piece = thread % CHUNKS, row0 = thread / CHUNKS;
     const bool held = piece * 8 < a.head_dim;
     const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * 2, v_row = (PAGED ? a.cache.row : a.v.row) * 2;
     const char *k0 = PAGED ? static_cast<const char *>(a.cache.keys) + (kv * a.cache.head + piece * 8) * 2
@@ -242,10 +257,10 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 
     if (block_most > 0) {
         const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
-        fetch(0);
-        bool special = __syncthreads_or(put(tile_s, KT > block_all));
+        int32_t base = SPLIT ? first_tile * KT : 0;
+        fetch(base);
+        bool special = __syncthreads_or(put(tile_s, base + KT > block_all));
         int buffer = 0;
-        int32_t base = 0;
         const auto pass = [&](auto masked) {
             constexpr bool MASK = decltype(masked)::value;
             const bool more = base + KT < block_most, part = MASK || base + 2 * KT > block_all;
@@ -262,11 +277,21 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             base += KT;
         };
         // tiles that every row of the block sees whole, then the others
-        while (base + KT <= block_all) pass(std::false_type());
+        while (base + KT <= block_all && (!SPLIT || base < block_most)) pass(std::false_type());
         while (base < block_most) pass(std::true_type());
     }
     if (PAGED) bad = __syncthreads_or(bad);
     l += __shfl_xor(l, 32);
+    if (SPLIT && sums) {
+        float *p = sums + wave * kPromptPiece<DP>;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) reinterpret_cast<f32x4 *>(p)[(4 * d + r) * 64 + lane] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+        p[32 * DP + lane] = m;
+        p[32 * DP + 64 + lane] = PAGED && bad ? __builtin_nanf("") : l;
+        return;
+    }
     const float factor = PAGED && bad ? __builtin_nanf("") : l == 0.0f ? 0.0f : 1.0f / l;
     if (mine) {
 #pragma unroll
@@ -277,6 +302,139 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 if (e < a.head_dim)
                     *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[d][r] * factor, o[d][r + 1] * factor), TR::pack(o[d][r + 2] * factor, o[d][r + 3] * factor)};
             }
+    }
+    };
+
+    if constexpr (!SPLIT) {
+        // Blocks of a key head follow each other at a distance that is a multiple of the number of its XCD, where that is one, and share that
+        // one's L2; the last rows of a sequence, which see most keys, come first.
+        const RowBlock blk = row_block_of<R>(a.s, a.blocks - 1 - (int32_t)(blockIdx.x / head_groups), heads_log2);
+        if (blk.sequence >= 0) work(blk, blockIdx.x % head_groups, 0, 0, nullptr);
+    } else {
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+        // tiles of a block of rows; one that sees nothing has one too, since its rows are written
+        const auto tiles_of = [&](const RowBlock &blk) {
+            if (blk.sequence < 0) return 0;
+            const int32_t n = keys_seen(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, blk.end - 1);
+            return n <= KT ? 1 : (n - 1) / KT + 1;
+        };
+        // In the line a block's tiles lie behind kBegin places that stand for its start and end, which cost about as much as they.
+        constexpr int kBegin = 2;
+        __shared__ int64_t upto_s[kSplitBlocks + 1], wave_s[NW];
+        constexpr int EACH = kSplitBlocks / (64 * NW);
+        int32_t places[EACH];
+        int64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int32_t number = threadIdx.x * EACH + i;
+            places[i] = number < a.blocks ? tiles_of(row_block_of<R>(a.s, number, heads_log2)) : 0;
+            if (places[i]) places[i] += kBegin;
+            sum += places[i];
+        }
+        int64_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t y = __shfl_up(upto, d);
+            upto += lane >= d ? y : 0;
+        }
+        if (lane == 63) wave_s[wave] = upto;
+        __syncthreads();
+        upto -= sum;
+        for (int i = 0; i < wave; ++i) upto += wave_s[i];
+        if (threadIdx.x == 0) upto_s[0] = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            upto += places[i];
+            upto_s[threadIdx.x * EACH + i + 1] = upto;
+        }
+        __syncthreads();
+        const int64_t all = upto_s[kSplitBlocks];
+        // shares of a key head one after the other on one XCD, which workgroups go to in turn
+        const int32_t w = gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x;
+        const int64_t units = all * head_groups, size = units <= 4 * (int64_t)gridDim.x ? 4 : (units - 1) / gridDim.x + 1;
+        const int64_t share1 = (w + 1) * size < units ? (w + 1) * size : units;
+        int64_t at = w * size;
+        int32_t begun_in = -1, ends_in = -1;   // blocks that this share has a piece of: one that began before it, one that goes on behind it
+        if (at < share1) {
+            int32_t head_group = __builtin_amdgcn_readfirstlane((int32_t)(at / all)), number = 0;
+            const int64_t place = at - head_group * all;
+            for (int32_t hi = kSplitBlocks; hi - number > 1;) {   // the last block that begins at `place` or before, which has it
+                const int32_t mid = (number + hi) / 2;
+                if (upto_s[mid] <= place) number = mid; else hi = mid;
+            }
+            number = __builtin_amdgcn_readfirstlane(number);
+            int32_t from = __builtin_amdgcn_readfirstlane((int32_t)(place - upto_s[number]));
+            while (true) {
+                const int32_t n = __builtin_amdgcn_readfirstlane((int32_t)(upto_s[number + 1] - upto_s[number]));
+                const int32_t to = share1 - at < n - from ? from + (int32_t)(share1 - at) : n, id = head_group * a.blocks + number;
+                const int32_t first = from < kBegin ? 0 : from - kBegin, last = to < kBegin ? 0 : to - kBegin;
+                if (first < last) {
+                    if (first > 0) begun_in = id;
+                    if (to < n) ends_in = id;
+                    float *sums = first > 0 || to < n ? a.pieces + (2 * (int64_t)w + (first > 0 ? 0 : 1)) * NW * kPromptPiece<DP> : nullptr;
+                    work(row_block_of<R>(a.s, number, heads_log2), head_group, first, last, sums);
+                }
+                at += to - from;
+                if (at >= share1) break;
+                from = 0;
+                do {
+                    if (++number == a.blocks) {
+                        number = 0;
+                        ++head_group;
+                    }
+                } while (upto_s[number + 1] == upto_s[number]);
+            }
+        }
+        if (threadIdx.x == 0) {
+            a.cut[2 * w] = begun_in;
+            a.cut[2 * w + 1] = ends_in;
+        }
+    }
+}
+
+// Joins the pieces of the block that begins in share blockIdx.x and goes on behind it, in the order of the shares; a wavefront has the 32 rows of one of the first kernel's.
+template <typename TR, int DP, int NW>
+__global__ void __launch_bounds__(64) prompt_join_kernel(AttendArgs a, int heads_log2, int32_t shares)
+{
+    constexpr int DT = DP / 32;
+    const int32_t w = blockIdx.x, wave = blockIdx.y;
+    const int lane = threadIdx.x;
+    const int32_t id = a.cut[2 * w + 1];
+    if (id < 0 || a.cut[2 * w] == id) return;
+    // shares behind w that begin in the block: as many in a row as there are
+    int32_t more = 0;
+    while (true) {
+        const int32_t n = w + 1 + more + lane;
+        const uint64_t bits = __ballot(n < shares && a.cut[2 * (n < shares ? n : w)] == id);
+        const int run = ~bits == 0 ? 64 : __builtin_ctzll(~bits);
+        more += run;
+        if (run < 64) break;
+    }
+    const RowBlock blk = row_block_of<32 * NW>(a.s, id % a.blocks, heads_log2);
+    const int32_t head = (id / a.blocks << heads_log2) + (wave & ((1 << heads_log2) - 1)), row = blk.first + 32 * (wave >> heads_log2) + lane % 32;
+    const auto piece = [&](int32_t n) { return a.pieces + (n == 0 ? 2 * (int64_t)w + 1 : 2 * ((int64_t)w + n)) * NW * kPromptPiece<DP> + wave * kPromptPiece<DP>; };
+    float top = kMinusInf;
+    for (int32_t n = 0; n <= more; ++n) top = fmaxf(top, piece(n)[32 * DP + lane]);
+    top = finite_max(top);
+    f32x4 o[4 * DT];
+    float l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) o[i] = f32x4{0, 0, 0, 0};
+    for (int32_t n = 0; n <= more; ++n) {
+        const float *p = piece(n);
+        const float m = p[32 * DP + lane], part = p[32 * DP + 64 + lane];
+        const float factor = __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
+        l += part * factor;
+#pragma unroll
+        for (int i = 0; i < 4 * DT; ++i) o[i] += reinterpret_cast<const f32x4 *>(p)[i * 64 + lane] * factor;
+    }
+    const float factor = l == 0.0f ? 0.0f : 1.0f / l;
+    if (blk.sequence < 0 || row >= blk.end) return;
+    char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+        const int e = 8 * i + 4 * (lane / 32);
+        if (e < a.head_dim) *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[i].x * factor, o[i].y * factor), TR::pack(o[i].z * factor, o[i].w * factor)};
     }
 }
 
