@@ -88,68 +88,100 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
     const int64_t units = line.all() * segments;
     const int64_t share0 = share_begin(units, blockIdx.x, a.groups_log2), share1 = share_begin(units, blockIdx.x + 1, a.groups_log2);
     if (share0 >= share1) return;
-    int64_t before = 0, at = share0;   // places in the line: of the first unit of sequence b, and the present one
-    int32_t b = line.find(quotient(share0, segments), before);
-    before *= segments;
-    int32_t length = __builtin_amdgcn_readfirstlane(paged_length(a.s, b)), n_units = units_of(length), segment = (int32_t)quotient(at - before, n_units);
-    int32_t u0 = (int32_t)(at - before - (int64_t)segment * n_units);
     W w;
-    while (true) {
-        const int32_t u1 = (int32_t)(share1 - at < n_units - u0 ? u0 + (share1 - at) : n_units);
-        const int32_t kv = segment / a.head_tiles, head0 = segment % a.head_tiles * kHeadTile, heads = a.group - head0 < kHeadTile ? a.group - head0 : kHeadTile;
-        w.init(lane, a.head_dim);
-        const int32_t head = kv * a.group + head0 + (w.col < heads ? w.col : 0);
-        w.load_q(static_cast<const char *>(a.q.data) + (b * a.q.row + head * a.q.head) * B, w.col < heads);
-        const char *k0 = static_cast<const char *>(a.cache.keys) + kv * a.cache.head * B, *v0 = static_cast<const char *>(a.cache.values) + kv * a.cache.head * B;
-        const int64_t row_bytes = a.cache.row * B;
-        const int32_t end = u1 == n_units ? length : u1 * kDecodeUnit;
-        bool bad = false;
-        // Keys of the next step are asked for when the scores have used this step's, values when the second product has: one of the two is always on its way.
-        // Every step masks: the vector ALUs have time, and a second form of it would be as much code again, which a short call waits for.
-        typename W::Keys keys;
-        typename W::Values values;
-        KeyTile t[TILES];
-        const auto find = [&](int32_t base) __attribute__((always_inline)) {
+    // Units [u0, u1) of a segment: what is worked on at a time.
+    struct Part {
+        int64_t before;   // place in the line of the first unit of sequence b
+        int32_t b, segment, length, n_units, u0, u1;
+    };
+    const auto upto = [&](Part &p, int64_t at) { p.u1 = (int32_t)(share1 - at < p.n_units - p.u0 ? p.u0 + (share1 - at) : p.n_units); };
+    int64_t at = share0;
+    Part part;
+    part.b = line.find(quotient(at, segments), part.before);
+    part.before *= segments;
+    part.length = __builtin_amdgcn_readfirstlane(paged_length(a.s, part.b));
+    part.n_units = units_of(part.length);
+    part.segment = (int32_t)quotient(at - part.before, part.n_units);
+    part.u0 = (int32_t)(at - part.before - (int64_t)part.segment * part.n_units);
+    upto(part, at);
+
+    const int64_t row_bytes = a.cache.row * B;
+    constexpr int32_t STEP = kWaves * W::KEYS;
+    const auto heads_of = [&](const Part &p) { const int32_t n = a.group - p.segment % a.head_tiles * kHeadTile; return n < kHeadTile ? n : kHeadTile; };
+    const auto head_of = [&](const Part &p, int32_t heads) { return p.segment / a.head_tiles * a.group + p.segment % a.head_tiles * kHeadTile + (w.col < heads ? w.col : 0); };
+    const auto end_of = [&](const Part &p) { return p.u1 == p.n_units ? p.length : p.u1 * kDecodeUnit; };
+    // Keys of the next step are asked for when the scores have used this step's, values when the second product has: one of the two is always on its way.
+    // Every step masks: the vector ALUs have time, and a second form of it would be as much code again, which a short call waits for.
+    typename W::Keys keys;
+    typename W::Values values;
+    KeyTile t[TILES];
+    bool bad = false;
+    const auto find = [&](const Part &p, int32_t base) __attribute__((always_inline)) {
+        const int32_t kv = p.segment / a.head_tiles;
 #pragma unroll
-            for (int n = 0; n < TILES; ++n) {
-                int32_t key = base + 16 * n;
-                if (key >= length) key = base;   // nothing of it is seen: any rows that are there
-                t[n].last = length - 1 - key;
-                int32_t page = page_of(a.s, b, key);
-                bad |= page < 0;
-                if (page < 0) page = 0;
-                const int64_t off = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * B;
-                t[n].k = k0 + off;
-                t[n].v = v0 + off;
-            }
-        };
-        constexpr int32_t STEP = kWaves * W::KEYS;
-        int32_t base = u0 * kDecodeUnit + wave * W::KEYS;
-        if (base < end) {
-            find(base);
+        for (int n = 0; n < TILES; ++n) {
+            int32_t key = base + 16 * n;
+            if (key >= p.length) key = base;   // nothing of it is seen: any rows that are there
+            t[n].last = p.length - 1 - key;
+            int32_t page = page_of(a.s, p.b, key);
+            bad |= page < 0;
+            if (page < 0) page = 0;
+            const int64_t off = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + kv * a.cache.head) * B;
+            t[n].k = static_cast<const char *>(a.cache.keys) + off;
+            t[n].v = static_cast<const char *>(a.cache.values) + off;
+        }
+    };
+    // Queries and the first step of a part.
+    const auto ask = [&](const Part &p) __attribute__((always_inline)) {
+        const int32_t heads = heads_of(p), base = p.u0 * kDecodeUnit + wave * W::KEYS;
+        w.load_q(static_cast<const char *>(a.q.data) + (p.b * a.q.row + head_of(p, heads) * a.q.head) * B, w.col < heads);
+        if (base < end_of(p)) {
+            find(p, base);
             w.load_keys(keys, t, row_bytes);
             w.load_values(values, t, row_bytes);
         }
-        for (; base < end; base += STEP) {
+    };
+    w.init(lane, a.head_dim);
+    ask(part);
+    while (true) {
+        // the next part is known, and its queries and first keys asked for, before this one's wavefronts are joined
+        const int64_t next_at = at + (part.u1 - part.u0);
+        const bool again = next_at < share1;
+        Part next = part;
+        if (again) {
+            next.u0 = 0;
+            if (++next.segment == segments) {
+                next.segment = 0;
+                next.before = next_at;
+                do next.length = __builtin_amdgcn_readfirstlane(paged_length(a.s, ++next.b)); while (units_of(next.length) == 0);   // share1 is not behind the last unit
+                next.n_units = units_of(next.length);
+            }
+            upto(next, next_at);
+        }
+        const int32_t end = end_of(part);
+        for (int32_t base = part.u0 * kDecodeUnit + wave * W::KEYS; base < end; base += STEP) {
             const bool more = base + STEP < end;
             typename W::Scores scores;
             w.scores(scores, keys);
             if (more) {
-                find(base + STEP);
+                find(part, base + STEP);
                 w.load_keys(keys, t, row_bytes);
             }
-            w.template add<true, true>(scores, values, a.scale_log2, length - base);
+            w.template add<true, true>(scores, values, a.scale_log2, part.length - base);
             if (more) w.load_values(values, t, row_bytes);
         }
-
         const float l = bad ? __builtin_nanf("") : over_groups_sum(w.l);
+        bad = false;
+        if (again) ask(next);
         float r[EPL], top, sum;
         Join<W>::run(w, join_s, wave, lane, l, a.scale_log2, r, top, sum);
-        if (u0 == 0 && u1 == n_units) {
+        const int32_t heads = heads_of(part);
+        if (part.u0 == 0 && part.u1 == part.n_units) {
             const float factor = sum == 0.0f ? 0.0f : 1.0f / sum;
-            if (w.col < heads) Join<W>::template store<TR, EXACT>(w, r, wave, static_cast<char *>(a.out.data) + (b * a.out.row + head * a.out.head) * B, factor);
+            if (w.col < heads)
+                Join<W>::template store<TR, EXACT>(w, r, wave, static_cast<char *>(a.out.data) + (part.b * a.out.row + head_of(part, heads) * a.out.head) * B, factor);
         } else {
-            float *piece = a.pieces + (int64_t)piece_slot(before + (int64_t)segment * n_units, share0, blockIdx.x) * piece_floats(DP);
+            float *piece = a.pieces + (int64_t)piece_slot(part.before + (int64_t)part.segment * part.n_units, share0, blockIdx.x) * piece_floats(DP);
             if (w.col < heads) {
                 const int e0 = (4 * w.g + wave) * EPL;
 #pragma unroll
@@ -160,15 +192,10 @@ __global__ void __launch_bounds__(64 * kWaves, DP == 256 ? 1 : 2) decode_kernel(
                 }
             }
         }
-        at += u1 - u0;
-        if (at >= share1) break;
-        u0 = 0;
-        if (++segment == segments) {
-            segment = 0;
-            before = at;
-            do length = __builtin_amdgcn_readfirstlane(paged_length(a.s, ++b)); while (units_of(length) == 0);   // share1 is not behind the last unit
-            n_units = units_of(length);
-        }
+        if (!again) break;
+        w.init(lane, a.head_dim);
+        part = next;
+        at = next_at;
     }
 }
 
