@@ -365,7 +365,7 @@ typedef struct {
  * keys of the sequence, its new rows included, so that its n rows are at positions length[b] - n .. length[b] - 1.
  * length = NULL (packed keys): as many as its rows.  Key j of sequence b is row j % page_rows of page
  * page[b * page_ld + j / page_rows]; a sequence has page_count entries, of which those that length[b] reaches are read.
- * Device memory all of it.  Kernels take row starts as if clamped to 0..rows; rows of no sequence are neither read nor written.  At most 2^24 - 1
+ * Device memory all of it.  Kernels take row starts as if clamped to 0..rows; rows of no sequence are not written, and what they hold does not matter.  At most 2^24 - 1
  * rows, 2^20 - 1 sequences and 2^30 keys of one (more are a wrong length). */
 typedef struct {
     int32_t batch;
@@ -384,7 +384,8 @@ sc_status sc_attention_create(sc_attention **out, const sc_attention_desc *desc)
  * are split over the GPU.  It does not depend on the sequences of a call.  Calls that share it must not overlap. */
 sc_status sc_attention_workspace_bytes(const sc_attention *attention, size_t *bytes);
 
-/* Bytes of device workspace that the two prompt operators can use (256-byte aligned, contents arbitrary), 0 where they use none. */
+/* Bytes of device workspace that the two prompt operators can use (256-byte aligned, contents arbitrary), 0 where they use none.  Calls that share
+ * it must not overlap, and it is not decode's. */
 sc_status sc_attention_prompt_workspace_bytes(const sc_attention *attention, size_t *bytes);
 
 /* Human-readable description of the operators and of what a call reads, writes and computes.  Always NUL-terminates;

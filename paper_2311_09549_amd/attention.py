@@ -29,7 +29,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 
 class Attention:
     """The operators for one head layout.  Holds the workspace of its calls: those of one Attention are to be queued on one stream, or
-    ordered by the caller; more streams at once take an Attention each."""
+    ordered by the caller; more streams at once take an Attention each.  A graph that holds its calls needs it as long as it is replayed."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
                  rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0"):
@@ -55,8 +55,7 @@ class Attention:
             raise ValueError(f"attention runs on a GPU, not on {self.device}")
         self._index = torch.cuda.current_device() if self.device.index is None else self.device.index
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
-        self.workspace = None   # made, or made larger, by the first calls that need it
-        self._ws_streams = set()
+        self._own = {}   # workspaces, made by the first calls that need them
         self._h = self.handle.handle
         self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
 
@@ -88,7 +87,7 @@ class Attention:
         out, result = self._out(q, out, shape)
         if stream is None:
             stream = _raw_stream(self._index)
-        address, size = self._workspace_of(stream, workspace, self.prompt_ws_bytes if rows >= _FEW_ROWS else 0)
+        address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or (self.prompt_ws_bytes and rows > _FEW_ROWS) else (None, 0)
         status = self._prompt(self._h, self._sequences(rows, row_start, None, None), query, key, value, result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_prompt")
@@ -101,7 +100,7 @@ class Attention:
         out, result = self._out(q, out, shape)
         if stream is None:
             stream = _raw_stream(self._index)
-        address, size = self._workspace_of(stream, workspace, self.prompt_ws_bytes)
+        address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or self.prompt_ws_bytes else (None, 0)
         status = self._prompt_paged(self._h, self._sequences(shape[0], row_start, lengths, pages), query, self._cache(keys, values), result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_prompt_paged")
@@ -114,7 +113,7 @@ class Attention:
         out, result = self._out(q, out, shape)
         if stream is None:
             stream = _raw_stream(self._index)
-        address, size = self._workspace_of(stream, workspace, self.ws_bytes)
+        address, size = self._workspace_of(stream, workspace, "ws_bytes")
         status = self._decode(self._h, self._sequences(shape[0], None, lengths, pages), query, self._cache(keys, values), result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_decode")
@@ -177,16 +176,15 @@ class Attention:
     def _refuse_table(self, name, what, x):
         raise ValueError(f"{name}: contiguous int32 on {self.device}, {what}; got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
 
-    def _workspace_of(self, stream, given, size):
+    def _workspace_of(self, stream, given, name):
+        """Address and size of a workspace: the caller's, or the handle's own, which is made once and stays where it is (a graph may hold its address)."""
         if given is not None:
             return given.data_ptr(), given.numel() * given.element_size()
-        if size == 0:
-            return None, 0
-        own = self.workspace
-        if own is None or own.numel() < size:
-            own = self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
-            self._ws_streams = {_raw_stream(self._index)}
-        if stream not in self._ws_streams:   # not given away before this stream is done with it either
-            self._ws_streams.add(stream)
-            own.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
-        return own.data_ptr(), own.numel()
+        own = self._own.get(name)
+        if own is None:
+            own = self._own[name] = (torch.empty(getattr(self, name), dtype=torch.uint8, device=self.device), {_raw_stream(self._index)})
+        tensor, streams = own
+        if stream not in streams:   # not given away before this stream is done with it either
+            streams.add(stream)
+            tensor.record_stream(torch.cuda.ExternalStream(stream, device=self.device))
+        return tensor.data_ptr(), tensor.numel()

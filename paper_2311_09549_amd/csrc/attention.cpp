@@ -185,12 +185,12 @@ extern "C" sc_status sc_attention_describe(const sc_attention *at, char *buf, si
              "attention %s: heads %d, key heads %d, head_dim %d (kernels padded to %d), pages of %d rows, %s\n"
              "  A(i,l) = sum_j softmax_j(%g * sum_k X(i,k) Y(j,k)) Z(j,l)\n"
              "  append: rotates %d of %d elements (%s), moves %d bytes a row\n"
-             "  prompt: %d flops per row and key, reads and writes %d bytes a row and %d bytes a key\n"
+             "  prompt: %d flops per row and key, reads and writes %d bytes a row and %d bytes a key, %zu bytes of workspace\n"
              "  decode: %d flops and %d bytes a key, %d workgroups, %zu bytes of workspace\n",
              at->dtype == SC_F32 ? "f32" : at->dtype == SC_F16 ? "f16" : "bf16", at->heads, at->kv_heads, d, padded_dim(d), at->page_rows,
              at->causal ? "causal" : "not causal", at->scale_log2 * 0.6931471805599453, 2 * at->pairs, d,
              at->interleaved ? "adjacent pairs" : "pairs of halves", 2 * (at->heads + 2 * at->kv_heads) * d * e, 4 * at->heads * d, 2 * at->heads * d * e,
-             2 * at->kv_heads * d * e, 4 * at->heads * d, 2 * at->kv_heads * d * e, 1 << at->groups_log2, at->ws_bytes);
+             2 * at->kv_heads * d * e, at->prompt_ws_bytes, 4 * at->heads * d, 2 * at->kv_heads * d * e, 1 << at->groups_log2, at->ws_bytes);
     return SC_OK;
 }
 
