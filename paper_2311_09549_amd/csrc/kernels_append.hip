@@ -3,6 +3,9 @@
 // A row is moved once, heads + 2 kv_heads heads in and as many out, and pairs / head_dim of it turned: nothing but memory traffic, or,
 // for the few rows of a decoding step, the latency of a launch and of three dependent reads (row start, length, page number).  A workgroup
 // takes one row: all its heads turn by the same angles, so it takes their sines and cosines once, into LDS.
+//
+// 4,623 rows of 32 + 2 * 8 heads of 128, bf16, 64 elements rotated: 25 us, 4.5 TB/s, where a large copy reaches 4.8; 33 us with the row asked for after its place
+// is known.  One row: 3.5 us, launch and chain of reads.
 #include "attention.h"
 
 namespace sck {

@@ -4,6 +4,9 @@
 // 16-bit types: prompt_tile.h.  fp32, here: the matrix cores have a sixteenth of the rate for it, so that keys and values straight from L2, for 16 rows of a
 // wavefront, keep up with them.  SPLIT: the four wavefronts of a workgroup have the same 16 rows and every fourth step of their keys; otherwise 16 rows
 // each and all keys.
+//
+// Five prompts up to 777 rows, 8 heads of 96 on 2: 37 us (30 TFLOP/s; a large product of the library reaches 153), 48 with the blocks in the order of their rows: matrix pipes busy a third of
+// the time, a quarter of it with the padding to 128.
 #include <type_traits>
 
 #include "prompt_tile.h"
@@ -12,7 +15,7 @@ namespace sck {
 
 namespace {
 
-// fp32: below so many workgroups of 64 rows the keys are split too.
+// fp32: below so many workgroups of 64 rows (four for each compute unit) the keys are split too: the five prompts above take 50 us with and 114 without.
 constexpr int64_t kSplitBlocks32 = 1024;
 
 template <typename TR, int DP, bool EXACT, bool PAGED, bool SPLIT>
@@ -121,11 +124,11 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendAr
     }
 }
 
-// 16-bit types: wavefronts of a workgroup, and how many blocks a share's worth of them is at most
-// where keys are split.
+// 16-bit types: wavefronts of a workgroup, and what a split costs besides.
 template <int DP>
 constexpr int kPromptWaves = DP == 256 ? 4 : 8;
-constexpr int64_t kSplitBelow = 2;
+template <int DP>
+constexpr int64_t kSplitTiles = DP == 128 ? 7 : 12;
 
 template <typename TR, int DP, bool PAGED>
 void launch_padded(AttendArgs a, hipStream_t stream)
@@ -136,10 +139,15 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;
         const bool far = a.scale_log2 > 1.0f;
-        // Keys are split where a block may have more than a few tiles of them, and there are too few blocks to come out even without.
-        const int64_t most = PAGED ? table_room(a.s) : a.s.rows;
+        // Keys are split where the longest block alone would take longer than everything in equal shares.  The host knows neither lengths nor their sum: the longest
+        // is taken as all that the table has room for, or twice the mean of packed sequences, the mean as half of that.  Measured in tiles, the start and
+        // the join of a split cost kSplitTiles, and its tiles 1.3 times as much (workgroups that begin at different keys do not meet in L2).  bf16, heads and key heads
+        // of d, with and without a split: 8, 1, 128, 4,096 rows 80 and 118 us; 4, 4, 256, 2,000 rows 69 and 128; 8, 8, 64, 2,000 rows 38 and 46; chunks
+        // behind up to 8,191 keys, 32, 8, 128: 264 and 320; but 32, 8, 128, 2,048 rows 90 and 73, 4,000 rows 196 and 172, 600 rows 50 and 29.
+        const int64_t longest = PAGED ? table_room(a.s) : a.s.batch > 1 ? 2 * (int64_t)a.s.rows / a.s.batch : a.s.rows;
+        const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / KT;
         const int shares = prompt_shares(a.n_cu);
-        if (a.pieces && !far && blocks <= kSplitBlocks && blocks * groups <= kSplitBelow * shares && most > 4 * KT) {
+        if (a.pieces && !far && blocks <= kSplitBlocks && tiles > 4 && tiles * shares > kSplitTiles<DP> * shares + 13 * blocks * groups * tiles / 20) {
             a.blocks = (int32_t)blocks;
             prompt_tile_kernel<TR, DP, PAGED, false, true, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
             prompt_join_kernel<TR, DP, NW><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);

@@ -52,6 +52,8 @@ def check_rows(got, q, k, v, before, dtype, causal, gen, what):
     (2, 1, 256, [530, 31, 700], True),
     (5, 1, 80, [900, 0, 0, 200], True),
     (1, 1, 64, [4000], True),
+    (4, 2, 128, [3000, 1, 0], True),
+    (5, 1, 80, [2500, 200], False),
 ])
 def test_prompt(dtype, heads, kv_heads, head_dim, rows, causal):
     gen = torch.Generator().manual_seed(sum(rows) + head_dim)
@@ -77,6 +79,8 @@ def test_prompt(dtype, heads, kv_heads, head_dim, rows, causal):
     (2, 1, 256, 16, [800, 100], [100, 100], True),
     (1, 1, 64, 16, [1, 2, 3], [1, 1, 1], True),            # room for many more keys than there are
     (2, 1, 64, 16, [5, 600], [12, 600], True),             # rows before position 0
+    (1, 1, 128, 16, [1, 2, 3], [1, 1, 1], True),
+    (2, 1, 128, 16, [5, 600], [12, 600], True),
 ])
 def test_prompt_paged(dtype, heads, kv_heads, head_dim, page_rows, lengths, rows, causal):
     gen = torch.Generator().manual_seed(sum(lengths) + head_dim)
@@ -97,16 +101,17 @@ def test_prompt_paged(dtype, heads, kv_heads, head_dim, page_rows, lengths, rows
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
-def test_wrong_tables(dtype):
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_wrong_tables(dtype, head_dim):
     """Wrong lengths and pages make NaN of rows of their sequences alone, wherever shares end; row starts out of order stay in range."""
     gen = torch.Generator().manual_seed(3)
     lengths = [900, 900, 900, 900, 900]
-    keys, values = ([normal(gen, 900, 1, 64, dtype=dtype) for _ in lengths] for _ in range(2))
-    q = normal(gen, 100 * len(lengths), 2, 64, dtype=dtype)
+    keys, values = ([normal(gen, 900, 1, head_dim, dtype=dtype) for _ in lengths] for _ in range(2))
+    q = normal(gen, 100 * len(lengths), 2, head_dim, dtype=dtype)
     kc, vc, table = cache_of(keys, values, 16, 64, gen)
     table[1, 2] = kc.shape[0]
     table[2, 0] = -5
-    attention = Attention(2, 1, 64, dtype, 16)
+    attention = Attention(2, 1, head_dim, dtype, 16)
     got = attention.prompt_paged(q.cuda(), kc, vc, table, int32([900, 900, 900, -1, 1025]), int32(starts([100] * 5))).cpu()
     check_rows(got[:100], q[:100], keys[0], values[0], 800, dtype, True, gen, "good sequence")
     assert bool(torch.isnan(got[100:]).all())
@@ -161,6 +166,28 @@ def test_step_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager[i])
+
+
+def test_workspaces_stay_where_a_graph_has_them():
+    """A captured token, then a long prompt through the same handle: replays go on as before."""
+    gen = torch.Generator().manual_seed(7)
+    keys, values = ([normal(gen, 1500, 1, 64, dtype=BF16)] for _ in range(2))
+    kc, vc, table = cache_of(keys, values, 64, 30, gen, fill=0.0)
+    attention = Attention(2, 1, 64, BF16, 64)
+    q, lengths, out = normal(gen, 1, 2, 64, dtype=BF16).cuda(), int32([1500]), torch.empty(1, 2, 64, dtype=BF16, device="cuda")
+    eager = attention.decode(q, kc, vc, table, lengths).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attention.decode(q, kc, vc, table, lengths, out=out)
+    x = normal(gen, 2000, 2, 64, dtype=BF16).cuda()
+    for _ in range(2):
+        attention.prompt(x, x[:, :1], x[:, :1], int32([0, 2000]))
+        others = [torch.full((1 << 22,), NAN, device="cuda") for _ in range(4)]   # would be given the memory of a workspace that is gone
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        assert all(bool(torch.isnan(x).all()) for x in others)
 
 
 def test_more_blocks_than_a_grid_holds():
