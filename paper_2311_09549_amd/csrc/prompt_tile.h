@@ -16,8 +16,8 @@
 // Eight wavefronts of 256 registers fill a compute unit; tiles of 128 keys halve the barriers of tiles of 64 (1,095 -> 1,045 us in the first case below).  bf16, heads of
 // 128: 16,384 rows, 16 heads on 4 key heads in 1,070 us, 1.03 PFLOP/s, where a large product of the library reaches 1.36: matrix pipes busy 0.51 of the time,
 // vector ALUs 0.49 (a maximum, a power of two, a sum and a conversion per score), and LDS reads, 256 rows' worth for every 32 that use them,
-// about as long again.  Twelve packed prompts up to 2,048 rows, 32 heads on 8: 146 us, 0.59 PFLOP/s, half of it the start and end of blocks
-// and tiles that the diagonal cuts.
+// about as long again.  Twelve packed prompts up to 2,048 rows, 32 heads on 8: 146 us, 0.59 PFLOP/s, matrix pipes 0.35: the start and end
+// of blocks, with nothing beside them on the compute unit.
 #pragma once
 
 #include "attention_device.h"
