@@ -29,7 +29,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 
 class Attention:
     """The operators for one head layout.  Holds the workspace of its calls: those of one Attention are to be queued on one stream, or
-    ordered by the caller; more streams at once take an Attention each.  A graph that holds its calls needs it as long as it is replayed."""
+    ordered by the caller; more streams at once take an Attention each.  A graph that holds its calls needs it as long as it is replayed.
+    Tensors are on `device`, which is the current one when a call is made."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
                  rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0"):

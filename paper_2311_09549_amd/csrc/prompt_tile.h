@@ -79,237 +79,237 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 
     // Keys of tiles first_tile .. last_tile - 1 for a block of rows and a group of heads; sums: where the sums go if those are not all tiles that it sees.
     const auto work = [&](const RowBlock &blk, int32_t head_group, int32_t first_tile, int32_t last_tile, float *sums) __attribute__((always_inline)) {
-    uint32_t thread = threadIdx.x;
-    asm volatile("" : "+v"(thread));   // what follows from it is made again for each block, instead of taking the registers of the main loop
-    const int lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64), q = lane % 32, half = lane / 32;
-    const int32_t head0 = head_group << heads_log2, kv = head0 / a.group;
-    const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
-    const int32_t head = head0 + (wave & ((1 << heads_log2) - 1)), first = blk.first + 32 * (wave >> heads_log2), row = first + q;
-    const bool mine = row < blk.end;
-    char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
-    if (length < 0) {
-        if (mine)
-            for (int d = 8 * half; d < a.head_dim; d += 16) *reinterpret_cast<u32x4 *>(out + 2 * d) = u32x4{0, 0, 0, 0} + TR::kExponent * 0x10001u + 0x00010001u;
-        return;
-    }
-
-    const auto sees = [&](int32_t r) { return keys_seen(a, blk, length, r); };
-    int32_t block_most = sees(blk.end - 1);
-    if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
-    const int32_t visible = mine ? sees(row) : 0;
-    const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
-
-    u32x4 qf[DP / 16];
-#pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-        qf[c] = u32x4{0, 0, 0, 0};
-        const int e = (2 * c + half) * 8;
-        if (mine && e < a.head_dim) qf[c] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q.data) + (row * a.q.row + head * a.q.head + e) * 2);
-    }
-    f32x16 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-    float m = kMinusInf, l = 0.0f, from = 0.0f;   // from: what weights are taken against, the maximum (FAR) or its product with scale_log2
-
-    // this thread's pieces of a tile
-    const int piece = thread % CHUNKS, row0 = thread / CHUNKS;
-    const bool held = piece * 8 < a.head_dim;
-    const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * 2, v_row = (PAGED ? a.cache.row : a.v.row) * 2;
-    const char *k0 = PAGED ? static_cast<const char *>(a.cache.keys) + (kv * a.cache.head + piece * 8) * 2
-                           : static_cast<const char *>(a.k.data) + (blk.begin * a.k.row + kv * a.k.head + piece * 8) * 2;
-    const char *v0 = PAGED ? static_cast<const char *>(a.cache.values) + (kv * a.cache.head + piece * 8) * 2
-                           : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head + piece * 8) * 2;
-    bool bad = false;
-    u32x4 ks[LOADS], vs[LOADS];
-    const auto fetch = [&](int32_t base) {
-#pragma unroll
-        for (int n = 0; n < LOADS; ++n) {
-            int32_t key = base + row0 + n * P::ROWS_PER_LOAD;
-            key = key < length ? key : length - 1;   // rows behind the last key are seen by none: any that are there
-            int64_t k_at = key * k_row, v_at = key * v_row;
-            if (PAGED) {
-                int32_t page = page_of(a.s, blk.sequence, key);
-                bad |= page < 0;
-                if (page < 0) page = 0;
-                k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
-            }
-            ks[n] = vs[n] = u32x4{0, 0, 0, 0};
-            if (held) {
-                ks[n] = *reinterpret_cast<const u32x4 *>(k0 + k_at);
-                vs[n] = *reinterpret_cast<const u32x4 *>(v0 + v_at);
-            }
+        uint32_t thread = threadIdx.x;
+        asm volatile("" : "+v"(thread));   // what follows from it is made again for each block, instead of taking the registers of the main loop
+        const int lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64), q = lane % 32, half = lane / 32;
+        const int32_t head0 = head_group << heads_log2, kv = head0 / a.group;
+        const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
+        const int32_t head = head0 + (wave & ((1 << heads_log2) - 1)), first = blk.first + 32 * (wave >> heads_log2), row = first + q;
+        const bool mine = row < blk.end;
+        char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
+        if (length < 0) {
+            if (mine)
+                for (int d = 8 * half; d < a.head_dim; d += 16) *reinterpret_cast<u32x4 *>(out + 2 * d) = u32x4{0, 0, 0, 0} + TR::kExponent * 0x10001u + 0x00010001u;
+            return;
         }
-    };
-    // Tiles that some rows see in part are stored without infinities and NaN among the values, which the product would spread to rows that do not see them
-    // (0 times infinity); the answer is whether there were any.
-    const auto put = [&](char *buffer, bool part) {
-        uint32_t any = 0;
+
+        const auto sees = [&](int32_t r) { return keys_seen(a, blk, length, r); };
+        int32_t block_most = sees(blk.end - 1);
+        if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
+        const int32_t visible = mine ? sees(row) : 0;
+        const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
+
+        u32x4 qf[DP / 16];
 #pragma unroll
-        for (int n = 0; n < LOADS; ++n) {
-            const int r = row0 + n * P::ROWS_PER_LOAD;
-            if (part) {
+        for (int c = 0; c < DP / 16; ++c) {
+            qf[c] = u32x4{0, 0, 0, 0};
+            const int e = (2 * c + half) * 8;
+            if (mine && e < a.head_dim) qf[c] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q.data) + (row * a.q.row + head * a.q.head + e) * 2);
+        }
+        f32x16 o[DT];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    any |= Special<TR>::infinite_or_nan(vs[n][i]);
-                    vs[n][i] = Special<TR>::without(vs[n][i]);
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+        float m = kMinusInf, l = 0.0f, from = 0.0f;   // from: what weights are taken against, the maximum (FAR) or its product with scale_log2
+
+        // this thread's pieces of a tile
+        const int piece = thread % CHUNKS, row0 = thread / CHUNKS;
+        const bool held = piece * 8 < a.head_dim;
+        const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * 2, v_row = (PAGED ? a.cache.row : a.v.row) * 2;
+        const char *k0 = PAGED ? static_cast<const char *>(a.cache.keys) + (kv * a.cache.head + piece * 8) * 2
+                               : static_cast<const char *>(a.k.data) + (blk.begin * a.k.row + kv * a.k.head + piece * 8) * 2;
+        const char *v0 = PAGED ? static_cast<const char *>(a.cache.values) + (kv * a.cache.head + piece * 8) * 2
+                               : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head + piece * 8) * 2;
+        bool bad = false;
+        u32x4 ks[LOADS], vs[LOADS];
+        const auto fetch = [&](int32_t base) {
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                int32_t key = base + row0 + n * P::ROWS_PER_LOAD;
+                key = key < length ? key : length - 1;   // rows behind the last key are seen by none: any that are there
+                int64_t k_at = key * k_row, v_at = key * v_row;
+                if (PAGED) {
+                    int32_t page = page_of(a.s, blk.sequence, key);
+                    bad |= page < 0;
+                    if (page < 0) page = 0;
+                    k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
+                }
+                ks[n] = vs[n] = u32x4{0, 0, 0, 0};
+                if (held) {
+                    ks[n] = *reinterpret_cast<const u32x4 *>(k0 + k_at);
+                    vs[n] = *reinterpret_cast<const u32x4 *>(v0 + v_at);
                 }
             }
-            *reinterpret_cast<u32x4 *>(buffer + r * P::ROW_BYTES + 16 * P::key_piece(r, piece)) = ks[n];
-            *reinterpret_cast<u32x4 *>(buffer + P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, piece)) = vs[n];
-        }
-        return any != 0;
-    };
-    // They are added to the rows that see them, from memory.
-    const auto add_special = [&](int32_t base) {
-#pragma unroll 1
-        for (int32_t key = base; key < base + KT && key < most; ++key) {
-            const char *p = static_cast<const char *>(PAGED ? a.cache.values : a.v.data);
-            if (PAGED) {
-                const int32_t page = page_of(a.s, blk.sequence, key);
-                p += ((page < 0 ? 0 : page) * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + kv * a.cache.head) * 2;
-            } else {
-                p += ((blk.begin + key) * a.v.row + kv * a.v.head) * 2;
-            }
+        };
+        // Tiles that some rows see in part are stored without infinities and NaN among the values, which the product would spread to rows that do not see them
+        // (0 times infinity); the answer is whether there were any.
+        const auto put = [&](char *buffer, bool part) {
+            uint32_t any = 0;
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int n = 0; n < LOADS; ++n) {
+                const int r = row0 + n * P::ROWS_PER_LOAD;
+                if (part) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        any |= Special<TR>::infinite_or_nan(vs[n][i]);
+                        vs[n][i] = Special<TR>::without(vs[n][i]);
+                    }
+                }
+                *reinterpret_cast<u32x4 *>(buffer + r * P::ROW_BYTES + 16 * P::key_piece(r, piece)) = ks[n];
+                *reinterpret_cast<u32x4 *>(buffer + P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, piece)) = vs[n];
+            }
+            return any != 0;
+        };
+        // They are added to the rows that see them, from memory.
+        const auto add_special = [&](int32_t base) {
+#pragma unroll 1
+            for (int32_t key = base; key < base + KT && key < most; ++key) {
+                const char *p = static_cast<const char *>(PAGED ? a.cache.values : a.v.data);
+                if (PAGED) {
+                    const int32_t page = page_of(a.s, blk.sequence, key);
+                    p += ((page < 0 ? 0 : page) * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + kv * a.cache.head) * 2;
+                } else {
+                    p += ((blk.begin + key) * a.v.row + kv * a.v.head) * 2;
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+                        if (key >= visible || e >= a.head_dim) continue;
+                        const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(p)[e];
+                        if ((__builtin_bit_cast(uint16_t, x) & TR::kExponent) == TR::kExponent) o[d][r] += (float)x;
+                    }
+            }
+        };
+
+        // Where the lane reads, of the first buffer: pieces of the keys of its query's number, and its part of a transposing read.  The other rows of a tile are
+        // at constant distances, which are multiples of what the exchange of pieces goes by.
+        int k_at[DP / 16], v_at[DT];
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) k_at[c] = q * P::ROW_BYTES + 16 * P::key_piece(q, 2 * c + half);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int r = 4 * half + lane % 16 / 4, c = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
+            v_at[d] = P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, c) + lane % 2 * 8;
+        }
+        typedef __attribute__((address_space(3))) char *Lds;
+        const auto tile = [&](Lds buffer, int32_t base, auto masked) {
+            constexpr bool MASK = decltype(masked)::value;
+            f32x16 s[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < DP / 16; ++c) {
+                    s[t] = TR::mfma32(*(__attribute__((address_space(3))) u32x4 *)(buffer + k_at[c] + 32 * t * P::ROW_BYTES), qf[c], s[t]);
+                }
+            }
+            float top = kMinusInf;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-                    if (key >= visible || e >= a.head_dim) continue;
-                    const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(p)[e];
-                    if ((__builtin_bit_cast(uint16_t, x) & TR::kExponent) == TR::kExponent) o[d][r] += (float)x;
+                    if (MASK) s[t][r] = 32 * t + 8 * (r / 4) + 4 * half + r % 4 < visible - base ? s[t][r] : kMinusInf;
+                    top = fmaxf(top, s[t][r]);
                 }
-        }
-    };
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any((top - m) * a.scale_log2 > P::kRaise)) {
+                const float next = fmaxf(m, top), base_next = finite_max(next);
+                const float shrink = __builtin_amdgcn_exp2f((m - base_next) * a.scale_log2);
+                m = next;
+                from = FAR ? base_next : base_next * a.scale_log2;
+                l *= shrink;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+            }
+            const float minus = P::kLift - from;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = __builtin_amdgcn_exp2f(FAR ? __builtin_fmaf(s[t][r] - from, a.scale_log2, P::kLift) : __builtin_fmaf(s[t][r], a.scale_log2, minus));
+            u32x4 w[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) {
+                    l += s[t][r] + s[t][r + 1];
+                    w[t][r / 8][r / 2 % 4] = TR::pack(s[t][r], s[t][r + 1]);
+                }
 
-    // Where the lane reads, of the first buffer: pieces of the keys of its query's number, and its part of a transposing read.  The other rows of a tile are
-    // at constant distances, which are multiples of what the exchange of pieces goes by.
-    int k_at[DP / 16], v_at[DT];
+            // operand of tile d of the head and keys 32 t + 16 n + ..
+            const auto values = [&](int d, int t, int n) {
+                u32x4 y;
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) k_at[c] = q * P::ROW_BYTES + 16 * P::key_piece(q, 2 * c + half);
+                for (int h = 0; h < 2; ++h) {
+                    const Lds p = buffer + v_at[d] + (32 * t + 16 * n + 8 * h) * P::ROW_BYTES;
+                    const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p));
+                    y[2 * h] = z.x;
+                    y[2 * h + 1] = z.y;
+                }
+                return y;
+            };
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-        const int r = 4 * half + lane % 16 / 4, c = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
-        v_at[d] = P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, c) + lane % 2 * 8;
-    }
-    typedef __attribute__((address_space(3))) char *Lds;
-    const auto tile = [&](Lds buffer, int32_t base, auto masked) {
-        constexpr bool MASK = decltype(masked)::value;
-        f32x16 s[NT];
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+                for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < DP / 16; ++c) {
-                s[t] = TR::mfma32(*(__attribute__((address_space(3))) u32x4 *)(buffer + k_at[c] + 32 * t * P::ROW_BYTES), qf[c], s[t]);
-            }
+                    for (int d = 0; d < DT; ++d) o[d] = TR::mfma32(values(d, t, n), w[t][n], o[d]);
+        };
+
+        if (block_most > 0) {
+            const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
+            int32_t base = SPLIT ? first_tile * KT : 0;
+            fetch(base);
+            bool special = __syncthreads_or(put(tile_s, base + KT > block_all));
+            int buffer = 0;
+            const auto pass = [&](auto masked) {
+                constexpr bool MASK = decltype(masked)::value;
+                const bool more = base + KT < block_most, part = MASK || base + 2 * KT > block_all;
+                if (more) fetch(base + KT);
+                if (!MASK || base < most) {
+                    tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked);
+                    if (MASK && special) add_special(base);
+                }
+                buffer ^= 1;
+                bool any = false;
+                if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
+                if (part) special = __syncthreads_or(any);
+                else __syncthreads();
+                base += KT;
+            };
+            // tiles that every row of the block sees whole, then the others
+            while (base + KT <= block_all && (!SPLIT || base < block_most)) pass(std::false_type());
+            while (base < block_most) pass(std::true_type());
         }
-        float top = kMinusInf;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if (MASK) s[t][r] = 32 * t + 8 * (r / 4) + 4 * half + r % 4 < visible - base ? s[t][r] : kMinusInf;
-                top = fmaxf(top, s[t][r]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any((top - m) * a.scale_log2 > P::kRaise)) {
-            const float next = fmaxf(m, top), base_next = finite_max(next);
-            const float shrink = __builtin_amdgcn_exp2f((m - base_next) * a.scale_log2);
-            m = next;
-            from = FAR ? base_next : base_next * a.scale_log2;
-            l *= shrink;
+        if (PAGED) bad = __syncthreads_or(bad);
+        l += __shfl_xor(l, 32);
+        if (SPLIT && sums) {
+            float *p = sums + wave * kPromptPiece<DP>;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+                for (int r = 0; r < 4; ++r) reinterpret_cast<f32x4 *>(p)[(4 * d + r) * 64 + lane] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+            p[32 * DP + lane] = m;
+            p[32 * DP + 64 + lane] = PAGED && bad ? __builtin_nanf("") : l;
+            return;
         }
-        const float minus = P::kLift - from;
+        const float factor = PAGED && bad ? __builtin_nanf("") : l == 0.0f ? 0.0f : 1.0f / l;
+        if (mine) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[t][r] = __builtin_amdgcn_exp2f(FAR ? __builtin_fmaf(s[t][r] - from, a.scale_log2, P::kLift) : __builtin_fmaf(s[t][r], a.scale_log2, minus));
-        u32x4 w[NT][2];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                l += s[t][r] + s[t][r + 1];
-                w[t][r / 8][r / 2 % 4] = TR::pack(s[t][r], s[t][r + 1]);
-            }
-
-        // operand of tile d of the head and keys 32 t + 16 n + ..
-        const auto values = [&](int d, int t, int n) {
-            u32x4 y;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const Lds p = buffer + v_at[d] + (32 * t + 16 * n + 8 * h) * P::ROW_BYTES;
-                const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p));
-                y[2 * h] = z.x;
-                y[2 * h + 1] = z.y;
-            }
-            return y;
-        };
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = TR::mfma32(values(d, t, n), w[t][n], o[d]);
-    };
-
-    if (block_most > 0) {
-        const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
-        int32_t base = SPLIT ? first_tile * KT : 0;
-        fetch(base);
-        bool special = __syncthreads_or(put(tile_s, base + KT > block_all));
-        int buffer = 0;
-        const auto pass = [&](auto masked) {
-            constexpr bool MASK = decltype(masked)::value;
-            const bool more = base + KT < block_most, part = MASK || base + 2 * KT > block_all;
-            if (more) fetch(base + KT);
-            if (!MASK || base < most) {
-                tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked);
-                if (MASK && special) add_special(base);
-            }
-            buffer ^= 1;
-            bool any = false;
-            if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
-            if (part) special = __syncthreads_or(any);
-            else __syncthreads();
-            base += KT;
-        };
-        // tiles that every row of the block sees whole, then the others
-        while (base + KT <= block_all && (!SPLIT || base < block_most)) pass(std::false_type());
-        while (base < block_most) pass(std::true_type());
-    }
-    if (PAGED) bad = __syncthreads_or(bad);
-    l += __shfl_xor(l, 32);
-    if (SPLIT && sums) {
-        float *p = sums + wave * kPromptPiece<DP>;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) reinterpret_cast<f32x4 *>(p)[(4 * d + r) * 64 + lane] = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
-        p[32 * DP + lane] = m;
-        p[32 * DP + 64 + lane] = PAGED && bad ? __builtin_nanf("") : l;
-        return;
-    }
-    const float factor = PAGED && bad ? __builtin_nanf("") : l == 0.0f ? 0.0f : 1.0f / l;
-    if (mine) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int e = 32 * d + 2 * r + 4 * half;
-                if (e < a.head_dim)
-                    *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[d][r] * factor, o[d][r + 1] * factor), TR::pack(o[d][r + 2] * factor, o[d][r + 3] * factor)};
-            }
-    }
+                for (int r = 0; r < 16; r += 4) {
+                    const int e = 32 * d + 2 * r + 4 * half;
+                    if (e < a.head_dim)
+                        *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[d][r] * factor, o[d][r + 1] * factor), TR::pack(o[d][r + 2] * factor, o[d][r + 3] * factor)};
+                }
+        }
     };
 
     if constexpr (!SPLIT) {
