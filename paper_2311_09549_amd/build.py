@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -11,7 +13,7 @@ SOURCES = ["host.cpp", "kernels.hip", "kernels_linear.hip", "kernels_order2.hip"
            "attention.cpp", "kernels_append.hip", "kernels_prompt.hip", "kernels_decode.hip"]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-munsafe-fp-atomics",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-Wno-unknown-attributes",
@@ -19,13 +21,20 @@ HIPCC_FLAGS = [
 
 
 def build_library(verbose: bool = False) -> str:
+    """Compiles every source, as many at a time as there are processors (16 at most), and links them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, "-x", "hip"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", LIB_PATH]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd)
+
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(16, len(os.sched_getaffinity(0)))) as pool:
+        names = [os.path.join(objects, s + ".o") for s in SOURCES]
+        compiled = [pool.submit(run, [hipcc, *HIPCC_FLAGS, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, names)]
+        for c in compiled:
+            c.result()
+        run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *names, "-o", LIB_PATH])
     return LIB_PATH
 
 
