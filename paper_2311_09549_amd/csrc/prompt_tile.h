@@ -67,7 +67,7 @@ __device__ __forceinline__ int32_t keys_seen(const AttendArgs &a, const RowBlock
 //
 // SPLIT: as in decode, the tiles of keys of all blocks are put in one line, block after block, one group of heads after the other, and every workgroup takes an
 // equal share of it; blocks that shares cut leave pieces, which prompt_join_kernel joins.  Without it a workgroup has one block, and a call takes as long as
-// the longest of them, or as the compute unit that was given most.  Chunks of four prompts behind up to 8,191 keys, 32 heads of 128: 264 us with, 320
+// the longest of them, or as the compute unit that was given most.  Chunks of four prompts behind up to 8,191 keys, 32 heads of 128: 262 to 274 us with, 320
 // without; L2 misses are six times as many, since workgroups begin at different keys, and the join is 18 us.
 template <typename TR, int DP, bool PAGED, bool FAR, bool SPLIT, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
