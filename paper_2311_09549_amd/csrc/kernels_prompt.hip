@@ -138,7 +138,6 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         int heads_log2 = 0;
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;
-        const bool far = a.scale_log2 > 1.0f;
         // Keys are split where the longest block alone would take longer than everything in equal shares.  The host knows neither lengths nor their sum: the longest
         // is taken as all that the table has room for, or twice the mean of packed sequences, the mean as half of that.  Measured in tiles, the start and
         // the join of a split cost kSplitTiles, and its tiles 1.3 times as much (workgroups that begin at different keys do not meet in L2).  bf16, heads and key heads
@@ -147,13 +146,13 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         const int64_t longest = PAGED ? table_room(a.s) : a.s.batch > 1 ? 2 * (int64_t)a.s.rows / a.s.batch : a.s.rows;
         const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / KT;
         const int shares = prompt_shares(a.n_cu);
-        if (a.pieces && !far && blocks <= kSplitBlocks && tiles > 4 && tiles * shares > kSplitTiles<DP> * shares + 13 * blocks * groups * tiles / 20) {
+        if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && tiles * shares > kSplitTiles<DP> * shares + 13 * blocks * groups * tiles / 20) {
             a.blocks = (int32_t)blocks;
-            prompt_tile_kernel<TR, DP, PAGED, false, true, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
+            prompt_tile_kernel<TR, DP, PAGED, true, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
             prompt_join_kernel<TR, DP, NW><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
             return;
         }
-        const auto kernel = far ? prompt_tile_kernel<TR, DP, PAGED, true, false, NW, KT> : prompt_tile_kernel<TR, DP, PAGED, false, false, NW, KT>;
+        const auto kernel = prompt_tile_kernel<TR, DP, PAGED, false, NW, KT>;
         // a grid has fewer than 2^32 threads
         const int64_t each = (((int64_t)1 << 32) / (64 * NW) - 1) / groups;
         for (int64_t end = blocks; end > 0; end -= each) {

@@ -30,6 +30,9 @@ struct PromptTile {
     static constexpr int LOADS = KT * CHUNKS / THREADS, ROWS_PER_LOAD = THREADS / CHUNKS;
     static constexpr int ROW_BYTES = DP * 2, TILE_BYTES = KT * ROW_BYTES, LDS_BYTES = 4 * TILE_BYTES;
     static constexpr float kRaise = 8.0f;
+    // A weight's exponent is s scale_log2 - m scale_log2 in one operation, off by roundings of the second product: less than 2^-14 of the weight where that
+    // is at most 2^8.  Beyond it, up to products that pass fp32, the difference of the scores is taken first, which is exact where it matters.
+    static constexpr float kFar = 256.0f;
     static constexpr float kLift = TR::kLift > 0.0f ? TR::kLift - kRaise + 1.0f : 0.0f;   // fp16: weights up to 2^15
     static_assert(KT * CHUNKS % THREADS == 0 && ROWS_PER_LOAD * CHUNKS == THREADS, "whole rows per load");
 
@@ -63,13 +66,11 @@ __device__ __forceinline__ int32_t keys_seen(const AttendArgs &a, const RowBlock
     return n < 0 ? 0 : n;
 }
 
-// FAR: the maximum times scale_log2 may be beyond fp32 (a scale above ln 2), so that differences are taken before they are scaled.
-//
 // SPLIT: as in decode, the tiles of keys of all blocks are put in one line, block after block, one group of heads after the other, and every workgroup takes an
 // equal share of it; blocks that shares cut leave pieces, which prompt_join_kernel joins.  Without it a workgroup has one block, and a call takes as long as
 // the longest of them, or as the compute unit that was given most.  Chunks of four prompts behind up to 8,191 keys, 32 heads of 128: 262 to 274 us with, 320
 // without; L2 misses are six times as many, since workgroups begin at different keys, and the join is 18 us.
-template <typename TR, int DP, bool PAGED, bool FAR, bool SPLIT, int NW, int KT>
+template <typename TR, int DP, bool PAGED, bool SPLIT, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
 {
     using P = PromptTile<TR, DP, NW, KT>;
@@ -111,7 +112,8 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-        float m = kMinusInf, l = 0.0f, from = 0.0f;   // from: what weights are taken against, the maximum (FAR) or its product with scale_log2
+        float m = kMinusInf, l = 0.0f;
+        bool far = false;   // of any query of the wavefront
 
         // this thread's pieces of a tile
         const int piece = thread % CHUNKS, row0 = thread / CHUNKS;
@@ -220,19 +222,25 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 const float next = fmaxf(m, top), base_next = finite_max(next);
                 const float shrink = __builtin_amdgcn_exp2f((m - base_next) * a.scale_log2);
                 m = next;
-                from = FAR ? base_next : base_next * a.scale_log2;
+                far = __any(fabsf(base_next * a.scale_log2) > P::kFar);
                 l *= shrink;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
             }
-            const float minus = P::kLift - from;
+            const float from = finite_max(m), minus = far ? P::kLift : P::kLift - from * a.scale_log2;
+            if (far) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[t][r] -= from;
+            }
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = __builtin_amdgcn_exp2f(FAR ? __builtin_fmaf(s[t][r] - from, a.scale_log2, P::kLift) : __builtin_fmaf(s[t][r], a.scale_log2, minus));
+                    s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], a.scale_log2, minus));
             u32x4 w[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t)

@@ -1,0 +1,77 @@
+"""Attention on the GPU at the ends of the types' ranges: scores of the lowest value, values near the largest, infinite values of weight 0."""
+import pytest
+import torch
+
+from paper_2311_09549_amd.attention import Attention
+
+from attention_reference import assert_within, attend, cache_of
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+INF = float("inf")
+
+
+def int32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def lowest_scores(rows, head_dim, dtype, cut):
+    """Queries, keys and values of one head; the first `cut` keys give scores of the type's lowest value, the others ordinary ones."""
+    gen = torch.Generator().manual_seed(head_dim + rows)
+    q, k, v = (torch.randn(rows, 1, head_dim, generator=gen).to(dtype) for _ in range(3))
+    q[..., 0] = 1.0
+    k[:cut] = 0.0
+    k[:cut, 0, 0] = torch.finfo(dtype).min
+    return q, k, v
+
+
+def prompts(q, k, v, paged, **kw):
+    """One sequence, packed or behind an empty cache."""
+    rows, _, head_dim = q.shape
+    attention = Attention(1, 1, head_dim, q.dtype, 16, **kw)
+    if not paged:
+        return attention.prompt(q.cuda(), k.cuda(), v.cuda(), int32([0, rows])).cpu()
+    kc, vc, table = cache_of([k], [v], 16, -(-rows // 16), torch.Generator().manual_seed(1))
+    return attention.prompt_paged(q.cuda(), kc, vc, table, int32([rows]), int32([0, rows])).cpu()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("head_dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("rows,paged", [(20, False), (300, False), (300, True), (2000, False)])
+def test_lowest_scores_alone(dtype, head_dim, rows, paged):
+    """Scores of the lowest value at the usual scale are alike: the mean of the values, which are 1 (but for the rounding of 1 / n and of its product)."""
+    q, k, v = lowest_scores(rows, head_dim, dtype, rows)
+    got = prompts(q, k, torch.ones_like(v), paged)
+    assert bool(((got.double() - 1.0).abs() <= 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("head_dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("paged", [False, True])
+def test_lowest_scores_before_others(dtype, head_dim, paged):
+    """Keys of the lowest scores, more than a tile of them, have weight 0 beside ordinary ones: rows that see some are as if the first were not there."""
+    rows, cut = 500, 300
+    q, k, v = lowest_scores(rows, head_dim, dtype, cut)
+    got = prompts(q, k, v, paged)
+    at = [300, 301, 383, 384, 400, 499]
+    want, bound = attend(q[at], k[cut:], v[cut:], torch.tensor(at) + 1 - cut, head_dim ** -0.5, dtype)
+    assert_within(got[at], want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("scale", [1.0, 30.0, 1e36])
+def test_large_scales(dtype, scale):
+    """Scales at which the product with a score passes the range of 32 bits, or nearly does, in prompts that are split and in others."""
+    gen = torch.Generator().manual_seed(9)
+    for rows in (90, 2000):
+        q, v = torch.zeros(rows, 1, 64), torch.randn(rows, 1, 64, generator=gen).to(dtype)
+        q[..., 0] = 1.0
+        k = torch.zeros(rows, 1, 64)
+        k[:, 0, 0] = -1000.0
+        k[rows // 2, 0, 0] = 1000.0    # from here on the only key of any weight
+        got = prompts(q.to(dtype), k.to(dtype), v, False, scale=scale)
+        want = torch.cat([v[:rows // 2].double().cumsum(0) / torch.arange(1, rows // 2 + 1)[:, None, None], v[rows // 2].double().expand(rows - rows // 2, 1, 64)])
+        size = torch.cat([v[:rows // 2].double().abs().cumsum(0) / torch.arange(1, rows // 2 + 1)[:, None, None], v[rows // 2].double().abs().expand(rows - rows // 2, 1, 64)])
+        # weights are alike, hence exact; fp32 sums of so many terms and their quotient, and the last rounding
+        assert_within(got, want, size * 2.0 ** -24 * (4 * rows + 64) + torch.finfo(dtype).eps / 2 * want.abs() * 1.01 + torch.finfo(dtype).tiny)
