@@ -11,7 +11,7 @@
 // row number), so that the 32 rows that a read of keys touches, and the 4 of a transposing read, lie in different banks.
 //
 // The maximum that weights are taken against is raised only where a score passes it by more than 2^8: sums are rescaled a few times a row instead of at
-// every new maximum, and weights up to 2^8 lose nothing.
+// every new maximum, and weights lose nothing: they are lowered by as much in bf16, which has the exponents of fp32.
 //
 // Eight wavefronts of 256 registers fill a compute unit; tiles of 128 keys halve the barriers of tiles of 64 (1,095 -> 1,045 us in the first case below).  bf16, heads of
 // 128: 16,384 rows, 16 heads on 4 key heads in 1,070 us, 1.03 PFLOP/s, where a large product of the library reaches 1.36: matrix pipes busy 0.51 of the time,
@@ -33,7 +33,8 @@ struct PromptTile {
     // A weight's exponent is s scale_log2 - m scale_log2 in one operation, off by roundings of the second product: less than 2^-14 of the weight where that
     // is at most 2^8.  Beyond it, up to products that pass fp32, the difference of the scores is taken first, which is exact where it matters.
     static constexpr float kFar = 256.0f;
-    static constexpr float kLift = TR::kLift > 0.0f ? TR::kLift - kRaise + 1.0f : 0.0f;   // fp16: weights up to 2^15
+    // Weights up to 2^15 in fp16; up to 1 in bf16, as without the lag, so that sums of values near the largest stay in fp32.
+    static constexpr float kLift = TR::kLift > 0.0f ? TR::kLift - kRaise + 1.0f : -kRaise;
     static_assert(KT * CHUNKS % THREADS == 0 && ROWS_PER_LOAD * CHUNKS == THREADS, "whole rows per load");
 
     // Place of piece c of row r.

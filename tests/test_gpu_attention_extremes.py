@@ -75,3 +75,18 @@ def test_large_scales(dtype, scale):
         size = torch.cat([v[:rows // 2].double().abs().cumsum(0) / torch.arange(1, rows // 2 + 1)[:, None, None], v[rows // 2].double().abs().expand(rows - rows // 2, 1, 64)])
         # weights are alike, hence exact; fp32 sums of so many terms and their quotient, and the last rounding
         assert_within(got, want, size * 2.0 ** -24 * (4 * rows + 64) + torch.finfo(dtype).eps / 2 * want.abs() * 1.01 + torch.finfo(dtype).tiny)
+
+
+@pytest.mark.parametrize("head_dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("paged", [False, True])
+def test_large_values(head_dim, paged):
+    """Values near the largest of bf16 and scores that rise a little from tile to tile: the row's maximum lags, weights do not pass 1 for it."""
+    gen = torch.Generator().manual_seed(head_dim)
+    rows = 200
+    q, k = torch.zeros(rows, 1, head_dim, dtype=BF16), torch.zeros(rows, 1, head_dim, dtype=BF16)
+    q[..., 0] = 1.0
+    k[128:, 0, 0] = 39.0   # 2^7 times the weight of the keys before
+    v = ((0.5 + 0.5 * torch.rand(rows, 1, head_dim, generator=gen)) * 2.0 ** 119).to(BF16)
+    got = prompts(q, k, v, paged, scale=0.125)
+    want, bound = attend(q, k, v, torch.arange(1, rows + 1), 0.125, BF16)
+    assert_within(got, want, bound)
