@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
     constexpr int B = TR::kBytes, LANES = DP / 4, PARTS = 256 / LANES;
     __shared__ f32x4 sum_s[PARTS][LANES];
     __shared__ float weight_s[PARTS], top_s[4], factor_s[1 << kMaxGroupsLog2], total_s[1 << kMaxGroupsLog2];
+    constexpr float kNoPiece = -1.0f;   // no sum of weights.  Pieces of weights 0 are added: infinite values reach their row from them as well
     const int32_t b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x % 64;
     const int part = threadIdx.x / LANES, e = threadIdx.x % LANES * 4;
     const int32_t length = paged_length(a.s, b), n_units = units_of(length);
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
             const int64_t at = (int64_t)piece_slot(first, share0, w) * piece_floats(DP) + kHeadTile * DP + col;
             const float m = none ? kMinusInf : a.pieces[at];
             factor_s[w - w0] = m;
-            total_s[w - w0] = none ? 0.0f : a.pieces[at + kHeadTile];
+            total_s[w - w0] = none ? kNoPiece : a.pieces[at + kHeadTile];
             top = fmaxf(top, m);
         }
 #pragma unroll
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(AttendArgs a)
 #pragma unroll 4
         for (int32_t w = w0 + part; w <= w1; w += PARTS) {
             const float factor = __builtin_amdgcn_exp2f((factor_s[w - w0] - top) * a.scale_log2), total = total_s[w - w0];
-            if (factor_s[w - w0] == kMinusInf && total == 0.0f) continue;   // no piece, or one of weights 0
+            if (total == kNoPiece) continue;
             const float *piece = a.pieces + (int64_t)piece_slot(first, share_begin(units, w, a.groups_log2), w) * piece_floats(DP);
             sum += *reinterpret_cast<const f32x4 *>(piece + col * DP + e) * factor;
             weight += total * factor;

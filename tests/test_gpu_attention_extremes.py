@@ -90,3 +90,25 @@ def test_large_values(head_dim, paged):
     got = prompts(q, k, v, paged, scale=0.125)
     want, bound = attend(q, k, v, torch.arange(1, rows + 1), 0.125, BF16)
     assert_within(got, want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("columns", [32, 400])   # in one kernel, and in pieces
+def test_infinite_values_of_weight_0_reach_their_row(dtype, columns):
+    """128 keys in a row, a piece of their own where the keys are split, have scores of -infinity, weight 0, and one of them an infinite value: 0 times
+    infinity is NaN in the row, as it is from the definition, and so in a prompt's last row."""
+    gen = torch.Generator().manual_seed(3)
+    n = 500
+    k, v = torch.randn(n, 1, 64, generator=gen).to(dtype), torch.randn(n, 1, 64, generator=gen).to(dtype)
+    q = torch.zeros(1, 4, 64, dtype=dtype)
+    q[..., 0] = 1.0
+    k[128:256, 0, 0] = -INF
+    v[200, 0, 5] = INF
+    kc, vc, table = cache_of([k], [v], 16, columns, gen, fill=0.0)
+    attention = Attention(4, 1, 64, dtype, 16)
+    for got in (attention.decode(q.cuda(), kc, vc, table, int32([n])), attention.prompt_paged(q.cuda(), kc, vc, table, int32([n]), int32([0, 1]))):
+        assert bool(torch.isnan(got[..., 5]).all())
+        finite = torch.arange(64) != 5
+        keep = torch.cat([torch.arange(128), torch.arange(256, n)])
+        want, bound = attend(q, k[keep], v[keep], torch.tensor([n - 128]), 0.125, dtype)
+        assert_within(got.cpu()[..., finite], want[..., finite], bound[..., finite])
