@@ -180,6 +180,10 @@ class Attention:
     def _workspace_of(self, stream, given, name):
         """Address and size of a workspace: the caller's, or the handle's own, which is made once and stays where it is (a graph may hold its address)."""
         if given is not None:
+            if given.get_device() != self._index:
+                raise TypeError(f"a workspace has to be on {self.device}, not on {given.device}")
+            if not given.is_contiguous():
+                raise ValueError(f"a workspace has to be contiguous, not {tuple(given.shape)} with strides {given.stride()}")
             return given.data_ptr(), given.numel() * given.element_size()
         own = self._own.get(name)
         if own is None:
