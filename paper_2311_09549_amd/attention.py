@@ -187,7 +187,9 @@ class Attention:
             return given.data_ptr(), given.numel() * given.element_size()
         own = self._own.get(name)
         if own is None:
-            own = self._own[name] = (torch.empty(getattr(self, name), dtype=torch.uint8, device=self.device), {_raw_stream(self._index)})
+            # torch's memory of another stream may still be in use there, by kernels that this stream does not wait for
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
+                own = self._own[name] = (torch.empty(getattr(self, name), dtype=torch.uint8, device=self.device), {stream})
         tensor, streams = own
         if stream not in streams:   # not given away before this stream is done with it either
             streams.add(stream)

@@ -3,11 +3,19 @@ the library's operators."""
 import pytest
 import torch
 
+from paper_2311_09549_amd import attention as module
 from paper_2311_09549_amd.attention import Attention
 
 BF16, F32 = torch.bfloat16, torch.float32
 A = 1 << 20   # an address that is a multiple of 256; nothing is launched here, so nothing is read
 STREAM = 4096   # that of a HIP stream, for a recorder
+
+
+def side_by_side(shape):
+    strides = [1]
+    for n in reversed(shape[1:]):
+        strides.insert(0, strides[0] * n)
+    return tuple(strides)
 
 
 class Record:
@@ -16,7 +24,7 @@ class Record:
     def __init__(self, *shape, dtype=BF16, index=0, strides=None, address=A, requires_grad=False):
         self.shape, self.dtype, self.requires_grad, self._index, self._address = torch.Size(shape), dtype, requires_grad, index, address
         self.device = torch.device("cpu") if index < 0 else torch.device("cuda", index)
-        self._strides = strides or torch.empty(shape, device="meta").stride()
+        self._strides = strides or side_by_side(shape)
 
     def stride(self):
         return self._strides
@@ -34,7 +42,7 @@ class Record:
         return self.dtype.itemsize
 
     def is_contiguous(self):
-        return self._strides == torch.empty(self.shape, device="meta").stride()
+        return self._strides == side_by_side(self.shape)
 
 
 class Recorder:
@@ -94,3 +102,54 @@ def test_workspace_of_the_caller():
     workspace = Record(attention.ws_bytes // 4, dtype=F32, address=3 * A)
     attention.decode(*paged(3), out=Record(3, 4, 64), workspace=workspace, stream=STREAM)
     assert recorder.calls[0][-3:] == (3 * A, attention.ws_bytes, STREAM)
+
+
+class Memory:
+    """Torch's streams and memory for a recorder: which stream was current when a tensor was made, and which streams it was told of."""
+
+    def __init__(self, monkeypatch, current):
+        self.current, self.made, self.told = current, [], {}
+        memory = self
+
+        class Made(Record):
+            def record_stream(self, stream):
+                memory.told.setdefault(self.data_ptr(), []).append(stream)
+
+        class On:
+            def __init__(self, stream):
+                self.stream = stream
+
+            def __enter__(self):
+                self.before, memory.current = memory.current, self.stream
+
+            def __exit__(self, *error):
+                memory.current = self.before
+
+        def empty(*shape, dtype, device):
+            assert torch.device(device) == torch.device("cuda", 0)
+            memory.made.append((memory.current, Made(*(shape[0] if isinstance(shape[0], (tuple, torch.Size)) else shape), dtype=dtype, address=(10 + len(memory.made)) * A)))
+            return memory.made[-1][1]
+
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda address, device=None: address)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: memory.current)
+        monkeypatch.setattr(torch.cuda, "stream", On)
+        monkeypatch.setattr(torch, "empty", empty)
+        monkeypatch.setattr(module, "_empty_like", lambda x: empty(x.shape, dtype=x.dtype, device=x.device))
+        monkeypatch.setattr(module, "_raw_stream", lambda index: memory.current)
+
+
+def test_own_workspace_belongs_to_the_stream_that_uses_it(monkeypatch):
+    """Memory of torch's current stream may still be in use there, by kernels that those of another stream do not wait for."""
+    attention, recorder = recorded()
+    rows, long, out = paged(3), packed(2000), Record(3, 4, 64)
+    memory = Memory(monkeypatch, 7)
+    attention.decode(*rows, out=out, stream=STREAM)
+    attention.prompt(*long, out=Record(2000, 4, 64))
+    assert [on for on, _ in memory.made] == [STREAM, 7]
+    attention.decode(*rows, out=out, stream=STREAM)
+    assert len(memory.made) == 2 and not memory.told
+    attention.decode(*rows, out=out)                    # the current one: not given away before that is done with it
+    attention.decode(*rows, out=out)
+    address = memory.made[0][1].data_ptr()
+    assert memory.told == {address: [7]}
+    assert [call[-3] for call in recorder.calls if call[-2] == attention.ws_bytes] == [address] * 4

@@ -1,0 +1,55 @@
+"""Attention queued on a stream that is not torch's current one."""
+import pytest
+import torch
+
+from paper_2311_09549_amd.attention import Attention
+
+from attention_reference import cache_of
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def int32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def operands():
+    """Calls whose keys are split: of one long sequence in the cache, and of a long packed prompt."""
+    gen = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(3000, 1, 64, generator=gen).to(BF16) for _ in range(2))
+    kc, vc, table = cache_of([k], [v], 64, 50, gen, fill=0.0)
+    q = torch.randn(1, 2, 64, generator=gen).to(BF16).cuda()
+    rows = torch.randn(3000, 2, 64, generator=gen).to(BF16).cuda()
+    return (q, kc, vc, table, int32([3000])), (rows, k.cuda(), v.cuda(), int32([0, 3000]))
+
+
+def busy(gate):
+    """Some milliseconds of work on the current stream."""
+    for _ in range(20):
+        gate = (gate @ gate).clamp_(-1.0, 1.0)
+    return gate
+
+
+def test_first_call_on_another_stream():
+    """The workspaces are made while the current stream still reads memory that was freed on it, of their sizes."""
+    token, prompt = operands()
+    expected = Attention(2, 1, 64, BF16, 64)
+    want = expected.decode(*token).clone(), expected.prompt(*prompt).clone()
+    gate = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    side, ready = torch.cuda.Stream(), torch.cuda.Event()
+    attention = Attention(2, 1, 64, BF16, 64)
+    out = torch.empty_like(token[0]), torch.empty_like(prompt[0])
+    ready.record()
+    side.wait_event(ready)
+    old = [torch.full((size // 4,), 3.0, device="cuda") for size in (attention.ws_bytes, attention.prompt_ws_bytes)]
+    busy(gate)
+    read = [x.clone() for x in old]     # queued behind that
+    del old
+    attention.decode(*token, out=out[0], stream=side.cuda_stream)
+    attention.prompt(*prompt, out=out[1], stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(bool((x == 3.0).all()) for x in read)
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
