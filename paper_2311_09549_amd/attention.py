@@ -64,7 +64,8 @@ class Attention:
         return sc.attention_describe(self.handle)
 
     # -- operators ---------------------------------------------------------------------------------------------------------
-    # `stream`: the address of a HIP stream, torch's current one unless given.  Results that are made here belong to the current one.
+    # `stream`: the address of a HIP stream, torch's current one unless given.  What is made here, results and workspaces, is memory of that
+    # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
         """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None."""
         shape = (k.shape[0], self.kv_heads, self.head_dim)
@@ -74,7 +75,7 @@ class Attention:
         if q is not None:
             shape = (shape[0], self.heads, self.head_dim)
             query = self._rows(q, shape)
-            out, result = self._out(q, out, shape)
+            out, result = self._out(q, out, shape, stream)
         status = self._append(self._h, sequences, query, key, value, result, cache, _raw_stream(self._index) if stream is None else stream)
         if status:
             raise sc.ScError(status, "sc_attention_append")
@@ -85,7 +86,7 @@ class Attention:
         rows = q.shape[0]
         shape, kv_shape = (rows, self.heads, self.head_dim), (rows, self.kv_heads, self.head_dim)
         query, key, value = self._rows(q, shape), self._rows(k, kv_shape), self._rows(v, kv_shape)
-        out, result = self._out(q, out, shape)
+        out, result = self._out(q, out, shape, stream)
         if stream is None:
             stream = _raw_stream(self._index)
         address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or (self.prompt_ws_bytes and rows > _FEW_ROWS) else (None, 0)
@@ -98,7 +99,7 @@ class Attention:
         """Attention of the last rows of each sequence over its keys in the cache."""
         shape = (q.shape[0], self.heads, self.head_dim)
         query = self._rows(q, shape)
-        out, result = self._out(q, out, shape)
+        out, result = self._out(q, out, shape, stream)
         if stream is None:
             stream = _raw_stream(self._index)
         address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or self.prompt_ws_bytes else (None, 0)
@@ -111,7 +112,7 @@ class Attention:
         """Attention of one row per sequence over all its keys in the cache.  `workspace`: device bytes of the caller's, `ws_bytes` of them."""
         shape = (q.shape[0], self.heads, self.head_dim)
         query = self._rows(q, shape)
-        out, result = self._out(q, out, shape)
+        out, result = self._out(q, out, shape, stream)
         if stream is None:
             stream = _raw_stream(self._index)
         address, size = self._workspace_of(stream, workspace, "ws_bytes")
@@ -133,9 +134,15 @@ class Attention:
             raise TypeError(f"rows have to be {self.dtype} on {self.device}, not {x.dtype} on {x.device}")
         raise ValueError(f"rows have to be {shape} with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
 
-    def _out(self, q, out, shape):
+    def _out(self, q, out, shape, stream):
         if out is not None:
             return out, self._rows(out, shape)
+        if stream is not None and stream != _raw_stream(self._index):
+            current = torch.cuda.current_stream(self.device)
+            with self._memory_of(stream):
+                out, result = self._out(q, None, shape, None)
+            out.record_stream(current)
+            return out, result
         out = _empty_like(q)
         stride = out.stride()
         if stride[2] != 1 or 0 in stride:   # of heads that share their memory, or a single one
@@ -177,6 +184,10 @@ class Attention:
     def _refuse_table(self, name, what, x):
         raise ValueError(f"{name}: contiguous int32 on {self.device}, {what}; got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
 
+    def _memory_of(self, stream):
+        """What torch makes here is memory of `stream`: that of another may still be in use there, by kernels that this stream does not wait for."""
+        return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device))
+
     def _workspace_of(self, stream, given, name):
         """Address and size of a workspace: the caller's, or the handle's own, which is made once and stays where it is (a graph may hold its address)."""
         if given is not None:
@@ -187,8 +198,7 @@ class Attention:
             return given.data_ptr(), given.numel() * given.element_size()
         own = self._own.get(name)
         if own is None:
-            # torch's memory of another stream may still be in use there, by kernels that this stream does not wait for
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
+            with self._memory_of(stream):
                 own = self._own[name] = (torch.empty(getattr(self, name), dtype=torch.uint8, device=self.device), {stream})
         tensor, streams = own
         if stream not in streams:   # not given away before this stream is done with it either

@@ -153,3 +153,23 @@ def test_own_workspace_belongs_to_the_stream_that_uses_it(monkeypatch):
     address = memory.made[0][1].data_ptr()
     assert memory.told == {address: [7]}
     assert [call[-3] for call in recorder.calls if call[-2] == attention.ws_bytes] == [address] * 4
+
+
+def test_results_belong_to_the_stream_of_their_call(monkeypatch):
+    """Results that are made for another stream than the current one are memory of that stream, not given away before the current one is done with them."""
+    attention, recorder = recorded()
+    rows, table, starts, long, cache = paged(3), paged(3, batch=1), Record(2, dtype=torch.int32), packed(3), Record(9, 16, 2, 64)
+    workspace = Record(1 << 27, dtype=torch.uint8)
+
+    def append(**kw):
+        return attention.append(*long[:3], cache, cache, Record(3, 5, dtype=torch.int32), Record(3, dtype=torch.int32), **kw)
+
+    calls = (append, lambda **kw: attention.prompt(*long, **kw), lambda **kw: attention.prompt_paged(*table, starts, workspace=workspace, **kw),
+             lambda **kw: attention.decode(*rows, workspace=workspace, **kw))
+    for call in calls:
+        memory = Memory(monkeypatch, 7)
+        made = [call(), call(stream=7), call(stream=STREAM)]
+        assert [on for on, _ in memory.made] == [7, 7, STREAM] and [x for _, x in memory.made] == made
+        assert memory.told == {made[2].data_ptr(): [7]} and memory.current == 7
+        out = Record(3, 4, 64)
+        assert call(out=out, stream=STREAM) is out and len(memory.made) == 3

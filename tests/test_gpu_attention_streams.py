@@ -53,3 +53,29 @@ def test_first_call_on_another_stream():
     torch.cuda.synchronize()
     assert all(bool((x == 3.0).all()) for x in read)
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_results_of_calls_on_another_stream():
+    """Results are made while the current stream still reads memory that was freed on it, of their size."""
+    token, prompt = operands()
+    attention = Attention(2, 1, 64, BF16, 64)
+    want = attention.prompt(*prompt).clone()
+    gate = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    side, ready, done = torch.cuda.Stream(), torch.cuda.Event(), torch.cuda.Event()
+    ready.record()
+    side.wait_event(ready)
+    old = torch.full_like(want, 3.0)
+    busy(gate)
+    read = old.clone()     # queued behind that
+    del old
+    got = attention.prompt(*prompt, stream=side.cuda_stream)
+    done.record(side)
+    torch.cuda.current_stream().wait_event(done)
+    kept = got.clone()     # read on the current stream, behind its work, and freed
+    del got
+    for _ in range(3):
+        attention.prompt(torch.zeros_like(prompt[0]), *prompt[1:], stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert bool((read == 3.0).all())
+    assert torch.equal(kept, want)
