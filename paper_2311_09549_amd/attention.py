@@ -12,6 +12,8 @@ A length counts the new rows of its sequence.  The library's header says what th
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
+
 import torch
 
 from . import binding as sc
@@ -25,12 +27,13 @@ _pack_rows, _pack_cache, _pack_sequences = sc.pack_rows, sc.pack_cache, sc.pack_
 
 # torch's own accessor of a stream's address alone: the stream object around it takes 2 us to make
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class Attention:
     """The operators for one head layout.  Holds the workspace of its calls: those of one Attention are to be queued on one stream, or
     ordered by the caller; more streams at once take an Attention each.  A graph that holds its calls needs it as long as it is replayed.
-    Tensors are on `device`, which is the current one when a call is made."""
+    Tensors are on `device`; calls are made there, whichever is the current one."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
                  rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0"):
@@ -46,15 +49,17 @@ class Attention:
             raise ValueError("the scale of the scores has to be positive")
         if rotary_dim and 2 * len(rotary_freq) != rotary_dim and rotary_dim % 2 == 0:
             raise ValueError("rotary_freq has one angle for each pair of rotary_dim")
-        self.heads, self.kv_heads, self.head_dim, self.page_rows, self.dtype = heads, kv_heads, head_dim, page_rows, dtype
-        self._page = (page_rows, kv_heads, head_dim)
-        self.handle = sc.attention_create(_DTYPES[dtype], heads, kv_heads, head_dim, page_rows, causal, 0.0 if scale is None else scale,
-                                          rotary_freq, interleaved, rotary_dim)
-        self.ws_bytes = sc.attention_workspace_bytes(self.handle)
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError(f"attention runs on a GPU, not on {self.device}")
         self._index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        self.device = torch.device("cuda", self._index)
+        self.heads, self.kv_heads, self.head_dim, self.page_rows, self.dtype = heads, kv_heads, head_dim, page_rows, dtype
+        self._page = (page_rows, kv_heads, head_dim)
+        with torch.cuda.device(self._index) if torch.cuda.is_available() else nullcontext():   # the library asks the current device
+            self.handle = sc.attention_create(_DTYPES[dtype], heads, kv_heads, head_dim, page_rows, causal, 0.0 if scale is None else scale,
+                                              rotary_freq, interleaved, rotary_dim)
+        self.ws_bytes = sc.attention_workspace_bytes(self.handle)
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
         self._own = {}   # workspaces, made by the first calls that need them
         self._h = self.handle.handle
@@ -68,6 +73,8 @@ class Attention:
     # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
         """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None."""
+        if _current_device() != self._index:
+            return self._there(self.append, q, k, v, keys, values, pages, lengths, row_start, out, stream)
         shape = (k.shape[0], self.kv_heads, self.head_dim)
         sequences, cache = self._sequences(shape[0], row_start, lengths, pages), self._cache(keys, values)
         key, value = self._rows(k, shape), self._rows(v, shape)
@@ -83,6 +90,8 @@ class Attention:
 
     def prompt(self, q, k, v, row_start, out=None, workspace=None, stream=None):
         """Attention of the rows of each sequence over the keys and values of the same rows."""
+        if _current_device() != self._index:
+            return self._there(self.prompt, q, k, v, row_start, out, workspace, stream)
         rows = q.shape[0]
         shape, kv_shape = (rows, self.heads, self.head_dim), (rows, self.kv_heads, self.head_dim)
         query, key, value = self._rows(q, shape), self._rows(k, kv_shape), self._rows(v, kv_shape)
@@ -97,6 +106,8 @@ class Attention:
 
     def prompt_paged(self, q, keys, values, pages, lengths, row_start, out=None, workspace=None, stream=None):
         """Attention of the last rows of each sequence over its keys in the cache."""
+        if _current_device() != self._index:
+            return self._there(self.prompt_paged, q, keys, values, pages, lengths, row_start, out, workspace, stream)
         shape = (q.shape[0], self.heads, self.head_dim)
         query = self._rows(q, shape)
         out, result = self._out(q, out, shape, stream)
@@ -110,6 +121,8 @@ class Attention:
 
     def decode(self, q, keys, values, pages, lengths, out=None, workspace=None, stream=None):
         """Attention of one row per sequence over all its keys in the cache.  `workspace`: device bytes of the caller's, `ws_bytes` of them."""
+        if _current_device() != self._index:
+            return self._there(self.decode, q, keys, values, pages, lengths, out, workspace, stream)
         shape = (q.shape[0], self.heads, self.head_dim)
         query = self._rows(q, shape)
         out, result = self._out(q, out, shape, stream)
@@ -120,6 +133,10 @@ class Attention:
         if status:
             raise sc.ScError(status, "sc_attention_decode")
         return out
+
+    def _there(self, operator, *args):
+        with torch.cuda.device(self._index):
+            return operator(*args)
 
     # -- records -----------------------------------------------------------------------------------------------------------
     # The host side of a call is most of the time of a short one: each attribute of a tensor is read once, and the messages are made apart.

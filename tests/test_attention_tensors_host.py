@@ -45,6 +45,12 @@ class Record:
         return self._strides == side_by_side(self.shape)
 
 
+@pytest.fixture(autouse=True)
+def current_device(monkeypatch):
+    """Torch does not know a current device where there is none."""
+    monkeypatch.setattr(module, "_current_device", lambda: 0, raising=False)
+
+
 class Recorder:
     """In the place of an operator of the library."""
 
@@ -173,3 +179,55 @@ def test_results_belong_to_the_stream_of_their_call(monkeypatch):
         assert memory.told == {made[2].data_ptr(): [7]} and memory.current == 7
         out = Record(3, 4, 64)
         assert call(out=out, stream=STREAM) is out and len(memory.made) == 3
+
+
+class Devices:
+    """Torch's current device for a recorder."""
+
+    def __init__(self, monkeypatch, current):
+        self.current, devices = current, self
+
+        class On:
+            def __init__(self, index):
+                self.index = torch.device("cuda", index).index if isinstance(index, int) else index.index
+
+            def __enter__(self):
+                self.before, devices.current = devices.current, self.index
+
+            def __exit__(self, *error):
+                devices.current = self.before
+
+        monkeypatch.setattr(torch.cuda, "device", On)
+        monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: self.current)
+        monkeypatch.setattr(module, "_current_device", lambda: self.current, raising=False)
+
+
+@pytest.mark.parametrize("current", [0, 2])
+def test_calls_are_made_on_the_device_of_the_handle(monkeypatch, current):
+    """A kernel is queued on the current device, whatever its operands are memory of."""
+    attention, _ = recorded()
+    devices, at = Devices(monkeypatch, current), []
+    attention._append = attention._prompt = attention._prompt_paged = attention._decode = lambda *args: at.append(devices.current) or 0
+    rows, table, starts, long, out, workspace = paged(3), paged(3, batch=1), Record(2, dtype=torch.int32), packed(3), Record(3, 4, 64), Record(1 << 27, dtype=torch.uint8)
+    cache = Record(9, 16, 2, 64)
+    assert attention.append(*long[:3], cache, cache, Record(3, 5, dtype=torch.int32), Record(3, dtype=torch.int32), out=out, stream=STREAM) is out
+    assert attention.prompt(*long, out=out, stream=STREAM) is out
+    assert attention.prompt_paged(*table, starts, out=out, workspace=workspace, stream=STREAM) is out
+    assert attention.decode(*rows, out=out, workspace=workspace, stream=STREAM) is out
+    assert at == [0] * 4 and devices.current == current
+
+
+@pytest.mark.parametrize("device,index", [("cuda:1", 1), ("cuda:0", 0), ("cuda", 2)])
+def test_handle_is_made_on_its_device(monkeypatch, device, index):
+    """The library reads how many compute units the current device has."""
+    devices, at = Devices(monkeypatch, 2), []
+    create = module.sc.attention_create
+    monkeypatch.setattr(module.sc, "attention_create", lambda *args: at.append(devices.current) or create(*args))
+    attention = Attention(4, 2, 64, device=device)
+    assert at == [index] and devices.current == 2 and attention.device == torch.device("cuda", index)
+
+
+def test_device_refusals():
+    with pytest.raises(ValueError):
+        Attention(4, 2, 64, device="cpu")
