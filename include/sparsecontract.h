@@ -339,7 +339,7 @@ typedef struct {
     int32_t head_dim;           /* a multiple of 8, 8..256 */
     int32_t page_rows;          /* rows of a page of the cache: a power of two, 16..4096 */
     int32_t causal;             /* prompt: 1 = row at position p sees keys 0..p, 0 = every key of its sequence */
-    float scale;                /* of the scores; 0 = 1 / sqrt(head_dim); not negative */
+    float scale;                /* of the scores; 0 = 1 / sqrt(head_dim); not negative, and scale / ln 2 is a normal number */
     int32_t rotary_dim;         /* append: leading elements of a row that are rotated; even, 0..head_dim */
     int32_t rotary_interleaved; /* 0: element t is paired with t + rotary_dim / 2, 1: 2 t with 2 t + 1 */
     const double *rotary_freq;  /* rotary_dim / 2 angles per position (host memory, read by sc_attention_create only) */

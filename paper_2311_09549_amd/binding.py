@@ -446,6 +446,8 @@ def attention_create(dtype: int, heads: int, kv_heads: int, head_dim: int, page_
                      interleaved=False, rotary_dim=None) -> AttentionHandle:
     """`rotary_freq`: angles per position of the rotated pairs; `rotary_dim`: 2 len(rotary_freq) unless given."""
     d = AttentionDesc(int(dtype), int(heads), int(kv_heads), int(head_dim), int(page_rows), int(causal), float(scale))
+    if scale and not d.scale:
+        raise ValueError(f"the scale of the scores is of 32 bits, which {scale} is too small for")   # 0 would stand for the usual one
     freq = np.ascontiguousarray(rotary_freq if rotary_freq is not None else [], dtype=np.float64)
     d.rotary_dim = 2 * freq.size if rotary_dim is None else int(rotary_dim)
     d.rotary_interleaved = int(interleaved)

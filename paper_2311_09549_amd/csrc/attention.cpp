@@ -126,7 +126,9 @@ extern "C" sc_status sc_attention_create(sc_attention **out, const sc_attention_
     if (d->heads < 1 || d->kv_heads < 1 || d->heads > 4096 || d->heads % d->kv_heads) return SC_ERR_BAD_DIMS;
     if (d->head_dim < 8 || d->head_dim > kMaxHeadDim || d->head_dim % 8) return SC_ERR_BAD_DIMS;
     if (d->page_rows < 16 || d->page_rows > 4096 || (d->page_rows & (d->page_rows - 1))) return SC_ERR_BAD_DIMS;
-    if (!(d->scale >= 0.0f) || std::isinf(d->scale)) return SC_ERR_BAD_DIMS;
+    const double scale = d->scale == 0.0f ? 1.0 / std::sqrt((double)d->head_dim) : (double)d->scale;
+    const float scale_log2 = (float)(scale * 1.4426950408889634);   // 1 / ln 2
+    if (!(scale > 0.0) || !std::isnormal(scale_log2)) return SC_ERR_BAD_DIMS;
     if (d->rotary_dim < 0 || d->rotary_dim > d->head_dim || d->rotary_dim % 2) return SC_ERR_BAD_DIMS;
     if (d->rotary_dim && !d->rotary_freq) return SC_ERR_NULL;
     for (int t = 0; t < d->rotary_dim / 2; ++t)
@@ -140,8 +142,7 @@ extern "C" sc_status sc_attention_create(sc_attention **out, const sc_attention_
     at->page_rows = d->page_rows;
     while ((1 << at->page_shift) < d->page_rows) ++at->page_shift;
     at->causal = d->causal != 0;
-    const double scale = d->scale > 0.0f ? (double)d->scale : 1.0 / std::sqrt((double)d->head_dim);
-    at->scale_log2 = (float)(scale * 1.4426950408889634);   // 1 / ln 2
+    at->scale_log2 = scale_log2;
     at->pairs = d->rotary_dim / 2;
     at->interleaved = d->rotary_interleaved != 0;
     for (int t = 0; t < at->pairs; ++t) at->turns[t] = d->rotary_freq[t] * 0.15915494309189535;   // 1 / (2 pi)
