@@ -15,6 +15,7 @@ from __future__ import annotations
 from contextlib import nullcontext
 
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 from . import binding as sc
 
@@ -33,7 +34,7 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 class Attention:
     """The operators for one head layout.  Holds the workspace of its calls: those of one Attention are to be queued on one stream, or
     ordered by the caller; more streams at once take an Attention each.  A graph that holds its calls needs it as long as it is replayed.
-    Tensors are on `device`; calls are made there, whichever is the current one."""
+    Tensors are on `device`; calls are made there, whichever is the current one.  Inference only: operands that require a gradient are refused."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
                  rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0"):
@@ -142,14 +143,24 @@ class Attention:
     # The host side of a call is most of the time of a short one: each attribute of a tensor is read once, and the messages are made apart.
     def _rows(self, x, shape):
         stride = x.stride()
-        if x.dtype is not self.dtype or x.get_device() != self._index or x.shape != shape or stride[2] != 1:
+        if (x.dtype is not self.dtype or x.get_device() != self._index or x.shape != shape or stride[2] != 1
+                or x.requires_grad or _forward_ad._current_level >= 0):
             self._refuse_rows(x, shape)
         return _pack_rows(x.data_ptr(), stride[0], stride[1])
 
     def _refuse_rows(self, x, shape):
         if x.dtype is not self.dtype or x.get_device() != self._index:
             raise TypeError(f"rows have to be {self.dtype} on {self.device}, not {x.dtype} on {x.device}")
+        if x.shape == shape and x.stride()[2] == 1:
+            return self._refuse_gradient(x)
         raise ValueError(f"rows have to be {shape} with the last dimension contiguous, not {tuple(x.shape)} with strides {x.stride()}")
+
+    def _refuse_gradient(self, *tensors):
+        """Results have none: better an error than training that goes without.  Under torch.no_grad() it is as asked for."""
+        if torch.is_grad_enabled() and any(x.requires_grad for x in tensors):
+            raise RuntimeError("attention has no backward pass: an operand requires a gradient (call it under torch.no_grad(), or on detached tensors)")
+        if _forward_ad._current_level >= 0 and any(_forward_ad.unpack_dual(x).tangent is not None for x in tensors):
+            raise RuntimeError("attention has no derivative: an operand has a tangent")
 
     def _out(self, q, out, shape, stream):
         if out is not None:
@@ -170,13 +181,16 @@ class Attention:
     def _cache(self, keys, values):
         shape, stride, dtype = keys.shape, keys.stride(), self.dtype
         if (keys.dtype is not dtype or values.dtype is not dtype or keys.get_device() != self._index or values.get_device() != self._index
-                or shape[1:] != self._page or stride[3] != 1 or values.shape != shape or values.stride() != stride):
+                or shape[1:] != self._page or stride[3] != 1 or values.shape != shape or values.stride() != stride
+                or keys.requires_grad or values.requires_grad or _forward_ad._current_level >= 0):
             self._refuse_cache(keys, values)
         return _pack_cache(keys.data_ptr(), values.data_ptr(), shape[0], stride[0], stride[1], stride[2])
 
     def _refuse_cache(self, keys, values):
         if any(x.dtype is not self.dtype or x.get_device() != self._index for x in (keys, values)):
             raise TypeError(f"the cache has to be {self.dtype} on {self.device}, not {keys.dtype} on {keys.device} and {values.dtype} on {values.device}")
+        if keys.shape[1:] == self._page and keys.stride()[3] == 1 and values.shape == keys.shape and values.stride() == keys.stride():
+            return self._refuse_gradient(keys, values)
         raise ValueError(f"keys and values have to be (pages, {self.page_rows}, {self.kv_heads}, {self.head_dim}) alike, with the last "
                          f"dimension contiguous, not {tuple(keys.shape)} and {tuple(values.shape)} with strides {keys.stride()} and {values.stride()}")
 

@@ -2,6 +2,7 @@
 the library's operators."""
 import pytest
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from paper_2311_09549_amd import attention as module
 from paper_2311_09549_amd.attention import Attention
@@ -231,3 +232,52 @@ def test_handle_is_made_on_its_device(monkeypatch, device, index):
 def test_device_refusals():
     with pytest.raises(ValueError):
         Attention(4, 2, 64, device="cpu")
+
+
+def operators(attention, q, k, v, keys, values, out=None):
+    """Calls of every operator with these operands, where it has them."""
+    rows, table, lengths, starts = q.shape[0], Record(3, 5, dtype=torch.int32), Record(3, dtype=torch.int32), Record(2, dtype=torch.int32)
+    workspace, kw = Record(1 << 27, dtype=torch.uint8), dict(out=out or Record(3, 4, 64), stream=STREAM)
+    return {
+        "append": lambda: attention.append(q, k, v, keys, values, table, lengths, **kw),
+        "prompt": lambda: attention.prompt(q, k, v, starts, **kw),
+        "prompt_paged": lambda: attention.prompt_paged(q, keys, values, Record(1, 5, dtype=torch.int32), Record(1, dtype=torch.int32), starts, workspace=workspace, **kw),
+        "decode": lambda: attention.decode(q, keys, values, table, lengths, workspace=workspace, **kw),
+    }
+
+
+TAKES = dict(q=("append", "prompt", "prompt_paged", "decode"), k=("append", "prompt"), v=("append", "prompt"), keys=("append", "prompt_paged", "decode"),
+             values=("append", "prompt_paged", "decode"), out=("append", "prompt", "prompt_paged", "decode"))
+
+
+@pytest.mark.parametrize("name", sorted(TAKES))
+def test_operands_that_require_a_gradient(name):
+    """There is no backward pass: results would be without a gradient, silently."""
+    attention, recorder = recorded()
+    cache = (9, 16, 2, 64)
+    shapes = dict(q=(3, 4, 64), k=(3, 2, 64), v=(3, 2, 64), keys=cache, values=cache, out=(3, 4, 64))
+    operands = {n: Record(*shape, requires_grad=n == name) for n, shape in shapes.items()}
+    for op, call in operators(attention, **operands).items():
+        if op in TAKES[name]:
+            with pytest.raises(RuntimeError, match="gradient"):
+                call()
+    assert not recorder.calls or name in ("k", "v", "keys", "values")
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            for call in operators(attention, **operands).values():
+                call()
+
+
+def test_operands_with_a_tangent(monkeypatch):
+    attention, recorder = recorded()
+    dual, plain = Record(3, 4, 64), {n: Record(*s) for n, s in dict(k=(3, 2, 64), v=(3, 2, 64), keys=(9, 16, 2, 64), values=(9, 16, 2, 64)).items()}
+    monkeypatch.setattr(forward_ad, "unpack_dual", lambda x: forward_ad.UnpackedDualTensor(x, x if x is dual else None))
+    for call in operators(attention, dual, **plain).values():
+        call()   # at no level there is none
+    with forward_ad.dual_level():
+        for call in operators(attention, dual, **plain).values():
+            with pytest.raises(RuntimeError, match="tangent"):
+                call()
+        for call in operators(attention, Record(3, 4, 64), **plain).values():
+            call()
+    assert len(recorder.calls) == 8
