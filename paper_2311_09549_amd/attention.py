@@ -21,8 +21,6 @@ from . import binding as sc
 
 _DTYPES = {torch.bfloat16: sc.SC_BF16, torch.float16: sc.SC_F16, torch.float32: sc.SC_F32}
 
-_FEW_ROWS = 512   # packed prompts of no more are never split along their keys
-
 _INT32, _empty_like = torch.int32, torch.empty_like
 _pack_rows, _pack_cache, _pack_sequences = sc.pack_rows, sc.pack_cache, sc.pack_sequences
 
@@ -62,6 +60,7 @@ class Attention:
                                               rotary_freq, interleaved, rotary_dim)
         self.ws_bytes = sc.attention_workspace_bytes(self.handle)
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
+        self._few_rows = 4 * (32 if head_dim > 128 else 128)   # of a packed prompt: no more than four tiles of keys, which the library never splits
         self._own = {}   # workspaces, made by the first calls that need them
         self._h = self.handle.handle
         self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
@@ -99,7 +98,7 @@ class Attention:
         out, result = self._out(q, out, shape, stream)
         if stream is None:
             stream = _raw_stream(self._index)
-        address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or (self.prompt_ws_bytes and rows > _FEW_ROWS) else (None, 0)
+        address, size = self._workspace_of(stream, workspace, "prompt_ws_bytes") if workspace is not None or (self.prompt_ws_bytes and rows > self._few_rows) else (None, 0)
         status = self._prompt(self._h, self._sequences(rows, row_start, None, None), query, key, value, result, address, size, stream)
         if status:
             raise sc.ScError(status, "sc_attention_prompt")

@@ -281,3 +281,19 @@ def test_operands_with_a_tangent(monkeypatch):
         for call in operators(attention, Record(3, 4, 64), **plain).values():
             call()
     assert len(recorder.calls) == 8
+
+
+@pytest.mark.parametrize("head_dim,rows", [(256, 129), (136, 416), (256, 512), (128, 513), (64, 2000)])
+def test_prompts_that_may_be_split_have_a_workspace(monkeypatch, head_dim, rows):
+    """Whether a packed prompt is split is the library's to say, from five tiles of keys on: 32 keys above a head size of 128, else 128."""
+    attention, recorder = recorded(head_dim=head_dim)
+    memory = Memory(monkeypatch, 7)
+    attention.prompt(*packed(rows, head_dim=head_dim), out=Record(rows, 4, head_dim))
+    assert recorder.calls[0][-3:] == (memory.made[0][1].data_ptr(), attention.prompt_ws_bytes, 7)
+
+
+@pytest.mark.parametrize("head_dim,rows", [(256, 128), (128, 512), (8, 1)])
+def test_prompts_that_are_never_split_have_none(head_dim, rows):
+    attention, recorder = recorded(head_dim=head_dim)
+    attention.prompt(*packed(rows, head_dim=head_dim), out=Record(rows, 4, head_dim), stream=STREAM)
+    assert recorder.calls[0][-3:] == (None, 0, STREAM)
