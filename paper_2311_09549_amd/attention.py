@@ -72,7 +72,7 @@ class Attention:
     # `stream`: the address of a HIP stream, torch's current one unless given.  What is made here, results and workspaces, is memory of that
     # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
-        """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None."""
+        """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None, and then there is no result."""
         if _current_device() != self._index:
             return self._there(self.append, q, k, v, keys, values, pages, lengths, row_start, out, stream)
         shape = (k.shape[0], self.kv_heads, self.head_dim)
@@ -83,6 +83,8 @@ class Attention:
             shape = (shape[0], self.heads, self.head_dim)
             query = self._rows(q, shape)
             out, result = self._out(q, out, shape, stream)
+        elif out is not None:
+            raise ValueError("out is for rotated queries, and there are no queries")
         status = self._append(self._h, sequences, query, key, value, result, cache, _raw_stream(self._index) if stream is None else stream)
         if status:
             raise sc.ScError(status, "sc_attention_append")

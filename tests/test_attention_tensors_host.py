@@ -297,3 +297,13 @@ def test_prompts_that_are_never_split_have_none(head_dim, rows):
     attention, recorder = recorded(head_dim=head_dim)
     attention.prompt(*packed(rows, head_dim=head_dim), out=Record(rows, 4, head_dim), stream=STREAM)
     assert recorder.calls[0][-3:] == (None, 0, STREAM)
+
+
+def test_append_without_queries_has_no_result():
+    """A place for rotated queries without queries would be given back as it was."""
+    attention, recorder = recorded()
+    rows = Record(3, 2, 64), Record(3, 2, 64), Record(9, 16, 2, 64), Record(9, 16, 2, 64), Record(3, 5, dtype=torch.int32), Record(3, dtype=torch.int32)
+    assert attention.append(None, *rows, stream=STREAM) is None and len(recorder.calls) == 1
+    with pytest.raises(ValueError, match="queries"):
+        attention.append(None, *rows, out=Record(3, 4, 64), stream=STREAM)
+    assert len(recorder.calls) == 1
