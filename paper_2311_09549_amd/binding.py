@@ -451,6 +451,8 @@ def attention_create(dtype: int, heads: int, kv_heads: int, head_dim: int, page_
     freq = np.ascontiguousarray(rotary_freq if rotary_freq is not None else [], dtype=np.float64)
     d.rotary_dim = 2 * freq.size if rotary_dim is None else int(rotary_dim)
     d.rotary_interleaved = int(interleaved)
+    if freq.size and d.rotary_dim % 2 == 0 and d.rotary_dim > 2 * freq.size:
+        raise ValueError(f"a rotation of {d.rotary_dim} elements takes {d.rotary_dim // 2} angles, not {freq.size}")   # the library would read on
     if freq.size:
         d.rotary_freq = freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
     h = ctypes.c_void_p()
