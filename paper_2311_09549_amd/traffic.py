@@ -4,8 +4,8 @@ Two `rocprofv3 --pmc` runs of `bench.py --calibrate-copy` (one collecting FETCH_
 WRITE_SIZE, both in KiB per dispatch) hold, next to the kernel of interest, dispatches of the
 library's plain copy kernel, which reads and writes a known number of bytes.  The ratio of
 what a counter reads for the copy to the copy's true size turns the kernel's counter value
-into bytes.  The result is stored with a digest of the kernel sources; `lookup` returns it
-only while the sources are unchanged.
+into bytes.  The result is stored with digests of the kernel sources and of the header; `lookup`
+returns it only while both are unchanged.
 
 Usage (from the repository root, after the two counter runs):
 
@@ -29,10 +29,12 @@ COPY_BYTES = 1 << 30  # size of the calibration copy bench.py queues (well beyon
 
 # Sources of the attention operators, which no contraction runs.
 ATTENTION = ("attention.cpp", "attention.h", "attention_device.h", "kernels_append.hip", "kernels_decode.hip", "kernels_prompt.hip", "prompt_tile.h")
+HEADER = os.path.join(HERE, "..", "include", "sparsecontract.h")
+ATTENTION_DECLARATIONS = " * Attention over packed rows and over a paged cache.\n"   # where they begin
 
 
 def source_digest() -> str:
-    """sha256 over the kernel and host sources that contractions are built from (the header declares their entry points and others')."""
+    """sha256 over the kernel and host sources that contractions are built from."""
     h = hashlib.sha256()
     files = sorted(f for f in glob.glob(os.path.join(HERE, "csrc", "*")) if os.path.basename(f) not in ATTENTION)
     for f in files:
@@ -40,6 +42,16 @@ def source_digest() -> str:
         with open(f, "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()
+
+
+def header_digest(path: str = HEADER) -> str:
+    """sha256 over the header without the declarations of attention, which are its end."""
+    with open(path) as f:
+        text = f.read()
+    at = text.find(ATTENTION_DECLARATIONS)
+    if at < 0:
+        raise ValueError(f"no declarations of attention in {path}")
+    return hashlib.sha256(text[:at].encode()).hexdigest()
 
 
 def _per_dispatch_mean(run_dir: str, counter: str, kernel_substr: str) -> float:
@@ -66,7 +78,7 @@ def lookup(key: str, path: str = DEFAULT_PATH):
     with open(path) as fh:
         rec = json.load(fh)
     ent = rec.get("entries", {}).get(key)
-    if ent is None or ent.get("source_sha256") != source_digest():
+    if ent is None or ent.get("source_sha256") != source_digest() or ent.get("header_sha256") != header_digest():
         return None
     return ent
 
@@ -94,7 +106,7 @@ def main() -> int:
         "fetch_factor": f_fetch, "write_factor": f_write,
         "hbm_read_bytes": k_fetch / f_fetch, "hbm_write_bytes": k_write / f_write,
         "hbm_bytes": k_fetch / f_fetch + k_write / f_write,
-        "source_sha256": source_digest(),
+        "source_sha256": source_digest(), "header_sha256": header_digest(),
     }
     if a.mfma_dir:
         # busy cycles of the matrix pipes summed over the four SIMDs of every CU, over the CUs' busy cycles
