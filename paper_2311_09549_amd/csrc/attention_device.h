@@ -94,16 +94,6 @@ __device__ __forceinline__ float over_groups_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// Maximum over the two lanes 32 apart, without LDS: the swap exchanges the upper half of one register with the lower half of another.
-__device__ __forceinline__ float over_halves_max(float x)
-{
-    uint32_t lo = __builtin_bit_cast(uint32_t, x), hi = lo;
-    asm volatile("" : "+v"(hi));   // a register of its own: a swap within one exchanges its halves
-    const auto y = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
-    const uint32_t first = y[0], second = y[1];
-    return fmaxf(__builtin_bit_cast(float, first), __builtin_bit_cast(float, second));
-}
-
 // A maximum of -infinity (no key yet, or scores of -infinity alone) is taken as 0 in differences: weights 0 instead of NaN.
 __device__ __forceinline__ float finite_max(float m) { return m == kMinusInf ? 0.0f : m; }
 
