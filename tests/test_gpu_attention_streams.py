@@ -79,3 +79,27 @@ def test_results_of_calls_on_another_stream():
     torch.cuda.synchronize()
     assert bool((read == 3.0).all())
     assert torch.equal(kept, want)
+
+
+@pytest.mark.parametrize("named", [False, True])
+def test_first_call_in_a_capture(named):
+    """A handle whose first calls are captured: its workspaces and results are the graph's memory, replays and eager calls beside them are right."""
+    token, prompt = operands()
+    expected = Attention(2, 1, 64, BF16, 64)
+    want = expected.decode(*token).clone(), expected.prompt(*prompt).clone()
+    torch.cuda.synchronize()
+    attention, side, graph = Attention(2, 1, 64, BF16, 64), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    kw = dict(stream=side.cuda_stream) if named else {}
+    with torch.cuda.graph(graph, stream=side):
+        got = attention.decode(*token, **kw), attention.prompt(*prompt, **kw)
+    for _ in range(3):
+        for x in got:
+            x.fill_(float("nan"))
+        others = [torch.full((1 << 22,), 3.0, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(attention.decode(*token), want[0]) and torch.equal(attention.prompt(*prompt), want[1])
+        torch.cuda.synchronize()
+        assert all(bool((x == 3.0).all()) for x in others)
