@@ -355,7 +355,7 @@ typedef struct {
 /* Cache of keys and values in pages: element (p, r, h, d) at keys[p * page_stride + r * row_stride + h * head_stride + d], and
  * likewise in values. */
 typedef struct {
-    void *keys, *values;
+    void *keys, *values;        /* no two elements of one may coincide */
     int64_t pages;
     int64_t page_stride, row_stride, head_stride;
 } sc_cache_view;
@@ -363,7 +363,8 @@ typedef struct {
 /* The sequences of a call.  `rows` counts the rows of its queries (and of packed keys and values): sequence b has the rows
  * [row_start[b], row_start[b + 1]), and row_start = NULL gives each sequence one row (rows = batch).  length[b] is the number of
  * keys of the sequence, its new rows included, so that its n rows are at positions length[b] - n .. length[b] - 1.
- * length = NULL (packed keys): as many as its rows.  Key j of sequence b is row j % page_rows of page
+ * length = NULL (packed keys): as many as its rows.  The host does not see lengths: where a choice between kernels depends on them it goes by what page_count
+ * has room for, so that a table of fixed width is better handed over with as small a page_count as the caller knows to be enough (page_ld stays).  Key j of sequence b is row j % page_rows of page
  * page[b * page_ld + j / page_rows]; a sequence has page_count entries, of which those that length[b] reaches are read.
  * Device memory all of it.  Kernels take row starts as if clamped to 0..rows; rows of no sequence are not written, and what they hold does not matter.  At most 2^24 - 1
  * rows, 2^20 - 1 sequences and 2^30 keys of one (more are a wrong length). */
@@ -401,8 +402,8 @@ sc_status sc_attention_append(const sc_attention *attention, const sc_sequence_v
                               const sc_rows_view *v, const sc_rows_view *q_out, const sc_cache_view *cache, void *hip_stream);
 
 /* Attention of the rows of each sequence over the keys and values of the same rows, packed side by side (length must be NULL).
- * `out` (heads heads) must not overlap the inputs.  `workspace` may be NULL; with one, few long sequences are split over the whole GPU along
- * their keys (a second kernel joins the pieces). */
+ * `out` (heads heads) must not overlap the inputs.  `workspace` may be NULL; with one, few long sequences of 16-bit types are split over the whole GPU
+ * along their keys (a second kernel joins the pieces), which gives other bits than without. */
 sc_status sc_attention_prompt(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_rows_view *k,
                               const sc_rows_view *v, const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
@@ -413,7 +414,8 @@ sc_status sc_attention_prompt_paged(const sc_attention *attention, const sc_sequ
                                     const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Attention of one row per sequence (row_start must be NULL) over all its keys in the cache.  Wrong lengths and page numbers as
- * for prompts.  Queues two kernels: pieces of equal length for the whole GPU, then the join of rows that have several. */
+ * for prompts.  Queues two kernels: pieces of equal length for the whole GPU, then the join of rows that have several; or one, where the table has
+ * room for few keys. */
 sc_status sc_attention_decode(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_cache_view *cache,
                               const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -9,6 +9,9 @@ and strides to the library and queues its kernels.  No arithmetic happens here.
 `q` is (rows, heads, head_dim), `k` and `v` (rows, kv_heads, head_dim), `keys` and `values` (pages, page_rows, kv_heads, head_dim); any strides
 that are multiples of 16 bytes, head_dim contiguous.  `pages` (batch, columns), `lengths` (batch) and `row_start` (batch + 1) are int32.
 A length counts the new rows of its sequence.  The library's header says what the kernels make of wrong lengths and page numbers.
+
+Choices between kernels go by the width of `pages`, for lengths are in device memory: where a table has room for many more keys than there are,
+`pages[:, :columns]` with as many columns as the longest length takes makes short calls shorter (a sequence with more keys than that becomes NaN).
 """
 from __future__ import annotations
 
@@ -70,7 +73,8 @@ class Attention:
 
     # -- operators ---------------------------------------------------------------------------------------------------------
     # `stream`: the address of a HIP stream, torch's current one unless given.  What is made here, results and workspaces, is memory of that
-    # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.
+    # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.  `out` is apart from the other operands,
+    # but for append's.
     def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
         """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None, and then there is no result."""
         if _current_device() != self._index:

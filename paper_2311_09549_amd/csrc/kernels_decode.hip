@@ -7,8 +7,9 @@
 // sums with their maximum and weight in the workspace, and a second kernel joins the pieces in order.
 //
 // 32 heads of 128 on 8: 64 sequences up to 8,191 keys, fp16, in 104 us (4.75 TB/s); 64 heads on 8, one sequence of 131,071 keys, bf16, in 100 us (5.4 TB/s; a large copy reaches
-// 4.8).  The join is 7.5 us of either.  16 heads of 80 with keys of their own, 24 sequences up to 1,500, fp32: 35 us (2.6 TB/s), a third of it
-// matrix products of which one column in sixteen is used.
+// 4.8).  The join is 7.5 us of either.  16 heads of 80 with keys of their own, 24 sequences up to 1,500, fp32: 35 us (2.6 TB/s).  Segments have 372 keys
+// there and a workgroup two or three units, so that the largest share has 384 keys beside a mean of 279; the matrix pipes, with one column in
+// sixteen of use, are busy a third of the time.
 #include "attention_device.h"
 
 namespace sck {
@@ -364,7 +365,8 @@ template <typename TR, int DP, bool EXACT>
 void launch_exact(const AttendArgs &a, hipStream_t stream)
 {
     // Few keys: a workgroup for each segment does with them before shares are found and pieces joined.  bf16, 32 heads of 128 on 8, us here and with shares: one sequence
-    // of 64 keys 4.3 and 8.1, of 333 7.2 and 11.6, of 512 8.7 and 12.5; 64 sequences of 512 25.9 and 28.2.
+    // of 64 keys 4.3 and 8.1, of 333 7.2 and 11.6, of 512 8.7 and 12.5; 64 sequences of 512 25.9 and 28.2.  Lengths are in device memory: the most that the
+    // table has room for decides, and a table for many more keys takes the longer way.
     if (table_room(a.s) <= kWholeKeys && (int64_t)a.s.batch * a.kv_heads * a.head_tiles < 1 << 22) {
         decode_whole_kernel<TR, DP, EXACT><<<a.s.batch * a.kv_heads * a.head_tiles, 64 * kWholeWaves<DP>, 0, stream>>>(a);
         return;

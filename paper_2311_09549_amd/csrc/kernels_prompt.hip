@@ -5,8 +5,9 @@
 // wavefront, keep up with them.  SPLIT: the four wavefronts of a workgroup have the same 16 rows and every fourth step of their keys; otherwise 16 rows
 // each and all keys.
 //
-// Five prompts up to 777 rows, 8 heads of 96 on 2: 37 us (30 TFLOP/s; a large product of the library reaches 153), 48 with the blocks in the order of their rows: matrix pipes busy a third of
-// the time, a quarter of it with the padding to 128.
+// Five prompts up to 777 rows, 8 heads of 96 on 2: 37 us (30 TFLOP/s; a large product of the library reaches 153), 48 with the blocks in the order of their rows.  Matrix pipes are busy a third of
+// the time, padding to 128 included: the 728 workgroups have 4.2 steps a wavefront on average, beside the search for their block, its rank among the others, the first
+// keys and a join, and the heads of a key head read its keys each for itself.
 #include <type_traits>
 
 #include "prompt_tile.h"
@@ -139,7 +140,8 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;
         // Keys are split where the longest block alone would take longer than everything in equal shares.  The host knows neither lengths nor their sum: the longest
-        // is taken as all that the table has room for, or twice the mean of packed sequences, the mean as half of that.  Measured in tiles, the start and
+        // is taken as all that the table has room for, or twice the mean of packed sequences, the mean as half of that.  (A table for many more keys than there are
+        // is split for nothing: 32, 8, 128, 4 sequences of 16 rows behind 100 keys 27 us with a table for 8,192, 10 with a view of the columns in use.)  Measured in tiles, the start and
         // the join of a split cost kSplitTiles, and its tiles 1.3 times as much (workgroups that begin at different keys do not meet in L2).  bf16, heads and key heads
         // of d, with and without a split: 8, 1, 128, 4,096 rows 80 and 118 us; 4, 4, 256, 2,000 rows 69 and 128; 8, 8, 64, 2,000 rows 38 and 46; chunks
         // behind up to 8,191 keys, 32, 8, 128: 264 and 320; but 32, 8, 128, 2,048 rows 90 and 73, 4,000 rows 196 and 172, 600 rows 50 and 29.

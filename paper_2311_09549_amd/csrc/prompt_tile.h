@@ -14,9 +14,9 @@
 // every new maximum, and weights lose nothing: they are lowered by as much in bf16, which has the exponents of fp32.
 //
 // Eight wavefronts of 256 registers fill a compute unit; tiles of 128 keys halve the barriers of tiles of 64 (1,095 -> 1,045 us in the first case below).  bf16, heads of
-// 128: 16,384 rows, 16 heads on 4 key heads in 1,070 us, 1.03 PFLOP/s, where a large product of the library reaches 1.36: matrix pipes busy 0.51 of the time,
+// 128: 16,384 rows, 16 heads on 4 key heads in 1,070 us, 1.03 PFLOP/s, where a large product of the library reaches 1.36: matrix pipes busy 0.50 of the time,
 // vector ALUs 0.49 (a maximum, a power of two, a sum and a conversion per score), and LDS reads, 256 rows' worth for every 32 that use them,
-// about as long again.  Twelve packed prompts up to 2,048 rows, 32 heads on 8: 146 us, 0.59 PFLOP/s, matrix pipes 0.35: the start and end
+// about as long again.  Twelve packed prompts up to 2,048 rows, 32 heads on 8: 146 us, 0.59 PFLOP/s, matrix pipes 0.34: the start and end
 // of blocks, with nothing beside them on the compute unit.
 #pragma once
 
@@ -126,6 +126,8 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                                : static_cast<const char *>(a.v.data) + (blk.begin * a.v.row + kv * a.v.head + piece * 8) * 2;
         bool bad = false;
         u32x4 ks[LOADS], vs[LOADS];
+        // In pages a row's keys and values wait for its page number, within every tile: chunks of four prompts behind up to 8,191 keys take 5.0 us a tile
+        // without a split, packed keys 4.1.
         const auto fetch = [&](int32_t base) {
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) {
