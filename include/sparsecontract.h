@@ -419,6 +419,77 @@ sc_status sc_attention_prompt_paged(const sc_attention *attention, const sc_sequ
 sc_status sc_attention_decode(const sc_attention *attention, const sc_sequence_view *sequences, const sc_rows_view *q, const sc_cache_view *cache,
                               const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* A handle whose rows see a window: a row at position p sees keys p - window + 1 .. p, and of the keys before those the first `sinks` (0: none).  Prompts, decode and trees go by
+ * it; desc->causal has to be 1.  Keys that no row of a call sees are not read, nor the entries of pages that hold none that one sees: those may be anything.
+ * `window` 1..2^30, `sinks` 0..2^30.  The decoding workspace of such a handle is larger. */
+sc_status sc_attention_create_window(sc_attention **out, const sc_attention_desc *desc, int32_t window, int32_t sinks);
+
+/* Trees of drafted rows.  The rows of a sequence are the nodes of a tree (of several, side by side) behind the length - n keys before them: node i is
+ * stored as key length - n + i, in the order of the rows, and parent[r] is the number, among the rows of its sequence, of the node that row r follows: a smaller one than its own, or -1
+ * for a row that follows the keys before the tree.  A node's position is that of the keys before the tree plus its depth.  It sees those keys, the nodes that it descends from and
+ * itself (through a window: by their positions).  `parent` is device memory, a number for each row.  A number that is neither -1 nor a smaller
+ * one is wrong, for its row and those that descend from it; a length below the number of rows, or more than 1,024 of them with parents, is a wrong length.
+ *
+ * sc_attention_append for nodes: rows are rotated by the positions of nodes and stored in their order.  Rows with wrong numbers and rows of sequences with
+ * wrong lengths are not stored. */
+sc_status sc_attention_append_tree(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const sc_rows_view *q, const sc_rows_view *k,
+                                   const sc_rows_view *v, const sc_rows_view *q_out, const sc_cache_view *cache, void *hip_stream);
+
+/* Bytes of device workspace sc_attention_tree needs (256-byte aligned, contents arbitrary).  Calls that share it must not overlap, and it is none of the others'. */
+sc_status sc_attention_tree_workspace_bytes(const sc_attention *attention, size_t *bytes);
+
+/* Attention of nodes over keys and values in the cache.  parent = NULL: each row follows the one before it, as in prompts, for few rows a sequence (no limit to
+ * their number).  Wrong lengths, page numbers and parents make NaN of the rows that they concern.  Queues two kernels, as decode does. */
+sc_status sc_attention_tree(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const sc_rows_view *q, const sc_cache_view *cache,
+                            const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The sequences go on from node last[b] of their trees (-1: from the keys before the tree): the keys and values of the path to it move to the places behind those keys, in
+ * order, and length_out[b] (NULL: not wanted) becomes their number with the path's, -1 where the length, the path or last[b] is wrong: nothing moves there.
+ * What rows behind the new length hold is not specified.  A row whose old or new place is in no page of the cache does not move.  Other layers of a model
+ * take the same call with their caches and the same (old) lengths; `length_out` is apart from them.  One kernel. */
+sc_status sc_attention_accept(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const int32_t *last, const sc_cache_view *cache,
+                              int32_t *length_out, void *hip_stream);
+
+/* Tables of pages, lengths, and holders: holders[p] is the number of entries that hold page p, of those that the length of their sequence reaches, 0 for a free page.
+ * All of it device memory.  `page_out` has page_count entries a sequence as well. */
+typedef struct {
+    int32_t batch, new_batch;
+    int64_t pages;              /* of the cache */
+    const int32_t *page;        /* entries of sequence b: page[b * page_ld .. + page_count - 1] */
+    int64_t page_ld, page_count;
+    const int32_t *length, *holders;
+    const int32_t *parent, *wanted;   /* fork, new_batch each; wanted may be NULL */
+    int32_t *page_out;
+    int64_t page_out_ld;
+    int32_t *length_out;        /* fork */
+    int32_t *holders_out;       /* may be holders */
+    int32_t *moves;             /* triples: page, page that it is copied to, rows of it */
+} sc_pages_view;
+
+/* Bytes of device workspace that sc_attention_fork needs for so many pages and new sequences, and sc_attention_compact for so many pages and new_batch = 0. */
+sc_status sc_attention_pages_workspace_bytes(int64_t pages, int32_t new_batch, size_t *bytes);
+
+/* The next batch of sequences from the present one: new sequence i has the first rows of sequence parent[i] (none for -1), as many of them as wanted[i] says (NULL: all), and room
+ * for the rest of the wanted[i] rows.  A sequence of the present batch that is nobody's parent is given up, and its pages become free; several may have one parent.
+ *   - Whole pages are shared.  A page that new sequences keep in part, and are going to write to, stays with the first of them, if no entry holds it whole; the others get a copy: moves[3 i ..]
+ *     is (page, copy, rows to copy), -1, -1, 0 for a sequence without one (new_batch triples).  sc_attention_copy makes them, in the cache of each layer.
+ *   - Pages that are taken are the free ones (0 holders when the present batch is given up) of the lowest numbers, in the order of the sequences.
+ *   - With a window, pages that are wholly behind the window of the last kept row, and hold none of the first `sinks`, are let go (entry -1).
+ *   - length_out[i] is wanted[i], -1 for a wrong parent, length or wanted number (outside 0 .. page_count * page_rows), and for a sequence that does not get the pages it
+ *     takes because those before it (such ones among them) and it take more than are free.  Such a sequence holds nothing; its entries are -1, as are all that hold no page.
+ *   - Entries whose number is no page stay out of it: -1 in the next batch as well.
+ * Sequences that are not in the call keep their pages by `holders`.  The results do not depend on the order in which the GPU works.  Four kernels. */
+sc_status sc_attention_fork(const sc_attention *attention, const sc_pages_view *tables, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Pages in use (holders not 0) move to the lowest numbers: with n of them, the k-th one from number n on goes to the k-th free one below n.  moves[3 k ..] (pages / 2 triples) is
+ * (page, where it goes, page_rows), -1, -1, 0 behind the last move; sc_attention_copy makes them.  Entries that lengths reach follow their pages, others stay as they are, and
+ * `page_out` may be `page`.  Tables of sequences that are not in the call have to follow by the moves.  new_batch is 0, and parent, wanted and length_out are NULL.  Four kernels. */
+sc_status sc_attention_compact(const sc_attention *attention, const sc_pages_view *tables, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Copies rows 0 .. moves[3 k + 2] - 1 of the keys and values of page moves[3 k] to page moves[3 k + 1], for `count` triples in device memory; a triple with a number outside 0..pages-1
+ * copies nothing.  A page that is copied to has to be in no other triple (those of fork and compact are not): its contents are not specified otherwise.  One kernel. */
+sc_status sc_attention_copy(const sc_attention *attention, const sc_cache_view *cache, const int32_t *moves, int64_t count, void *hip_stream);
+
 /* Frees the handle; NULL is accepted. */
 sc_status sc_attention_destroy(sc_attention *attention);
 

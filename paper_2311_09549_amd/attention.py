@@ -6,6 +6,18 @@ and strides to the library and queues its kernels.  No arithmetic happens here.
     y = attention.prompt_paged(q, keys, values, pages, lengths, row_start)     # many new rows per sequence
     y = attention.decode(q, keys, values, pages, lengths)                      # one new row per sequence
 
+Drafted tokens, nodes of a tree behind each sequence (`parents`: one number per row, within its sequence, -1 for a node that follows what is before the tree):
+
+    q = attention.append(q, k, v, keys, values, pages, lengths, row_start, parents=parents)      # rotated by their depths
+    y = attention.tree(q, keys, values, pages, lengths, row_start, parents)                      # each sees its ancestors
+    lengths = attention.accept(keys, values, pages, lengths, row_start, parents, last)           # the path to node last[b] becomes the sequence
+
+Sequences that branch, end, shrink and grow share pages (`holders`: how many entries hold each page, 0 for a free one):
+
+    pages, lengths, holders, moves = attention.fork(pages, lengths, holders, parents, wanted)    # sequence i goes on from sequence parents[i]
+    pages, holders, moves = attention.compact(pages, lengths, holders)                           # pages in use to the lowest numbers
+    attention.copy(keys, values, moves)                                                          # in every layer's cache, after either
+
 `q` is (rows, heads, head_dim), `k` and `v` (rows, kv_heads, head_dim), `keys` and `values` (pages, page_rows, kv_heads, head_dim); any strides
 that are multiples of 16 bytes, head_dim contiguous.  `pages` (batch, columns), `lengths` (batch) and `row_start` (batch + 1) are int32.
 A length counts the new rows of its sequence.  The library's header says what the kernels make of wrong lengths and page numbers.
@@ -25,7 +37,7 @@ from . import binding as sc
 _DTYPES = {torch.bfloat16: sc.SC_BF16, torch.float16: sc.SC_F16, torch.float32: sc.SC_F32}
 
 _INT32, _empty_like = torch.int32, torch.empty_like
-_pack_rows, _pack_cache, _pack_sequences = sc.pack_rows, sc.pack_cache, sc.pack_sequences
+_pack_rows, _pack_cache, _pack_sequences, _pack_pages = sc.pack_rows, sc.pack_cache, sc.pack_sequences, sc.pack_pages
 
 # torch's own accessor of a stream's address alone: the stream object around it takes 2 us to make
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -38,9 +50,10 @@ class Attention:
     Tensors are on `device`; calls are made there, whichever is the current one.  Inference only: operands that require a gradient are refused."""
 
     def __init__(self, heads, kv_heads, head_dim, dtype=torch.bfloat16, page_rows=64, *, causal=True, scale=None, rotary_dim=0,
-                 rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0"):
+                 rotary_theta=10000.0, rotary_freq=None, interleaved=False, device="cuda:0", window=None, sinks=0):
         """`scale`: of the scores, 1 / sqrt(head_dim) unless given.  `rotary_freq`: angles per position of the rotated pairs, or
-        `rotary_dim` and `rotary_theta` for theta ** (-2 t / rotary_dim)."""
+        `rotary_dim` and `rotary_theta` for theta ** (-2 t / rotary_dim).  `window`: a row sees the last so many positions, its own
+        included, and the first `sinks`; None for all of them."""
         if dtype not in _DTYPES:
             raise TypeError(f"attention takes {', '.join(str(t) for t in _DTYPES)}, not {dtype}")
         if rotary_freq is None and rotary_dim:
@@ -49,6 +62,10 @@ class Attention:
             rotary_dim = 2 * len(rotary_freq)
         if scale is not None and not scale > 0:
             raise ValueError("the scale of the scores has to be positive")
+        if window is None and sinks:
+            raise ValueError("without a window every row sees the first keys")
+        if window is not None and not causal:
+            raise ValueError("a window is of causal attention")
         if rotary_dim and 2 * len(rotary_freq) != rotary_dim and rotary_dim % 2 == 0:
             raise ValueError("rotary_freq has one angle for each pair of rotary_dim")
         self.device = torch.device(device)
@@ -60,13 +77,16 @@ class Attention:
         self._page = (page_rows, kv_heads, head_dim)
         with torch.cuda.device(self._index) if torch.cuda.is_available() else nullcontext():   # the library asks the current device
             self.handle = sc.attention_create(_DTYPES[dtype], heads, kv_heads, head_dim, page_rows, causal, 0.0 if scale is None else scale,
-                                              rotary_freq, interleaved, rotary_dim)
+                                              rotary_freq, interleaved, rotary_dim, window, sinks)
+        self.window, self.sinks = window, sinks
         self.ws_bytes = sc.attention_workspace_bytes(self.handle)
+        self.tree_ws_bytes = sc.attention_tree_workspace_bytes(self.handle)
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
         self._few_rows = 4 * (32 if head_dim > 128 else 128)   # of a packed prompt: no more than four tiles of keys, which the library never splits
         self._own = {}   # workspaces, made by the first calls that need them
         self._h = self.handle.handle
-        self._append, self._prompt, self._prompt_paged, self._decode = sc.attention_calls()
+        (self._append, self._prompt, self._prompt_paged, self._decode, self._append_tree, self._tree, self._accept, self._fork, self._compact,
+         self._copy) = sc.attention_calls()
 
     def describe(self) -> str:
         return sc.attention_describe(self.handle)
@@ -75,13 +95,14 @@ class Attention:
     # `stream`: the address of a HIP stream, torch's current one unless given.  What is made here, results and workspaces, is memory of that
     # stream; operands are the caller's to order before the call, and to keep until the stream is done with them.  `out` is apart from the other operands,
     # but for append's.
-    def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None):
-        """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None, and then there is no result."""
+    def append(self, q, k, v, keys, values, pages, lengths, row_start=None, out=None, stream=None, parents=None):
+        """Stores k, rotated, and v in the pages of their positions; returns q, rotated (in `out`, which may be q).  q may be None, and then there is no result.
+        `parents`: rows are nodes of trees, stored in their order and rotated by the positions of their depths."""
         if _current_device() != self._index:
-            return self._there(self.append, q, k, v, keys, values, pages, lengths, row_start, out, stream)
+            return self._there(self.append, q, k, v, keys, values, pages, lengths, row_start, out, stream, parents)
         shape = (k.shape[0], self.kv_heads, self.head_dim)
         sequences, cache = self._sequences(shape[0], row_start, lengths, pages), self._cache(keys, values)
-        key, value = self._rows(k, shape), self._rows(v, shape)
+        key, value, key_rows = self._rows(k, shape), self._rows(v, shape), shape[0]
         query = result = None
         if q is not None:
             shape = (shape[0], self.heads, self.head_dim)
@@ -89,9 +110,14 @@ class Attention:
             out, result = self._out(q, out, shape, stream)
         elif out is not None:
             raise ValueError("out is for rotated queries, and there are no queries")
-        status = self._append(self._h, sequences, query, key, value, result, cache, _raw_stream(self._index) if stream is None else stream)
+        if stream is None:
+            stream = _raw_stream(self._index)
+        if parents is None:
+            status = self._append(self._h, sequences, query, key, value, result, cache, stream)
+        else:
+            status = self._append_tree(self._h, sequences, self._numbers("parents", parents, key_rows), query, key, value, result, cache, stream)
         if status:
-            raise sc.ScError(status, "sc_attention_append")
+            raise sc.ScError(status, "sc_attention_append" if parents is None else "sc_attention_append_tree")
         return out
 
     def prompt(self, q, k, v, row_start, out=None, workspace=None, stream=None):
@@ -139,6 +165,85 @@ class Attention:
         if status:
             raise sc.ScError(status, "sc_attention_decode")
         return out
+
+    def tree(self, q, keys, values, pages, lengths, row_start, parents=None, out=None, workspace=None, stream=None):
+        """Attention of the nodes of trees, the last rows of each sequence, over what is before the tree, their ancestors and themselves.  Without
+        `parents` each row follows the one before it.  `workspace`: device bytes of the caller's, `tree_ws_bytes` of them."""
+        if _current_device() != self._index:
+            return self._there(self.tree, q, keys, values, pages, lengths, row_start, parents, out, workspace, stream)
+        shape = (q.shape[0], self.heads, self.head_dim)
+        query = self._rows(q, shape)
+        parent = None if parents is None else self._numbers("parents", parents, shape[0])
+        out, result = self._out(q, out, shape, stream)
+        if stream is None:
+            stream = _raw_stream(self._index)
+        address, size = self._workspace_of(stream, workspace, "tree_ws_bytes")
+        status = self._tree(self._h, self._sequences(shape[0], row_start, lengths, pages), parent, query, self._cache(keys, values), result, address, size, stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_tree")
+        return out
+
+    def accept(self, keys, values, pages, lengths, row_start, parents, last, out=None, stream=None):
+        """Sequence b goes on from node last[b] of its tree (-1: from what is before it): the rows of the path move to the places behind what is before the
+        tree.  Returns the lengths after that (in `out`, apart from the operands), -1 where a length, a path or its end is wrong.  Every layer's
+        cache takes the call, with the lengths of before."""
+        if _current_device() != self._index:
+            return self._there(self.accept, keys, values, pages, lengths, row_start, parents, last, out, stream)
+        rows = parents.shape[0]
+        sequences, cache, parent = self._sequences(rows, row_start, lengths, pages), self._cache(keys, values), self._numbers("parents", parents, rows)
+        batch = lengths.shape[0]
+        end = self._numbers("last", last, batch)
+        if out is None:
+            out, = self._made(stream, (batch,))
+        status = self._accept(self._h, sequences, parent, end, cache, self._numbers("out", out, batch), _raw_stream(self._index) if stream is None else stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_accept")
+        return out
+
+    def fork(self, pages, lengths, holders, parents, wanted=None, out=None, workspace=None, stream=None):
+        """The next batch of sequences: number i has the first rows of sequence parents[i] (-1: none), up to wanted[i] of them (all unless given), and pages for
+        the rest of wanted[i] rows.  Returns its pages and lengths (-1 for a sequence that is wrong or finds no free page), holders, and the copies of pages that
+        `copy` has to make in every layer's cache before anything is written there (rows of `moves`: page, copy, rows).  `out`: those four, apart from the
+        operands, but for holders, which may stay where they are.  `workspace`: device bytes of the caller's (binding.attention_pages_workspace_bytes)."""
+        if _current_device() != self._index:
+            return self._there(self.fork, pages, lengths, holders, parents, wanted, out, workspace, stream)
+        batch, columns, page, page_ld = self._table(pages, lengths)
+        new, count = parents.shape[0], holders.shape[0]
+        shapes = (new, columns), (new,), (count,), (new, 3)
+        if out is None:
+            out = self._made(stream, *shapes)
+        record = (batch, new, count, page, page_ld, columns, self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count),
+                  self._numbers("parents", parents, new), 0 if wanted is None else self._numbers("wanted", wanted, new), *self._results(out, shapes))
+        self._pages_call(self._fork, "sc_attention_fork", record, count, new, workspace, stream)
+        return tuple(out)
+
+    def compact(self, pages, lengths, holders, out=None, workspace=None, stream=None):
+        """Moves the pages in use to the lowest numbers.  Returns pages, holders and the moves that `copy` has to make in every layer's cache before anything
+        is written there (rows: page, where it goes, rows).  `out`: those three; the first two may be the operands themselves."""
+        if _current_device() != self._index:
+            return self._there(self.compact, pages, lengths, holders, out, workspace, stream)
+        batch, columns, page, page_ld = self._table(pages, lengths)
+        count = holders.shape[0]
+        shapes = (batch, columns), (count,), (count // 2, 3)
+        if out is None:
+            out = self._made(stream, *shapes)
+        table, table_ld, after, moves = self._results(out, shapes)
+        record = (batch, 0, count, page, page_ld, columns, self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count), 0, 0,
+                  table, table_ld, 0, after, moves)
+        self._pages_call(self._compact, "sc_attention_compact", record, count, 0, workspace, stream)
+        return tuple(out)
+
+    def copy(self, keys, values, moves, stream=None):
+        """Copies the first rows of pages to other pages, as `fork` and `compact` say."""
+        if _current_device() != self._index:
+            return self._there(self.copy, keys, values, moves, stream)
+        shape = moves.shape
+        if len(shape) != 2:
+            self._refuse_table("moves", "rows of three", moves)
+        count = shape[0]
+        status = self._copy(self._h, self._cache(keys, values), self._numbers("moves", moves, count, 3), count, _raw_stream(self._index) if stream is None else stream)
+        if status:
+            raise sc.ScError(status, "sc_attention_copy")
 
     def _there(self, operator, *args):
         with torch.cuda.device(self._index):
@@ -216,6 +321,55 @@ class Attention:
                 self._refuse_table("pages", f"a row for each of {batch} sequences", pages)
             page, page_ld, columns = pages.data_ptr(), stride[0], shape[1]
         return _pack_sequences(batch, rows, starts, length, page, page_ld, columns)
+
+    def _numbers(self, name, x, *shape):
+        """Address of a contiguous table of that shape."""
+        if x.dtype is not _INT32 or x.get_device() != self._index or x.shape != shape or not x.is_contiguous():
+            self._refuse_table(name, " x ".join(str(n) for n in shape), x)
+        return x.data_ptr()
+
+    def _table(self, pages, lengths):
+        shape, stride = pages.shape, pages.stride()
+        if pages.dtype is not _INT32 or pages.get_device() != self._index or len(shape) != 2 or lengths.shape != shape[:1] or (shape[1] > 1 and stride[1] != 1):
+            self._refuse_table("pages", f"a row for each of {tuple(lengths.shape)} sequences", pages)
+        return shape[0], shape[1], pages.data_ptr(), stride[0]
+
+    def _results(self, out, shapes):
+        """Addresses of the tables that are written, of the first one its row stride too."""
+        if len(out) != len(shapes):
+            raise ValueError(f"out: {len(shapes)} tables, not {len(out)}")
+        first, *rest = out
+        stride = first.stride()
+        if first.dtype is not _INT32 or first.get_device() != self._index or first.shape != shapes[0] or (shapes[0][1] > 1 and stride[1] != 1):
+            self._refuse_table("out", " x ".join(str(n) for n in shapes[0]), first)
+        return (first.data_ptr(), stride[0], *(self._numbers("out", x, *shape) for x, shape in zip(rest, shapes[1:])))
+
+    def _made(self, stream, *shapes):
+        """Tables of the results, memory of the stream of the call."""
+        if stream is not None and stream != _raw_stream(self._index):
+            current = torch.cuda.current_stream(self.device)
+            with self._memory_of(stream):
+                tables = self._made(None, *shapes)
+            for x in tables:
+                x.record_stream(current)
+            return tables
+        return tuple(torch.empty(shape, dtype=_INT32, device=self.device) for shape in shapes)
+
+    def _pages_call(self, call, name, record, count, new, workspace, stream):
+        """The workspace of such a call goes back to its stream with it."""
+        if stream is None:
+            stream = _raw_stream(self._index)
+        if workspace is None:
+            size = sc.attention_pages_workspace_bytes(count, new)
+            if stream == _raw_stream(self._index):
+                workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+            else:
+                with self._memory_of(stream):
+                    workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+        address, size = self._workspace_of(stream, workspace, None)
+        status = call(self._h, _pack_pages(*record), address, size, stream)
+        if status:
+            raise sc.ScError(status, name)
 
     def _refuse_table(self, name, what, x):
         raise ValueError(f"{name}: contiguous int32 on {self.device}, {what}; got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")

@@ -37,6 +37,8 @@ EXPORTS = [
     "sc_tuning_set", "sc_stream_copy", "sc_plan_destroy", "sc_execute_static", "sc_plan_chosen",
     "sc_attention_create", "sc_attention_workspace_bytes", "sc_attention_prompt_workspace_bytes", "sc_attention_describe", "sc_attention_append", "sc_attention_prompt",
     "sc_attention_prompt_paged", "sc_attention_decode", "sc_attention_destroy",
+    "sc_attention_create_window", "sc_attention_append_tree", "sc_attention_tree_workspace_bytes", "sc_attention_tree", "sc_attention_accept",
+    "sc_attention_pages_workspace_bytes", "sc_attention_fork", "sc_attention_compact", "sc_attention_copy",
 ]
 
 _c_i32p = ctypes.POINTER(ctypes.c_int32)
@@ -87,11 +89,19 @@ class SequenceView(ctypes.Structure):
                 ("page", ctypes.c_void_p), ("page_ld", ctypes.c_int64), ("page_count", ctypes.c_int64)]
 
 
+class PagesView(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("new_batch", ctypes.c_int32), ("pages", ctypes.c_int64), ("page", ctypes.c_void_p), ("page_ld", ctypes.c_int64),
+                ("page_count", ctypes.c_int64), ("length", ctypes.c_void_p), ("holders", ctypes.c_void_p), ("parent", ctypes.c_void_p), ("wanted", ctypes.c_void_p),
+                ("page_out", ctypes.c_void_p), ("page_out_ld", ctypes.c_int64), ("length_out", ctypes.c_void_p), ("holders_out", ctypes.c_void_p),
+                ("moves", ctypes.c_void_p)]
+
+
 # Records of attention packed by one call each, like those of an execution: a decoding step of a layer is two calls of a few microseconds.
 pack_rows = struct.Struct("@Pqq").pack
 pack_cache = struct.Struct("@PPqqqq").pack
 pack_sequences = struct.Struct("@iqPPPqq").pack
-for _pack, _n, _record in ((pack_rows, 3, RowsView), (pack_cache, 6, CacheView), (pack_sequences, 7, SequenceView)):
+pack_pages = struct.Struct("@iiqPqqPPPPPqPPP").pack
+for _pack, _n, _record in ((pack_rows, 3, RowsView), (pack_cache, 6, CacheView), (pack_sequences, 7, SequenceView), (pack_pages, 15, PagesView)):
     assert len(_pack(*[0] * _n)) == ctypes.sizeof(_record)
 
 
@@ -138,6 +148,12 @@ def lib():
         for name, records in (("prompt", 6), ("prompt_paged", 5), ("decode", 5)):
             getattr(_lib, "sc_attention_" + name).argtypes = [ptr] * (records + 1) + [ctypes.c_size_t, ptr]
         _lib.sc_attention_destroy.argtypes = [ptr]
+        _lib.sc_attention_append_tree.argtypes = [ptr] * 9
+        _lib.sc_attention_tree.argtypes = [ptr] * 7 + [ctypes.c_size_t, ptr]
+        _lib.sc_attention_accept.argtypes = [ptr] * 7
+        for name in ("fork", "compact"):
+            getattr(_lib, "sc_attention_" + name).argtypes = [ptr, ptr, ptr, ctypes.c_size_t, ptr]
+        _lib.sc_attention_copy.argtypes = [ptr, ptr, ptr, ctypes.c_int64, ptr]
     return _lib
 
 
@@ -443,8 +459,8 @@ class AttentionHandle:
 
 
 def attention_create(dtype: int, heads: int, kv_heads: int, head_dim: int, page_rows: int, causal=True, scale=0.0, rotary_freq=None,
-                     interleaved=False, rotary_dim=None) -> AttentionHandle:
-    """`rotary_freq`: angles per position of the rotated pairs; `rotary_dim`: 2 len(rotary_freq) unless given."""
+                     interleaved=False, rotary_dim=None, window=None, sinks=0) -> AttentionHandle:
+    """`rotary_freq`: angles per position of the rotated pairs; `rotary_dim`: 2 len(rotary_freq) unless given; `window`: None for every key."""
     d = AttentionDesc(int(dtype), int(heads), int(kv_heads), int(head_dim), int(page_rows), int(causal), float(scale))
     if scale and not d.scale:
         raise ValueError(f"the scale of the scores is of 32 bits, which {scale} is too small for")   # 0 would stand for the usual one
@@ -456,7 +472,12 @@ def attention_create(dtype: int, heads: int, kv_heads: int, head_dim: int, page_
     if freq.size:
         d.rotary_freq = freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
     h = ctypes.c_void_p()
-    _check(lib().sc_attention_create(ctypes.byref(h), ctypes.byref(d)), "sc_attention_create")
+    if window is None:
+        _check(lib().sc_attention_create(ctypes.byref(h), ctypes.byref(d)), "sc_attention_create")
+    else:
+        if not (-2 ** 31 <= window < 2 ** 31 and -2 ** 31 <= sinks < 2 ** 31):
+            raise ValueError(f"a window of {window} and {sinks} first keys: more than 32 bits")
+        _check(lib().sc_attention_create_window(ctypes.byref(h), ctypes.byref(d), ctypes.c_int32(window), ctypes.c_int32(sinks)), "sc_attention_create_window")
     return AttentionHandle(h)
 
 
@@ -469,6 +490,18 @@ def attention_workspace_bytes(attention: AttentionHandle) -> int:
 def attention_prompt_workspace_bytes(attention: AttentionHandle) -> int:
     n = ctypes.c_size_t()
     _check(lib().sc_attention_prompt_workspace_bytes(attention.handle, ctypes.byref(n)), "sc_attention_prompt_workspace_bytes")
+    return int(n.value)
+
+
+def attention_tree_workspace_bytes(attention: AttentionHandle) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().sc_attention_tree_workspace_bytes(attention.handle, ctypes.byref(n)), "sc_attention_tree_workspace_bytes")
+    return int(n.value)
+
+
+def attention_pages_workspace_bytes(pages: int, new_batch: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().sc_attention_pages_workspace_bytes(ctypes.c_int64(pages), ctypes.c_int32(new_batch), ctypes.byref(n)), "sc_attention_pages_workspace_bytes")
     return int(n.value)
 
 
@@ -495,9 +528,34 @@ def attention_decode(attention: AttentionHandle, sequences, q, cache, out, works
     _check(lib().sc_attention_decode(attention.handle, sequences, q, cache, out, workspace, workspace_bytes, stream), "sc_attention_decode")
 
 
+def attention_append_tree(attention: AttentionHandle, sequences, parent, q, k, v, q_out, cache, stream=0):
+    _check(lib().sc_attention_append_tree(attention.handle, sequences, parent, q, k, v, q_out, cache, stream), "sc_attention_append_tree")
+
+
+def attention_tree(attention: AttentionHandle, sequences, parent, q, cache, out, workspace, workspace_bytes, stream=0):
+    _check(lib().sc_attention_tree(attention.handle, sequences, parent, q, cache, out, workspace, workspace_bytes, stream), "sc_attention_tree")
+
+
+def attention_accept(attention: AttentionHandle, sequences, parent, last, cache, length_out, stream=0):
+    _check(lib().sc_attention_accept(attention.handle, sequences, parent, last, cache, length_out, stream), "sc_attention_accept")
+
+
+def attention_fork(attention: AttentionHandle, tables, workspace, workspace_bytes, stream=0):
+    """`tables`: bytes of pack_pages."""
+    _check(lib().sc_attention_fork(attention.handle, tables, workspace, workspace_bytes, stream), "sc_attention_fork")
+
+
+def attention_compact(attention: AttentionHandle, tables, workspace, workspace_bytes, stream=0):
+    _check(lib().sc_attention_compact(attention.handle, tables, workspace, workspace_bytes, stream), "sc_attention_compact")
+
+
+def attention_copy(attention: AttentionHandle, cache, moves, count, stream=0):
+    _check(lib().sc_attention_copy(attention.handle, cache, moves, count, stream), "sc_attention_copy")
+
+
 def attention_calls():
-    """The four operators above as functions of the same arguments (a handle's address first) that return the status: two calls
+    """The operators above as functions of the same arguments (a handle's address first) that return the status: two calls
     less on the way of a step that is made for every layer and token."""
     def of(name):
         return ctypes.CFUNCTYPE(ctypes.c_int, *getattr(lib(), name).argtypes)((name, _lib))
-    return tuple(of("sc_attention_" + name) for name in ("append", "prompt", "prompt_paged", "decode"))
+    return tuple(of("sc_attention_" + name) for name in ("append", "prompt", "prompt_paged", "decode", "append_tree", "tree", "accept", "fork", "compact", "copy"))

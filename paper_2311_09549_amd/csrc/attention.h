@@ -21,6 +21,7 @@ constexpr int64_t kMaxUnits = (int64_t)1 << 52;   // of decode: 2^10 times as ma
 constexpr int32_t kMaxKeys = 1 << 30;   // of a sequence: a tile beyond the last one fits 32 bits
 constexpr int32_t kMaxBatch = (1 << 20) - 1;
 constexpr int kSplitBlocks = 1024;   // of rows of a prompt whose keys are split
+constexpr int32_t kMaxNodes = 1024;  // of a tree of drafted rows
 constexpr int32_t kMaxGroupsLog2 = 10;   // 2^n workgroups of decode at most
 
 // ------------------------------------------------------------------------------------------
@@ -130,6 +131,52 @@ ATTN_HD RowBlock row_block(const Sequences &s, int32_t number)
 }
 
 // ------------------------------------------------------------------------------------------
+// a window: a row at position p sees keys p - window + 1 .. p, and those of the first `sinks` that are before it
+// ------------------------------------------------------------------------------------------
+
+// The first key that a row at position p sees through its window.
+ATTN_HD int32_t window_low(int32_t window, int32_t p) { return window > 0 && p >= window ? p - window + 1 : 0; }
+
+// What rows from position p on see of a sequence of `length` keys, as one line: the first keys, up to `first` (whole sixteens, 0 if the line has no gap), then those from
+// first + skip on.  Nobody sees the `skip` keys between (whole sixteens too).
+struct Span {
+    int32_t first, skip, length;   // length: of the line
+};
+
+ATTN_HD Span span_of(int32_t length, int32_t window, int32_t sinks, int32_t p)
+{
+    const int32_t low = window_low(window, p) & ~15;
+    if (low > 0 && sinks < low && (sinks + 15 & ~15) < low) {
+        const int32_t first = sinks + 15 & ~15;
+        return {first, low - first, length - (low - first)};
+    }
+    return {0, 0, length};
+}
+
+// The key at place v of the line.
+ATTN_HD int32_t key_at(const Span &s, int32_t v) { return v < s.first ? v : v + s.skip; }
+
+// ------------------------------------------------------------------------------------------
+// trees of drafted rows: parent[r] is the row that row r follows, counted from the first row of its sequence, -1 for one that follows what is before the tree
+// ------------------------------------------------------------------------------------------
+
+// Whether node i may follow node p.  A number that is neither -1 nor of an earlier row is wrong.
+ATTN_HD bool parent_ok(int32_t i, int32_t p) { return p >= -1 && p < i; }
+
+// Depth of node i, or -1 if its chain has a wrong number.  Every step goes to an earlier row.
+ATTN_HD int32_t depth_of(const int32_t *parent, int32_t i)
+{
+    int32_t depth = 0;
+    while (true) {
+        const int32_t p = parent[i];
+        if (!parent_ok(i, p)) return -1;
+        if (p < 0) return depth;
+        i = p;
+        ++depth;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
 // split of decode: the units of all segments (a segment is a sequence and a tile of the heads of one key head) in one
 // line, a workgroup takes an equal share of it
 // ------------------------------------------------------------------------------------------
@@ -173,6 +220,7 @@ struct AppendArgs {
     Rows q, k, v, q_out;
     Cache cache;
     int32_t heads, kv_heads, head_dim, pairs, interleaved;
+    const int32_t *parent;      // null: rows are in order
     double turns[kMaxPairs];    // turns per position of each pair
 };
 
@@ -188,6 +236,56 @@ struct AttendArgs {
     int32_t *cut;               // prompt: blocks that each share has pieces of
     int32_t blocks;             // prompt: numbers of blocks of rows
     int32_t n_cu;
+    int32_t window, sinks;      // window 0: every key before a row
+    const int32_t *parent;      // trees: null, rows are in order
+    int32_t tree;               // rows of trees: no more of them than keys, and no more than kMaxNodes where they have parents
+    struct TreeCut *tree_cut;   // trees: the segment that each workgroup leaves to others
+};
+
+// The segment that a workgroup began and left to others, for the kernel that joins its pieces: its place in the line and units, and those of the whole line.  No units: none.
+struct TreeCut {
+    int64_t first, all;
+    int32_t units, b, kv, tile;
+};
+
+// The accepted rows of trees.
+struct AcceptArgs {
+    Sequences s;
+    Cache cache;
+    int32_t kv_heads, head_dim;
+    const int32_t *parent, *last;
+    int32_t *length_out;        // null: not wanted
+};
+
+// Pages of the sequences that come after (new_batch of them) from those that are.
+struct ForkArgs {
+    int32_t batch, new_batch, columns, pages, page_shift, window, sinks;
+    const int32_t *page, *length, *holders;
+    int64_t page_ld;
+    const int32_t *parent, *wanted;   // wanted null: as many rows as the parent has
+    int32_t *page_out, *length_out, *holders_out, *moves;
+    int64_t page_out_ld;
+    // workspace
+    int32_t *keeper;        // per page: the first sequence that keeps it in part
+    uint64_t *free_bits;    // per page
+    int32_t *free_before;   // per block of pages: how many are free
+    int64_t *needed;        // per sequence: pages that those before it take
+};
+
+struct CompactArgs {
+    int32_t batch, columns, pages, page_shift;
+    const int32_t *page, *length, *holders;
+    int64_t page_ld;
+    int32_t *page_out, *holders_out, *moves;
+    int64_t page_out_ld;
+    int32_t *to, *used_before;   // workspace: per page where it goes, per block of pages how many are in use
+};
+
+struct CopyArgs {
+    Cache cache;
+    int32_t kv_heads, head_dim, page_shift, pages;
+    const int32_t *moves;
+    int64_t count;
 };
 
 // Padded head_dim of the kernels.
@@ -198,9 +296,25 @@ ATTN_HD int piece_floats(int padded) { return kHeadTile * (padded + 2); }
 int prompt_shares(int n_cu);
 size_t prompt_workspace(sc_dtype dtype, int head_dim, int n_cu);
 
+// The same for trees, and for single rows through a window.  The table of cut segments is behind the pieces.
+size_t tree_pieces(int head_dim, int groups_log2);
+size_t row_pieces(int head_dim, int groups_log2);
+inline size_t cut_bytes(int groups_log2) { return sizeof(TreeCut) << groups_log2; }
+
+// Pages that a workgroup of fork and compact counts.
+constexpr int32_t kPagesPerBlock = 4096;
+constexpr int32_t kMaxPages = 1 << 30;
+inline int32_t blocks_of_pages(int32_t pages) { return (pages + kPagesPerBlock - 1) / kPagesPerBlock; }
+
 hipError_t launch_append(const AppendArgs &a, sc_dtype dtype, hipStream_t stream);
 hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream);
+hipError_t launch_prompt_window(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream);
 hipError_t launch_decode(const AttendArgs &a, sc_dtype dtype, hipStream_t stream);
+hipError_t launch_tree(const AttendArgs &a, sc_dtype dtype, hipStream_t stream);
+hipError_t launch_accept(const AcceptArgs &a, sc_dtype dtype, hipStream_t stream);
+hipError_t launch_fork(const ForkArgs &a, hipStream_t stream);
+hipError_t launch_compact(const CompactArgs &a, hipStream_t stream);
+hipError_t launch_copy(const CopyArgs &a, sc_dtype dtype, hipStream_t stream);
 
 }  // namespace sck
 
@@ -213,5 +327,6 @@ struct sc_attention {
     bool has_device;
     int32_t n_cu;
     int32_t groups_log2;
-    size_t ws_bytes, prompt_ws_bytes;
+    size_t ws_bytes, prompt_ws_bytes, tree_ws_bytes;
+    int32_t window, sinks;
 };

@@ -97,6 +97,9 @@ __device__ __forceinline__ float over_groups_sum(float x)
 // A maximum of -infinity (no key yet, or scores of -infinity alone) is taken as 0 in differences: weights 0 instead of NaN.
 __device__ __forceinline__ float finite_max(float m) { return m == kMinusInf ? 0.0f : m; }
 
+// Of 16 bits those below x.
+__device__ __forceinline__ uint32_t below(int32_t x) { return x <= 0 ? 0u : x >= 16 ? 0xffffu : (1u << x) - 1; }
+
 // Where 16 keys lie (wave-uniform): first rows of keys and values for the lane's head, and the last key of the tile that may be read (0..15).
 struct KeyTile {
     const char *k, *v;
@@ -231,16 +234,21 @@ struct Wave {
         }
     }
 
-    // Infinities and NaN among values that some query of the step does not see: the product would spread them to it (0 times infinity).
-    // They are taken out of x; queries that see one get it from a product of indicators, one for each of +infinity, -infinity, NaN.
-    __device__ __forceinline__ void part_infinities(Values &x, int visible)
+    static __device__ __forceinline__ bool any_special(const Values &x)
     {
         uint32_t any = 0;
 #pragma unroll
         for (int j = 0; j < TILES * 4; ++j)
 #pragma unroll
             for (int w = 0; w < VW; ++w) any |= Special<TR>::infinite_or_nan(x.v[j][w]);
-        if (!__any(any != 0)) return;
+        return __any(any != 0);
+    }
+
+    // Infinities and NaN among values that some query of the step does not see: the product would spread them to it (0 times infinity).
+    // They are taken out of x; queries that see one get it from a product of indicators, one for each of +infinity, -infinity, NaN.
+    __device__ __forceinline__ void part_infinities(Values &x, int visible)
+    {
+        if (!any_special(x)) return;
         const f32x4 none = {0, 0, 0, 0};
         uint32_t one[TILES * 4];
 #pragma unroll
@@ -274,6 +282,10 @@ struct Wave {
             __builtin_amdgcn_sched_barrier(0);   // one at a time: side by side they would take the registers of the main loop
         }
         fresh(x);
+        without_infinities(x);
+    }
+    static __device__ __forceinline__ void without_infinities(Values &x)
+    {
 #pragma unroll
         for (int j = 0; j < TILES * 4; ++j)
 #pragma unroll
@@ -344,6 +356,54 @@ struct Wave {
         for (int u = 0; u < EPL; ++u) o[u] *= shrink;
         if (MASK && ALIKE) hide(v, visible);
         else if (MASK) part_infinities(v, visible);
+        add_values(v, p);
+    }
+
+    // Adds the infinities and NaN of a row of values that the lane's query sees.
+    __device__ __forceinline__ void add_special(const char *row)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int u = 0; u < EPL; ++u) {
+                const int e = (4 * g + i) * EPL + u;
+                if (!EXACT && e >= head_dim) continue;
+                const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(row)[e];
+                if (!(__builtin_fabsf((float)x) < -kMinusInf)) o[u][i] += (float)x;
+            }
+    }
+
+    // Bit of the lane's j-th key among bits of the step's keys, shifted by 4 g.
+    static constexpr int seen_bit(int j) { return j / 4 * 16 + j % 4; }
+
+    // Scores of keys whose bits are not set become -infinity.
+    static __device__ __forceinline__ void mask(Scores &x, uint32_t seen)
+    {
+#pragma unroll
+        for (int j = 0; j < TILES * 4; ++j) x.s[j / 4][j % 4] = seen >> seen_bit(j) & 1 ? x.s[j / 4][j % 4] : kMinusInf;
+    }
+
+    // The rest of a step for scores that have been masked, if they had to be, and values of which those that a query does not see are finite.
+    __device__ __forceinline__ void add_seen(const Scores &x, const Values &v, float scale_log2)
+    {
+        float p[TILES * 4], top = kMinusInf;
+#pragma unroll
+        for (int j = 0; j < TILES * 4; ++j) {
+            p[j] = x.s[j / 4][j % 4];
+            top = fmaxf(top, p[j]);
+        }
+        const float next = fmaxf(m, over_groups_max(top));
+        const float from = finite_max(next), shrink = __builtin_amdgcn_exp2f((m - from) * scale_log2);
+        m = next;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < TILES * 4; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[j] - from, scale_log2, TR::kLift));
+            sum += p[j];
+        }
+        l = l * shrink + sum;
+#pragma unroll
+        for (int u = 0; u < EPL; ++u) o[u] *= shrink;
         add_values(v, p);
     }
 

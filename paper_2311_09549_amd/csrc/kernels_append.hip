@@ -107,10 +107,17 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a)
     const int32_t b = sequence_of(a.s, row);
     if (b < 0) return;
     const int32_t begin = row_begin(a.s, b), count = row_begin(a.s, b + 1) - begin;
-    const int64_t position = (int64_t)a.s.length[b] - count + (row - begin);
+    const int64_t place = (int64_t)a.s.length[b] - count + (row - begin);
     // row of the cache, or none
     int32_t page = -1;
-    if (position >= 0 && position < table_room(a.s)) page = page_of(a.s, b, (int32_t)position);
+    if (place >= 0 && place < table_room(a.s)) page = page_of(a.s, b, (int32_t)place);
+    // a node of a tree is at the position of its depth, wherever it is stored
+    int64_t position = place;
+    if (a.parent) {
+        const int32_t depth = depth_of(a.parent + begin, row - begin);
+        position = (int64_t)a.s.length[b] - count + (depth < 0 ? row - begin : depth);
+        if (depth < 0 || a.s.length[b] < count) page = -1;
+    }
     for (int t = threadIdx.x; t < a.pairs; t += kAppendThreads) {
         const double x = (double)position * a.turns[t];
         float c, s;
@@ -118,7 +125,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a)
         cos_s[t] = c;
         sin_s[t] = s;
     }
-    const int64_t at = page < 0 ? -1 : page * a.cache.page + ((int32_t)position & ((1 << a.s.page_shift) - 1)) * a.cache.row;
+    const int64_t at = page < 0 ? -1 : page * a.cache.page + ((int32_t)place & ((1 << a.s.page_shift) - 1)) * a.cache.row;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)

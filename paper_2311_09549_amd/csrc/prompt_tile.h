@@ -67,11 +67,31 @@ __device__ __forceinline__ int32_t keys_seen(const AttendArgs &a, const RowBlock
     return n < 0 ? 0 : n;
 }
 
+// The tiles of keys that a block of rows sees, as one line: those of the first keys, up to key `first`, then those from first + skip on (whole tiles both).  `length`: keys that
+// its last row sees, without the skipped ones.  `low` and `last_low`: the first key that its first and its last row see through the window.
+struct BlockKeys {
+    int32_t first, skip, length, low, last_low;
+};
+
+template <bool WINDOW>
+__device__ __forceinline__ BlockKeys block_keys(const AttendArgs &a, const RowBlock &blk, int32_t length, int32_t tile)
+{
+    const int32_t n = keys_seen(a, blk, length, blk.end - 1);
+    BlockKeys k = {0, 0, n, 0, 0};
+    if (!WINDOW) return k;
+    k.low = window_low(a.window, keys_seen(a, blk, length, blk.first) - 1);
+    k.last_low = window_low(a.window, n - 1);
+    const int32_t from = k.low / tile * tile, first = a.sinks < from ? (a.sinks + tile - 1) / tile * tile : from;
+    if (first < from) k = {first, from - first, n - (from - first), k.low, k.last_low};
+    return k;
+}
+
+// WINDOW: rows see the keys of a window alone, and the first ones (attention.h).
 // SPLIT: as in decode, the tiles of keys of all blocks are put in one line, block after block, one group of heads after the other, and every workgroup takes an
 // equal share of it; blocks that shares cut leave pieces, which prompt_join_kernel joins.  Without it a workgroup has one block, and a call takes as long as
 // the longest of them, or as the compute unit that was given most.  Chunks of four prompts behind up to 8,191 keys, 32 heads of 128: 262 to 274 us with, 320
 // without; L2 misses are six times as many, since workgroups begin at different keys, and the join is 18 us.
-template <typename TR, int DP, bool PAGED, bool SPLIT, int NW, int KT>
+template <typename TR, int DP, bool PAGED, bool SPLIT, bool WINDOW, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
 {
     using P = PromptTile<TR, DP, NW, KT>;
@@ -96,10 +116,14 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         }
 
         const auto sees = [&](int32_t r) { return keys_seen(a, blk, length, r); };
-        int32_t block_most = sees(blk.end - 1);
+        const BlockKeys line = block_keys<WINDOW>(a, blk, length, KT);
+        int32_t block_most = line.length;
         if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
+        const auto key_of = [&](int32_t place) { return WINDOW && place >= line.first ? place + line.skip : place; };
         const int32_t visible = mine ? sees(row) : 0;
         const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
+        // the first key that the lane's row, and any row of the wavefront, sees through the window
+        const int32_t low = WINDOW ? window_low(a.window, visible - 1) : 0, least = WINDOW && first < blk.end ? window_low(a.window, sees(first) - 1) : 0;
 
         u32x4 qf[DP / 16];
 #pragma unroll
@@ -136,7 +160,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 int64_t k_at = key * k_row, v_at = key * v_row;
                 if (PAGED) {
                     int32_t page = page_of(a.s, blk.sequence, key);
-                    bad |= page < 0;
+                    bad |= page < 0 && (!WINDOW || key >= line.low || key < a.sinks);   // pages behind every row's window may be gone
                     if (page < 0) page = 0;
                     k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
                 }
@@ -182,7 +206,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-                        if (key >= visible || e >= a.head_dim) continue;
+                        if (key >= visible || e >= a.head_dim || (WINDOW && key < low && key >= a.sinks)) continue;
                         const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(p)[e];
                         if ((__builtin_bit_cast(uint16_t, x) & TR::kExponent) == TR::kExponent) o[d][r] += (float)x;
                     }
@@ -217,7 +241,9 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    if (MASK) s[t][r] = 32 * t + 8 * (r / 4) + 4 * half + r % 4 < visible - base ? s[t][r] : kMinusInf;
+                    const int n = 32 * t + 8 * (r / 4) + 4 * half + r % 4;   // number of the key in the tile
+                    if (MASK && !WINDOW) s[t][r] = n < visible - base ? s[t][r] : kMinusInf;
+                    if (MASK && WINDOW) s[t][r] = n < visible - base && (n >= low - base || n < a.sinks - base) ? s[t][r] : kMinusInf;
                     top = fmaxf(top, s[t][r]);
                 }
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -275,15 +301,18 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 
         if (block_most > 0) {
             const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
-            int32_t base = SPLIT ? first_tile * KT : 0;
-            fetch(base);
-            bool special = __syncthreads_or(put(tile_s, base + KT > block_all));
+            // whether every row of the block sees the whole tile of keys from `key` on
+            const auto whole = [&](int32_t key) { return key + KT <= block_all && (!WINDOW || key >= line.last_low || key + KT <= a.sinks); };
+            int32_t place = SPLIT ? first_tile * KT : 0;
+            fetch(key_of(place));
+            bool special = __syncthreads_or(put(tile_s, !whole(key_of(place))));
             int buffer = 0;
             const auto pass = [&](auto masked) {
                 constexpr bool MASK = decltype(masked)::value;
-                const bool more = base + KT < block_most, part = MASK || base + 2 * KT > block_all;
-                if (more) fetch(base + KT);
-                if (!MASK || base < most) {
+                const int32_t base = key_of(place);
+                const bool more = place + KT < block_most, part = (MASK && !WINDOW) || !whole(key_of(place + KT));
+                if (more) fetch(key_of(place + KT));
+                if (!MASK || (base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
                     tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked);
                     if (MASK && special) add_special(base);
                 }
@@ -292,11 +321,19 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
                 if (part) special = __syncthreads_or(any);
                 else __syncthreads();
-                base += KT;
+                place += KT;
             };
-            // tiles that every row of the block sees whole, then the others
-            while (base + KT <= block_all && (!SPLIT || base < block_most)) pass(std::false_type());
-            while (base < block_most) pass(std::true_type());
+            if constexpr (WINDOW) {
+                // edges of the window and of the first keys, and what every row of the block sees whole, in turn
+                while (place < block_most) {
+                    while (place < block_most && !whole(key_of(place))) pass(std::true_type());
+                    while (place < block_most && whole(key_of(place))) pass(std::false_type());
+                }
+            } else {
+                // tiles that every row of the block sees whole, then the others
+                while (place + KT <= block_all && (!SPLIT || place < block_most)) pass(std::false_type());
+                while (place < block_most) pass(std::true_type());
+            }
         }
         if (PAGED) bad = __syncthreads_or(bad);
         l += __shfl_xor(l, 32);
@@ -333,7 +370,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         // tiles of a block of rows; one that sees nothing has one too, since its rows are written
         const auto tiles_of = [&](const RowBlock &blk) {
             if (blk.sequence < 0) return 0;
-            const int32_t n = keys_seen(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, blk.end - 1);
+            const int32_t n = block_keys<WINDOW>(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, KT).length;
             return n <= KT ? 1 : (n - 1) / KT + 1;
         };
         // In the line a block's tiles lie behind kBegin places that stand for its start and end, which cost about as much as they.
