@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libsparsecontract.so")
 SOURCES = ["host.cpp", "kernels.hip", "kernels_linear.hip", "kernels_order2.hip", "kernels_order4.hip", "kernels_traverse.hip", "kernels_ttmc3.hip", "kernels_slice.hip", "kernels_chain4.hip", "kernels_mttkrp.hip", "kernels_ttmc4.hip", "kernels_ttmc_all.hip", "kernels_gemm.hip", "static_scratch.hip",
-           "attention.cpp", "kernels_append.hip", "kernels_prompt.hip", "kernels_prompt_window.hip", "kernels_decode.hip", "kernels_tree.hip", "kernels_pages.hip"]
+           "attention.cpp", "kernels_append.hip", "kernels_prompt.hip", "kernels_prompt_window.hip", "kernels_prompt_tree.hip", "kernels_decode.hip", "kernels_tree.hip", "kernels_pages.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

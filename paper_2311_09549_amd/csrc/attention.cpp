@@ -218,7 +218,7 @@ sc_status create(sc_attention **out, const sc_attention_desc *d, int32_t window,
     while (at->groups_log2 < kMaxGroupsLog2 && (1 << at->groups_log2) < 2 * at->n_cu) ++at->groups_log2;
     at->ws_bytes = row_pieces(at->head_dim, at->groups_log2) + (window ? cut_bytes(at->groups_log2) : 0);
     at->prompt_ws_bytes = prompt_workspace(at->dtype, at->head_dim, at->n_cu);
-    at->tree_ws_bytes = tree_pieces(at->head_dim, at->groups_log2) + cut_bytes(at->groups_log2);
+    at->tree_ws_bytes = std::max(tree_pieces(at->head_dim, at->groups_log2), up_to(at->prompt_ws_bytes, 256)) + cut_bytes(at->groups_log2);
     *out = at;
     return SC_OK;
 }
@@ -405,10 +405,13 @@ extern "C" sc_status sc_attention_tree(const sc_attention *at, const sc_sequence
     if ((uintptr_t)workspace % 256) return SC_ERR_SHAPE_MISMATCH;
     a.tree = 1;
     a.parent = parent;
+    a.causal = 1;
+    a.n_cu = at->n_cu;
     if (!tree_line_ok(a)) return SC_ERR_BAD_DIMS;
     if (!at->has_device) return SC_ERR_DEVICE;
     a.pieces = static_cast<float *>(workspace);
     a.tree_cut = reinterpret_cast<TreeCut *>(static_cast<char *>(workspace) + at->tree_ws_bytes - cut_bytes(at->groups_log2));
+    a.cut = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + at->prompt_ws_bytes - 2 * prompt_shares(at->n_cu) * sizeof(int32_t));   // of the other kernels
     return launched(launch_tree(a, at->dtype, (hipStream_t)hip_stream));
 }
 
@@ -463,7 +466,7 @@ extern "C" sc_status sc_attention_compact(const sc_attention *at, const sc_pages
     if (!at->has_device) return SC_ERR_DEVICE;
     char *w = static_cast<char *>(workspace);
     const CompactArgs a = {v->batch, (int32_t)v->page_count, (int32_t)v->pages, at->page_shift, v->page, v->length, v->holders, v->page_ld, v->page_out, v->holders_out, v->moves,
-                           v->page_out_ld, reinterpret_cast<int32_t *>(w), reinterpret_cast<int32_t *>(w + space.before)};
+                           v->page_out_ld, reinterpret_cast<int32_t *>(w), reinterpret_cast<uint64_t *>(w + space.bits), reinterpret_cast<int32_t *>(w + space.before)};
     return launched(launch_compact(a, (hipStream_t)hip_stream));
 }
 

@@ -278,7 +278,10 @@ struct CompactArgs {
     int64_t page_ld;
     int32_t *page_out, *holders_out, *moves;
     int64_t page_out_ld;
-    int32_t *to, *used_before;   // workspace: per page where it goes, per block of pages how many are in use
+    // workspace
+    int32_t *to;            // per page: where it goes
+    uint64_t *used_bits;    // per page
+    int32_t *used_before;   // per block of pages: how many are in use
 };
 
 struct CopyArgs {
@@ -309,6 +312,7 @@ inline int32_t blocks_of_pages(int32_t pages) { return (pages + kPagesPerBlock -
 hipError_t launch_append(const AppendArgs &a, sc_dtype dtype, hipStream_t stream);
 hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream);
 hipError_t launch_prompt_window(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream);
+hipError_t launch_prompt_tree(const AttendArgs &a, sc_dtype dtype, hipStream_t stream);   // 16-bit types
 hipError_t launch_decode(const AttendArgs &a, sc_dtype dtype, hipStream_t stream);
 hipError_t launch_tree(const AttendArgs &a, sc_dtype dtype, hipStream_t stream);
 hipError_t launch_accept(const AcceptArgs &a, sc_dtype dtype, hipStream_t stream);

@@ -84,6 +84,99 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(CopyArgs a, int32_t elem
 }
 
 // -- the next batch --------------------------------------------------------------------------------------------------------------
+// Fork and compact are a few steps over tables, each of which needs the one before it whole.  Small tables: one workgroup takes all steps; others: a kernel for each.
+constexpr int kWide = 1024;   // threads of a workgroup of theirs
+
+// What another workgroup, or an atomic operation of this one, has written.
+__device__ __forceinline__ int32_t fresh(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Sum over the threads of a workgroup, and of those before each.
+template <typename T>
+__device__ __forceinline__ T sum_before(T x, T &all)
+{
+    __shared__ T wave_s[kWide / 64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    T upto = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const T y = __shfl_up(upto, d);
+        upto += lane >= d ? y : 0;
+    }
+    __syncthreads();
+    if (lane == 63) wave_s[wave] = upto;
+    __syncthreads();
+    T before = 0;
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < kWide / 64; ++k) {
+        before += k < wave ? wave_s[k] : 0;
+        all += wave_s[k];
+    }
+    return before + upto - x;
+}
+
+// A bit for each of the kPagesPerBlock pages of a block, and how many are set.
+template <typename IS>
+__device__ __forceinline__ void count_block(int32_t block, int32_t pages, uint64_t *bits, int32_t *count, const IS &is)
+{
+    __shared__ int32_t wave_s[kWide / 64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    int32_t n = 0;
+#pragma unroll
+    for (int k = 0; k < kPagesPerBlock; k += kWide) {
+        const int64_t p = (int64_t)block * kPagesPerBlock + k + threadIdx.x;
+        const uint64_t word = __ballot(p < pages && is((int32_t)p));
+        if (lane == 0) bits[p / 64] = word;
+        n += __popcll(word);
+    }
+    __syncthreads();
+    if (lane == 0) wave_s[wave] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        n = 0;
+        for (int k = 0; k < kWide / 64; ++k) n += wave_s[k];
+        count[block] = n;
+    }
+}
+
+// Of the counts of all blocks: the sum of those before one, and of all.
+__device__ __forceinline__ void sum_counts(const int32_t *count, int32_t blocks, int32_t block, int32_t &before, int32_t &all)
+{
+    before = all = 0;
+    for (int32_t k0 = 0; k0 < blocks; k0 += kWide) {
+        const int32_t k = k0 + (int32_t)threadIdx.x, n = k < blocks ? fresh(count + k) : 0;
+        int32_t sum;
+        sum_before(k < block ? n : 0, sum);
+        before += sum;
+        sum_before(n, sum);
+        all += sum;
+    }
+}
+
+// Calls f(page, whether its bit is set, set bits before it) for the pages of a block, of which each wavefront looks at the words by itself.
+template <typename F>
+__device__ __forceinline__ void each_page(int32_t block, int32_t pages, const uint64_t *bits, int32_t before, const F &f)
+{
+    static_assert(kPagesPerBlock == 64 * 64, "a word for each lane");
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint64_t word = __hip_atomic_load(bits + (int64_t)block * 64 + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int32_t upto = __popcll(word);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t y = __shfl_up(upto, d);
+        upto += lane >= d ? y : 0;
+    }
+    upto -= __popcll(word);
+#pragma unroll
+    for (int k = 0; k < kPagesPerBlock / kWide; ++k) {
+        const int at = k * (kWide / 64) + wave;
+        const uint64_t w = __shfl(word, at);
+        const int64_t p = (int64_t)block * kPagesPerBlock + 64 * at + lane;
+        const int32_t rank = before + __shfl(upto, at) + __popcll(w & (((uint64_t)1 << lane) - 1));
+        if (p < pages) f((int32_t)p, (bool)(w >> lane & 1), rank);
+    }
+}
+
 // What sequence i of the next batch has of the present one.
 struct Branch {
     int32_t parent;         // -1: nothing
@@ -131,30 +224,26 @@ __device__ __forceinline__ int32_t page_in_part(const ForkArgs &a, const Branch 
     return entry_of(a, r.parent, r.kept >> a.page_shift);
 }
 
-// Whether it is left with that page: the first of those that keep it in part, if none holds it whole.  `holders`: of whole pages.
-__device__ __forceinline__ bool keeps_part(const ForkArgs &a, int32_t i, int32_t page) { return a.keeper[page] == i && a.holders_out[page] == 0; }
-
-__global__ void __launch_bounds__(kThreads) fork_begin_kernel(ForkArgs a)
+// First step, page by page.
+__device__ __forceinline__ void fork_begin(const ForkArgs &a, int64_t p)
 {
-    const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (p >= a.pages) return;
     a.holders_out[p] = a.holders[p];
     a.keeper[p] = kNone;
 }
 
-// Entries of the present batch hold their pages no more, whole ones of the next do.  Sums of whole numbers: their order does not matter.
-__global__ void __launch_bounds__(kThreads) fork_hold_kernel(ForkArgs a)
+// Second step, entry by entry: those of the present batch (rows 0 .. batch - 1) hold their pages no more, whole ones of the next do.  Sums and minima of whole numbers: their
+// order does not matter.
+__device__ __forceinline__ void fork_hold(const ForkArgs &a, int32_t row, int32_t c0, int32_t step)
 {
-    const int32_t b = blockIdx.x, c0 = blockIdx.y * kThreads + threadIdx.x, step = gridDim.y * kThreads;
-    if (b < a.batch) {
-        const int32_t columns = columns_of(fork_length(a, b), a.page_shift);
+    if (row < a.batch) {
+        const int32_t columns = columns_of(fork_length(a, row), a.page_shift);
         for (int32_t c = c0; c < columns; c += step) {
-            const int32_t p = entry_of(a, b, c);
+            const int32_t p = entry_of(a, row, c);
             if (p >= 0) atomicAdd(a.holders_out + p, -1);
         }
         return;
     }
-    const int32_t i = b - a.batch;
+    const int32_t i = row - a.batch;
     const Branch r = branch_of(a, i);
     for (int32_t c = c0; c < a.columns; c += step) {
         int32_t entry = -1;
@@ -169,197 +258,236 @@ __global__ void __launch_bounds__(kThreads) fork_hold_kernel(ForkArgs a)
     }
 }
 
-// Sum over the threads of a workgroup, and of those before each.
-template <typename T>
-__device__ __forceinline__ T sum_before(T x, T &all)
+// Third step: free pages, and the pages that the sequences before each take.  A sequence is left with the page that it keeps in part if it is the first of those and none holds
+// it whole.
+__device__ __forceinline__ void fork_count(const ForkArgs &a, int32_t block)
 {
-    __shared__ T wave_s[kThreads / 64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    T upto = x;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const T y = __shfl_up(upto, d);
-        upto += lane >= d ? y : 0;
-    }
-    __syncthreads();
-    if (lane == 63) wave_s[wave] = upto;
-    __syncthreads();
-    T before = 0;
-    all = 0;
-#pragma unroll
-    for (int k = 0; k < kThreads / 64; ++k) {
-        before += k < wave ? wave_s[k] : 0;
-        all += wave_s[k];
-    }
-    return before + upto - x;
+    count_block(block, a.pages, a.free_bits, a.free_before, [&](int32_t p) { return fresh(a.holders_out + p) == 0 && fresh(a.keeper + p) == kNone; });
 }
 
-// Pages that a sequence of the next batch takes.
-__device__ __forceinline__ int32_t pages_needed(const ForkArgs &a, int32_t i)
+__device__ __forceinline__ void fork_need(const ForkArgs &a)
 {
-    const Branch r = branch_of(a, i);
-    if (r.wanted < 0) return 0;
-    const int32_t part = page_in_part(a, r);
-    return (part >= 0 && !keeps_part(a, i, part) ? 1 : 0) + columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
-}
-
-// Free pages, a bit each and their number in each block of them, and, by the last workgroup, the pages that the sequences before each take.
-__global__ void __launch_bounds__(kThreads) fork_count_kernel(ForkArgs a)
-{
-    if (blockIdx.x + 1 == gridDim.x) {
-        int64_t before = 0, all;
-        for (int32_t i0 = 0; i0 < a.new_batch; i0 += kThreads) {
-            const int32_t i = i0 + threadIdx.x;
-            const int64_t mine = sum_before<int64_t>(i < a.new_batch ? pages_needed(a, i) : 0, all);
-            if (i < a.new_batch) a.needed[i] = before + mine;
-            before += all;
-        }
-        if (threadIdx.x == 0) a.needed[a.new_batch] = before;
-        return;
-    }
-    int32_t n = 0, all;
-    for (int32_t k = threadIdx.x; k < kPagesPerBlock; k += kThreads) {
-        const int64_t p = (int64_t)blockIdx.x * kPagesPerBlock + k;
-        const bool is = p < a.pages && a.holders_out[p] == 0 && a.keeper[p] == kNone;
-        const uint64_t bits = __ballot(is);
-        if (k % 64 == 0) a.free_bits[p / 64] = bits;
-        n += is;
-    }
-    sum_before(n, all);
-    if (threadIdx.x == 0) a.free_before[blockIdx.x] = all;
-}
-
-// The n-th free page goes to the sequence that takes it; lengths, moves, and holders of pages that are taken or kept in part.
-__global__ void __launch_bounds__(kThreads) fork_take_kernel(ForkArgs a, int32_t blocks)
-{
-    // free pages before this block of them, and of all
-    int32_t before = 0, free_all = 0, all;
-    for (int32_t k0 = 0; k0 < blocks; k0 += kThreads) {
-        const int32_t k = k0 + threadIdx.x, n = k < blocks ? a.free_before[k] : 0;
-        sum_before(k < (int32_t)blockIdx.x ? n : 0, all);
-        before += all;
-        sum_before(n, all);
-        free_all += all;
-    }
-    const int64_t taken_all = a.needed[a.new_batch];
-    const auto served = [&](int32_t i) { return a.needed[i + 1] == a.needed[i] || a.needed[i + 1] <= free_all; };
-    if ((int32_t)blockIdx.x >= blocks) {
-        // sequences, 256 a workgroup
-        __shared__ int32_t dropped_s[kThreads];
-        const int32_t i0 = (blockIdx.x - blocks) * kThreads, i = i0 + threadIdx.x;
-        dropped_s[threadIdx.x] = 0;
+    int64_t before = 0, all;
+    for (int32_t i0 = 0; i0 < a.new_batch; i0 += kWide) {
+        const int32_t i = i0 + (int32_t)threadIdx.x;
+        int64_t mine = 0;
         if (i < a.new_batch) {
             const Branch r = branch_of(a, i);
-            const bool is = r.wanted >= 0 && served(i);
             const int32_t part = page_in_part(a, r);
-            const bool copied = is && part >= 0 && a.needed[i + 1] - a.needed[i] > columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
-            a.length_out[i] = is ? r.wanted : -1;
-            a.moves[3 * i] = copied ? part : -1;
-            if (!copied) a.moves[3 * i + 1] = -1;
-            a.moves[3 * i + 2] = copied ? r.kept & ((1 << a.page_shift) - 1) : 0;
-            if (is && part >= 0 && !copied) a.holders_out[part] = 1;
-            dropped_s[threadIdx.x] = r.wanted >= 0 && !is;
+            const bool copied = part >= 0 && !(fresh(a.keeper + part) == i && fresh(a.holders_out + part) == 0);
+            if (r.wanted >= 0) mine = (copied ? 1 : 0) + columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
         }
-        __syncthreads();
-        // those that found no room hold nothing
-        for (int k = 0; k < kThreads; ++k) {
-            if (!dropped_s[k]) continue;
-            const int32_t part = branch_of(a, i0 + k).kept >> a.page_shift;   // of a page kept in part the holder was not counted
-            for (int32_t c = threadIdx.x; c < a.columns; c += kThreads) {
-                int32_t &entry = a.page_out[(i0 + k) * a.page_out_ld + c];
-                if (entry >= 0 && c != part) atomicAdd(a.holders_out + entry, -1);
-                entry = -1;
-            }
-        }
-        return;
-    }
-    for (int32_t k0 = 0; k0 < kPagesPerBlock && before < taken_all; k0 += kThreads) {
-        const int64_t p = (int64_t)blockIdx.x * kPagesPerBlock + k0 + threadIdx.x;
-        const bool mine = a.free_bits[p / 64] >> (threadIdx.x % 64) & 1;
-        const int32_t rank = before + sum_before<int32_t>(mine, all);
+        const int64_t mine_before = sum_before(mine, all);
+        if (i < a.new_batch) a.needed[i] = before + mine_before;
         before += all;
-        if (!mine || rank >= taken_all) continue;
-        // the sequence: the last one that begins at this page or before, which takes some
+    }
+    if (threadIdx.x == 0) a.needed[a.new_batch] = before;
+}
+
+__device__ __forceinline__ int64_t needed(const ForkArgs &a, int32_t i) { return __hip_atomic_load(a.needed + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool served(const ForkArgs &a, int32_t i, int32_t free_all)
+{
+    const int64_t upto = needed(a, i + 1);
+    return upto == needed(a, i) || upto <= free_all;
+}
+
+// Fourth step, for kWide sequences from i0 on: lengths, moves, and holders of pages that are kept in part.
+__device__ __forceinline__ void fork_finish(const ForkArgs &a, int32_t i0, int32_t free_all)
+{
+    __shared__ int32_t dropped_s[kWide];
+    const int32_t i = i0 + (int32_t)threadIdx.x;
+    bool dropped = false;
+    if (i < a.new_batch) {
+        const Branch r = branch_of(a, i);
+        const bool is = r.wanted >= 0 && served(a, i, free_all);
+        const int32_t part = page_in_part(a, r);
+        const bool copied = is && part >= 0 && needed(a, i + 1) - needed(a, i) > columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
+        a.length_out[i] = is ? r.wanted : -1;
+        a.moves[3 * (int64_t)i] = copied ? part : -1;
+        if (!copied) a.moves[3 * (int64_t)i + 1] = -1;
+        a.moves[3 * (int64_t)i + 2] = copied ? r.kept & ((1 << a.page_shift) - 1) : 0;
+        if (is && part >= 0 && !copied) a.holders_out[part] = 1;
+        dropped = r.wanted >= 0 && !is;
+    }
+    dropped_s[threadIdx.x] = dropped;
+    if (!__syncthreads_or(dropped)) return;
+    // those that found no room hold nothing
+    for (int k = 0; k < kWide; ++k) {
+        if (!dropped_s[k]) continue;
+        const int32_t part = branch_of(a, i0 + k).kept >> a.page_shift;   // of a page kept in part the holder was not counted
+        for (int32_t c = threadIdx.x; c < a.columns; c += kWide) {
+            int32_t &entry = a.page_out[(i0 + k) * a.page_out_ld + c];
+            if (entry >= 0 && c != part) atomicAdd(a.holders_out + entry, -1);
+            entry = -1;
+        }
+    }
+}
+
+// And for the pages of a block: the n-th free page goes to the sequence that takes it.
+__device__ __forceinline__ void fork_take(const ForkArgs &a, int32_t block, int32_t before, int32_t free_all)
+{
+    const int64_t taken_all = needed(a, a.new_batch);
+    if (before >= taken_all) return;
+    each_page(block, a.pages, a.free_bits, before, [&](int32_t p, bool is, int32_t rank) {
+        if (!is || rank >= taken_all) return;
+        // the last sequence that begins at this page or before, which takes some
         int32_t lo = 0, hi = a.new_batch;
         while (hi - lo > 1) {
             const int32_t mid = (lo + hi) / 2;
-            if (a.needed[mid] <= rank) lo = mid; else hi = mid;
+            if (needed(a, mid) <= rank) lo = mid; else hi = mid;
         }
-        if (!served(lo)) continue;
+        if (!served(a, lo, free_all)) return;
         const Branch r = branch_of(a, lo);
         const int32_t first = columns_of(r.kept, a.page_shift), grown = columns_of(r.wanted, a.page_shift) - first;
-        const int32_t copied = (int32_t)(a.needed[lo + 1] - a.needed[lo]) - grown, n = (int32_t)(rank - a.needed[lo]);
-        if (n < copied) a.moves[3 * lo + 1] = (int32_t)p;
-        a.page_out[lo * a.page_out_ld + (n < copied ? r.kept >> a.page_shift : first + n - copied)] = (int32_t)p;
+        const int64_t mine = needed(a, lo);
+        const int32_t copied = (int32_t)(needed(a, lo + 1) - mine) - grown, n = (int32_t)(rank - mine);
+        if (n < copied) a.moves[3 * (int64_t)lo + 1] = p;
+        a.page_out[lo * a.page_out_ld + (n < copied ? r.kept >> a.page_shift : first + n - copied)] = p;
         a.holders_out[p] = 1;
+    });
+}
+
+__global__ void __launch_bounds__(kThreads) fork_begin_kernel(ForkArgs a)
+{
+    const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (p < a.pages) fork_begin(a, p);
+}
+
+__global__ void __launch_bounds__(kThreads) fork_hold_kernel(ForkArgs a) { fork_hold(a, blockIdx.x, blockIdx.y * kThreads + threadIdx.x, gridDim.y * kThreads); }
+
+__global__ void __launch_bounds__(kWide) fork_count_kernel(ForkArgs a, int32_t blocks)
+{
+    if ((int32_t)blockIdx.x < blocks) fork_count(a, blockIdx.x);
+    else fork_need(a);
+}
+
+__global__ void __launch_bounds__(kWide) fork_take_kernel(ForkArgs a, int32_t blocks)
+{
+    int32_t before, free_all;
+    sum_counts(a.free_before, blocks, blockIdx.x, before, free_all);
+    if ((int32_t)blockIdx.x < blocks) fork_take(a, blockIdx.x, before, free_all);
+    else fork_finish(a, (blockIdx.x - blocks) * kWide, free_all);
+}
+
+// All of it by one workgroup.  Pages that are given up by sequences that found no room are not taken by others here either: what is free is settled in the third step.
+__global__ void __launch_bounds__(kWide) fork_kernel(ForkArgs a, int32_t blocks)
+{
+    for (int32_t p = threadIdx.x; p < a.pages; p += kWide) fork_begin(a, p);
+    __threadfence();
+    __syncthreads();
+    // a wavefront for each row
+    for (int32_t row = threadIdx.x / 64; row < a.batch + a.new_batch; row += kWide / 64) fork_hold(a, row, threadIdx.x % 64, 64);
+    __threadfence();
+    __syncthreads();
+    for (int32_t block = 0; block < blocks; ++block) fork_count(a, block);
+    fork_need(a);
+    __threadfence();
+    __syncthreads();
+    int32_t free_all, none;
+    sum_counts(a.free_before, blocks, 0, none, free_all);
+    for (int32_t i0 = 0; i0 < a.new_batch; i0 += kWide) fork_finish(a, i0, free_all);
+    __threadfence();
+    __syncthreads();   // entries of pages that are copied were written in the second step, by others
+    int32_t before = 0;
+    for (int32_t block = 0; block < blocks; ++block) {
+        fork_take(a, block, before, free_all);
+        before += fresh(a.free_before + block);
     }
 }
 
 // -- pages to the lowest numbers ---------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(kThreads) compact_count_kernel(CompactArgs a)
+__device__ __forceinline__ void compact_count(const CompactArgs &a, int32_t block)
 {
+    count_block(block, a.pages, a.used_bits, a.used_before, [&](int32_t p) { return a.holders[p] != 0; });
+}
+
+// Pages in use below number `count`, that of all of them.
+__device__ __forceinline__ int32_t used_below(const CompactArgs &a, int32_t count)
+{
+    const int32_t edge = count / kPagesPerBlock, words = count / 64, rest = count % 64;
     int32_t n = 0, all;
-    for (int32_t k = threadIdx.x; k < kPagesPerBlock; k += kThreads) {
-        const int32_t p = blockIdx.x * kPagesPerBlock + k;
-        n += p < a.pages && a.holders[p] != 0;
+    for (int32_t k = threadIdx.x; k < edge; k += kWide) n += fresh(a.used_before + k);
+    for (int32_t w = edge * 64 + (int32_t)threadIdx.x; w <= words && w * 64 < count; w += kWide) {
+        const uint64_t word = __hip_atomic_load(a.used_bits + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        n += __popcll(w < words ? word : word & (((uint64_t)1 << rest) - 1));
     }
     sum_before(n, all);
-    if (threadIdx.x == 0) a.used_before[blockIdx.x] = all;
+    return all;
 }
 
 // The k-th page in use from number `count` on goes to the k-th free one below it: sources and targets of the moves, each by its own thread.  holders_out may be holders.
-__global__ void __launch_bounds__(kThreads) compact_moves_kernel(CompactArgs a, int32_t blocks)
+__device__ __forceinline__ void compact_moves(const CompactArgs &a, int32_t block, int32_t before, int32_t count, int32_t below_count)
 {
-    // pages in use before this block of them, in all, and below `count`: in the blocks before the one that has number `count`, and some of that one
-    int32_t before = 0, count = 0, below_count = 0, n = 0, all;
-    for (int32_t k0 = 0; k0 < blocks; k0 += kThreads) {
-        const int32_t k = k0 + threadIdx.x, used = k < blocks ? a.used_before[k] : 0;
-        sum_before(k < (int32_t)blockIdx.x ? used : 0, all);
-        before += all;
-        sum_before(used, all);
-        count += all;
-    }
-    const int32_t edge = count / kPagesPerBlock;
-    for (int32_t k = threadIdx.x; k < edge; k += kThreads) n += a.used_before[k];
-    for (int32_t p = edge * kPagesPerBlock + threadIdx.x; p < count; p += kThreads) n += a.holders[p] != 0;
-    sum_before(n, below_count);
     const int32_t moved = count - below_count;   // as many are free below `count`
-    for (int32_t k0 = 0; k0 < kPagesPerBlock; k0 += kThreads) {
-        const int64_t at = (int64_t)blockIdx.x * kPagesPerBlock + k0 + threadIdx.x;
-        const int32_t p = (int32_t)at;
-        const bool used = at < a.pages && a.holders[p] != 0;
-        const int32_t used_before = before + sum_before<int32_t>(used, all);
-        before += all;
-        if (at >= a.pages) continue;
+    each_page(block, a.pages, a.used_bits, before, [&](int32_t p, bool used, int32_t used_before) {
         if (used && p >= count) a.moves[3 * (int64_t)(used_before - below_count)] = p;
         if (!used && p < count) a.moves[3 * (int64_t)(p - used_before) + 1] = p;
         if (p < a.pages / 2) {
-            if (p >= moved) a.moves[3 * at] = a.moves[3 * at + 1] = -1;
-            a.moves[3 * at + 2] = p < moved ? 1 << a.page_shift : 0;
+            const int64_t at = 3 * (int64_t)p;
+            if (p >= moved) a.moves[at] = a.moves[at + 1] = -1;
+            a.moves[at + 2] = p < moved ? 1 << a.page_shift : 0;
         }
         a.to[p] = p;
         a.holders_out[p] = a.holders[p];
-    }
+    });
 }
 
-// Where pages went, and their holders.
-__global__ void __launch_bounds__(kThreads) compact_to_kernel(CompactArgs a)
+// Where page number k of the moves went, and its holders.
+__device__ __forceinline__ void compact_to(const CompactArgs &a, int64_t k)
 {
-    const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (k >= a.pages / 2 || a.moves[3 * k] < 0) return;
-    const int32_t from = a.moves[3 * k], to = a.moves[3 * k + 1];
+    const int32_t from = fresh(a.moves + 3 * k), to = fresh(a.moves + 3 * k + 1);
+    if (from < 0) return;
     a.to[from] = to;
-    a.holders_out[to] = a.holders_out[from];
+    a.holders_out[to] = fresh(a.holders_out + from);
     a.holders_out[from] = 0;
 }
 
-__global__ void __launch_bounds__(kThreads) compact_tables_kernel(CompactArgs a)
+__device__ __forceinline__ void compact_table(const CompactArgs &a, int32_t b, int32_t c0, int32_t step)
 {
-    const int32_t b = blockIdx.x, n = a.length[b], used = n > (int64_t)a.columns << a.page_shift ? 0 : columns_of(n, a.page_shift);
-    for (int32_t c = blockIdx.y * kThreads + threadIdx.x; c < a.columns; c += gridDim.y * kThreads) {
+    const int32_t n = a.length[b], used = n > (int64_t)a.columns << a.page_shift ? 0 : columns_of(n, a.page_shift);
+    for (int32_t c = c0; c < a.columns; c += step) {
         const int32_t p = a.page[b * a.page_ld + c];
-        a.page_out[b * a.page_out_ld + c] = c < used && (uint32_t)p < (uint32_t)a.pages ? a.to[p] : p;
+        a.page_out[b * a.page_out_ld + c] = c < used && (uint32_t)p < (uint32_t)a.pages ? fresh(a.to + p) : p;
     }
+}
+
+__global__ void __launch_bounds__(kWide) compact_count_kernel(CompactArgs a) { compact_count(a, blockIdx.x); }
+
+__global__ void __launch_bounds__(kWide) compact_moves_kernel(CompactArgs a, int32_t blocks)
+{
+    int32_t before, count;
+    sum_counts(a.used_before, blocks, blockIdx.x, before, count);
+    compact_moves(a, blockIdx.x, before, count, used_below(a, count));
+}
+
+__global__ void __launch_bounds__(kThreads) compact_to_kernel(CompactArgs a)
+{
+    const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (k < a.pages / 2) compact_to(a, k);
+}
+
+__global__ void __launch_bounds__(kThreads) compact_tables_kernel(CompactArgs a) { compact_table(a, blockIdx.x, blockIdx.y * kThreads + threadIdx.x, gridDim.y * kThreads); }
+
+// All of it by one workgroup.
+__global__ void __launch_bounds__(kWide) compact_kernel(CompactArgs a, int32_t blocks)
+{
+    for (int32_t block = 0; block < blocks; ++block) compact_count(a, block);
+    __threadfence();
+    __syncthreads();
+    int32_t none, count;
+    sum_counts(a.used_before, blocks, 0, none, count);
+    const int32_t below_count = used_below(a, count);
+    int32_t before = 0;
+    for (int32_t block = 0; block < blocks; ++block) {
+        compact_moves(a, block, before, count, below_count);
+        before += fresh(a.used_before + block);
+    }
+    __threadfence();
+    __syncthreads();
+    for (int32_t k = threadIdx.x; k < a.pages / 2; k += kWide) compact_to(a, k);
+    __threadfence();
+    __syncthreads();
+    for (int32_t b = threadIdx.x / 64; b < a.batch; b += kWide / 64) compact_table(a, b, threadIdx.x % 64, 64);
 }
 
 }  // namespace
@@ -379,21 +507,32 @@ uint32_t page_blocks(int32_t pages) { return (uint32_t)(((int64_t)pages + kThrea
 
 }  // namespace
 
+// Tables and pages that one workgroup takes: as many as it does with in the time of the launches that it saves.
+constexpr int64_t kSmallEntries = 16384, kSmallPages = 16384;
+
 hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 {
-    const int32_t blocks = blocks_of_pages(a.pages);
+    const int32_t blocks = blocks_of_pages(a.pages), rows = a.batch + a.new_batch;
+    if ((int64_t)rows * a.columns <= kSmallEntries && rows <= kSmallEntries && a.pages <= kSmallPages) {
+        fork_kernel<<<1, kWide, 0, stream>>>(a, blocks);
+        return hipGetLastError();
+    }
     fork_begin_kernel<<<page_blocks(a.pages), kThreads, 0, stream>>>(a);
-    if (a.columns > 0 && a.batch + a.new_batch > 0) fork_hold_kernel<<<dim3(a.batch + a.new_batch, column_blocks(a.columns)), kThreads, 0, stream>>>(a);
-    fork_count_kernel<<<blocks + 1, kThreads, 0, stream>>>(a);
-    fork_take_kernel<<<blocks + (a.new_batch + kThreads - 1) / kThreads, kThreads, 0, stream>>>(a, blocks);
+    if (a.columns > 0 && rows > 0) fork_hold_kernel<<<dim3(rows, column_blocks(a.columns)), kThreads, 0, stream>>>(a);
+    fork_count_kernel<<<blocks + 1, kWide, 0, stream>>>(a, blocks);
+    fork_take_kernel<<<blocks + (a.new_batch + kWide - 1) / kWide, kWide, 0, stream>>>(a, blocks);
     return hipGetLastError();
 }
 
 hipError_t launch_compact(const CompactArgs &a, hipStream_t stream)
 {
     const int32_t blocks = blocks_of_pages(a.pages);
-    compact_count_kernel<<<blocks, kThreads, 0, stream>>>(a);
-    compact_moves_kernel<<<blocks, kThreads, 0, stream>>>(a, blocks);
+    if ((int64_t)a.batch * a.columns <= kSmallEntries && a.batch <= kSmallEntries && a.pages <= kSmallPages) {
+        compact_kernel<<<1, kWide, 0, stream>>>(a, blocks);
+        return hipGetLastError();
+    }
+    compact_count_kernel<<<blocks, kWide, 0, stream>>>(a);
+    compact_moves_kernel<<<blocks, kWide, 0, stream>>>(a, blocks);
     if (a.pages > 1) compact_to_kernel<<<page_blocks(a.pages / 2), kThreads, 0, stream>>>(a);
     if (a.batch > 0 && a.columns > 0) compact_tables_kernel<<<dim3(a.batch, column_blocks(a.columns)), kThreads, 0, stream>>>(a);
     return hipGetLastError();

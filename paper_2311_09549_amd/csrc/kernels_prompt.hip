@@ -16,7 +16,7 @@ size_t prompt_workspace(sc_dtype dtype, int head_dim, int n_cu)
 hipError_t launch_prompt(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream)
 {
     if (a.window) return launch_prompt_window(a, dtype, paged, stream);
-    launch_all<false>(a, dtype, paged, stream);
+    launch_all<kEverything>(a, dtype, paged, stream);
     return hipGetLastError();
 }
 

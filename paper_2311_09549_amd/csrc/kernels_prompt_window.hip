@@ -5,7 +5,7 @@ namespace sck {
 
 hipError_t launch_prompt_window(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream)
 {
-    launch_all<true>(a, dtype, paged, stream);
+    launch_all<kWindow>(a, dtype, paged, stream);
     return hipGetLastError();
 }
 

@@ -408,6 +408,9 @@ void launch_typed(const AttendArgs &a, hipStream_t stream)
 
 }  // namespace
 
+// Pairs of a sequence and a key head, on average, from which on the keys of a tile are shared by the wavefronts of a workgroup, through LDS (prompt_tile.h).
+constexpr int64_t kManyPairs = 96;
+
 size_t row_pieces(int head_dim, int groups_log2) { return sizeof(float) * 2 * ((size_t)1 << groups_log2) * piece_floats(padded_dim(head_dim)); }
 
 // Four tiles of pairs: of heads of 128 for half as many workgroups.
@@ -419,6 +422,7 @@ size_t tree_pieces(int head_dim, int groups_log2)
 
 hipError_t launch_tree(const AttendArgs &a, sc_dtype dtype, hipStream_t stream)
 {
+    if (a.tree && !a.window && dtype != SC_F32 && (int64_t)a.s.rows * a.group >= kManyPairs * a.s.batch) return launch_prompt_tree(a, dtype, stream);
     if (dtype == SC_BF16) launch_typed<Bf16>(a, stream);
     else if (dtype == SC_F16) launch_typed<F16>(a, stream);
     else launch_typed<F32>(a, stream);

@@ -21,11 +21,12 @@ namespace {
 // fp32: below so many workgroups of 64 rows (four for each compute unit) the keys are split too: the five prompts above take 50 us with and 114 without.
 constexpr int64_t kSplitBlocks32 = 1024;
 
-template <typename TR, int DP, bool EXACT, bool PAGED, bool SPLIT, bool WINDOW>
+template <typename TR, int DP, bool EXACT, bool PAGED, bool SPLIT, Sees SEES>
 __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendArgs a)
 {
     using W = Wave<TR, DP, EXACT>;
     constexpr int B = TR::kBytes, TILES = W::TILES, STEP = SPLIT ? 4 * W::KEYS : W::KEYS;
+    constexpr bool WINDOW = SEES == kWindow;
     __shared__ typename std::conditional<SPLIT, typename Join<W>::Space, char>::type join_s;
     const int32_t head = blockIdx.x % a.heads, kv = head / a.group, place = blockIdx.x / a.heads;
     RowBlock blk;
@@ -34,7 +35,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendAr
         __shared__ int32_t keys_s[256];
         __shared__ RowBlock blk_s;
         blk = (int32_t)threadIdx.x < a.blocks ? row_block<16>(a.s, threadIdx.x) : RowBlock{-1, 0, 0, 0, 0};
-        const int32_t mine = blk.sequence < 0 ? -1 : block_keys<WINDOW>(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, 16).length;
+        const int32_t mine = blk.sequence < 0 ? -1 : block_keys<SEES>(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, 16).length;
         keys_s[threadIdx.x] = mine;
         __syncthreads();
         int32_t ahead = 0;
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) prompt_kernel(AttendAr
     RowBlock rows = blk;   // the wavefront's
     rows.first = first;
     rows.end = end;
-    const BlockKeys line = block_keys<WINDOW>(a, rows, length, 16);
+    const BlockKeys line = block_keys<SEES>(a, rows, length, 16);
     const int32_t most = line.length, low = WINDOW ? window_low(a.window, visible - 1) : 0;
     const auto key_of = [&](int32_t place) { return WINDOW && place >= line.first ? place + line.skip : place; };
     const int64_t k_row = (PAGED ? a.cache.row : a.k.row) * B, v_row = (PAGED ? a.cache.row : a.v.row) * B;
@@ -160,7 +161,7 @@ constexpr int kPromptWaves = DP == 256 ? 4 : 8;
 template <int DP>
 constexpr int64_t kSplitTiles = DP == 128 ? 7 : 12;
 
-template <typename TR, int DP, bool PAGED, bool WINDOW>
+template <typename TR, int DP, bool PAGED, Sees SEES>
 void launch_padded(AttendArgs a, hipStream_t stream)
 {
     if constexpr (TR::kBytes == 2) {
@@ -175,16 +176,16 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         // of d, with and without a split: 8, 1, 128, 4,096 rows 80 and 118 us; 4, 4, 256, 2,000 rows 69 and 128; 8, 8, 64, 2,000 rows 38 and 46; chunks
         // behind up to 8,191 keys, 32, 8, 128: 264 and 320; but 32, 8, 128, 2,048 rows 90 and 73, 4,000 rows 196 and 172, 600 rows 50 and 29.
         int64_t longest = PAGED ? table_room(a.s) : a.s.batch > 1 ? 2 * (int64_t)a.s.rows / a.s.batch : a.s.rows;
-        if (WINDOW && longest > (int64_t)a.window + a.sinks + (32 * NW >> heads_log2)) longest = (int64_t)a.window + a.sinks + (32 * NW >> heads_log2);
+        if (SEES == kWindow && longest > (int64_t)a.window + a.sinks + (32 * NW >> heads_log2)) longest = (int64_t)a.window + a.sinks + (32 * NW >> heads_log2);
         const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / KT;
         const int shares = prompt_shares(a.n_cu);
         if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && tiles * shares > kSplitTiles<DP> * shares + 13 * blocks * groups * tiles / 20) {
             a.blocks = (int32_t)blocks;
-            prompt_tile_kernel<TR, DP, PAGED, true, WINDOW, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
+            prompt_tile_kernel<TR, DP, PAGED, true, SEES, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
             prompt_join_kernel<TR, DP, NW><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
             return;
         }
-        const auto kernel = prompt_tile_kernel<TR, DP, PAGED, false, WINDOW, NW, KT>;
+        const auto kernel = prompt_tile_kernel<TR, DP, PAGED, false, SEES, NW, KT>;
         // a grid has fewer than 2^32 threads
         const int64_t each = (((int64_t)1 << 32) / (64 * NW) - 1) / groups;
         for (int64_t end = blocks; end > 0; end -= each) {
@@ -194,8 +195,8 @@ void launch_padded(AttendArgs a, hipStream_t stream)
     } else {
         const bool split = (int64_t)row_blocks<64>(a.s.rows, a.s.batch) * a.heads < kSplitBlocks32;
         a.blocks = split ? row_blocks<16>(a.s.rows, a.s.batch) : row_blocks<64>(a.s.rows, a.s.batch);
-        const auto kernel = a.head_dim == DP ? (split ? prompt_kernel<TR, DP, true, PAGED, true, WINDOW> : prompt_kernel<TR, DP, true, PAGED, false, WINDOW>)
-                                             : (split ? prompt_kernel<TR, DP, false, PAGED, true, WINDOW> : prompt_kernel<TR, DP, false, PAGED, false, WINDOW>);
+        const auto kernel = a.head_dim == DP ? (split ? prompt_kernel<TR, DP, true, PAGED, true, SEES> : prompt_kernel<TR, DP, true, PAGED, false, SEES>)
+                                             : (split ? prompt_kernel<TR, DP, false, PAGED, true, SEES> : prompt_kernel<TR, DP, false, PAGED, false, SEES>);
         // a grid has fewer than 2^32 threads
         const int32_t each = (int32_t)(((int64_t)1 << 24) - 1) / a.heads;
         for (int32_t end = a.blocks; end > 0; end -= each) {
@@ -205,22 +206,22 @@ void launch_padded(AttendArgs a, hipStream_t stream)
     }
 }
 
-template <typename TR, bool PAGED, bool WINDOW>
+template <typename TR, bool PAGED, Sees SEES>
 void launch_typed(const AttendArgs &a, hipStream_t stream)
 {
     const int dp = padded_dim(a.head_dim);
-    if (dp == 64) launch_padded<TR, 64, PAGED, WINDOW>(a, stream);
-    else if (dp == 128) launch_padded<TR, 128, PAGED, WINDOW>(a, stream);
-    else launch_padded<TR, 256, PAGED, WINDOW>(a, stream);
+    if (dp == 64) launch_padded<TR, 64, PAGED, SEES>(a, stream);
+    else if (dp == 128) launch_padded<TR, 128, PAGED, SEES>(a, stream);
+    else launch_padded<TR, 256, PAGED, SEES>(a, stream);
 }
 
-// Through a window or without, each in a source of its own: they take a minute each to compile.
-template <bool WINDOW>
+// What rows see, each kind in a source of its own: they take a minute each to compile.
+template <Sees SEES>
 void launch_all(const AttendArgs &a, sc_dtype dtype, bool paged, hipStream_t stream)
 {
-    if (dtype == SC_BF16) paged ? launch_typed<Bf16, true, WINDOW>(a, stream) : launch_typed<Bf16, false, WINDOW>(a, stream);
-    else if (dtype == SC_F16) paged ? launch_typed<F16, true, WINDOW>(a, stream) : launch_typed<F16, false, WINDOW>(a, stream);
-    else paged ? launch_typed<F32, true, WINDOW>(a, stream) : launch_typed<F32, false, WINDOW>(a, stream);
+    if (dtype == SC_BF16) paged ? launch_typed<Bf16, true, SEES>(a, stream) : launch_typed<Bf16, false, SEES>(a, stream);
+    else if (dtype == SC_F16) paged ? launch_typed<F16, true, SEES>(a, stream) : launch_typed<F16, false, SEES>(a, stream);
+    else paged ? launch_typed<F32, true, SEES>(a, stream) : launch_typed<F32, false, SEES>(a, stream);
 }
 
 }  // namespace

@@ -73,12 +73,15 @@ struct BlockKeys {
     int32_t first, skip, length, low, last_low;
 };
 
-template <bool WINDOW>
+// What rows see: every key before them; of those the ones in a window, and the first ones; what is before their tree, their ancestors and themselves (attention.h).
+enum Sees { kEverything, kWindow, kTree };
+
+template <Sees SEES>
 __device__ __forceinline__ BlockKeys block_keys(const AttendArgs &a, const RowBlock &blk, int32_t length, int32_t tile)
 {
     const int32_t n = keys_seen(a, blk, length, blk.end - 1);
     BlockKeys k = {0, 0, n, 0, 0};
-    if (!WINDOW) return k;
+    if (SEES != kWindow) return k;
     k.low = window_low(a.window, keys_seen(a, blk, length, blk.first) - 1);
     k.last_low = window_low(a.window, n - 1);
     const int32_t from = k.low / tile * tile, first = a.sinks < from ? (a.sinks + tile - 1) / tile * tile : from;
@@ -86,18 +89,28 @@ __device__ __forceinline__ BlockKeys block_keys(const AttendArgs &a, const RowBl
     return k;
 }
 
-// WINDOW: rows see the keys of a window alone, and the first ones (attention.h).
+// Length of a sequence whose rows are trees, -1 for a wrong one.
+__device__ __forceinline__ int32_t tree_length(const AttendArgs &a, int32_t b, int32_t count)
+{
+    const int32_t n = paged_length(a.s, b);
+    return n < count || (a.parent && count > kMaxNodes) ? -1 : n;
+}
+
+// kTree: a lane finds the ancestors of its row among the keys of a tile by going up from it, parents in LDS; all lanes of a wavefront go as long as one has any.
 // SPLIT: as in decode, the tiles of keys of all blocks are put in one line, block after block, one group of heads after the other, and every workgroup takes an
 // equal share of it; blocks that shares cut leave pieces, which prompt_join_kernel joins.  Without it a workgroup has one block, and a call takes as long as
 // the longest of them, or as the compute unit that was given most.  Chunks of four prompts behind up to 8,191 keys, 32 heads of 128: 262 to 274 us with, 320
 // without; L2 misses are six times as many, since workgroups begin at different keys, and the join is 18 us.
-template <typename TR, int DP, bool PAGED, bool SPLIT, bool WINDOW, int NW, int KT>
+template <typename TR, int DP, bool PAGED, bool SPLIT, Sees SEES, int NW, int KT>
 __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs a, int heads_log2)
 {
     using P = PromptTile<TR, DP, NW, KT>;
     constexpr int CHUNKS = P::CHUNKS, DT = P::DT, NT = P::NT, LOADS = P::LOADS, R = 32 * NW;
+    constexpr bool WINDOW = SEES == kWindow, TREE = SEES == kTree;
     __shared__ __attribute__((aligned(16))) char tile_s[P::LDS_BYTES];   // [buffer][keys, values]
+    __shared__ int32_t parent_s[TREE ? kMaxNodes : 1];
     const int32_t head_groups = a.heads >> heads_log2;
+    const auto length_of = [&](const RowBlock &blk) { return TREE ? tree_length(a, blk.sequence, blk.count) : PAGED ? paged_length(a.s, blk.sequence) : blk.count; };
 
     // Keys of tiles first_tile .. last_tile - 1 for a block of rows and a group of heads; sums: where the sums go if those are not all tiles that it sees.
     const auto work = [&](const RowBlock &blk, int32_t head_group, int32_t first_tile, int32_t last_tile, float *sums) __attribute__((always_inline)) {
@@ -105,7 +118,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         asm volatile("" : "+v"(thread));   // what follows from it is made again for each block, instead of taking the registers of the main loop
         const int lane = thread % 64, wave = __builtin_amdgcn_readfirstlane(thread / 64), q = lane % 32, half = lane / 32;
         const int32_t head0 = head_group << heads_log2, kv = head0 / a.group;
-        const int32_t length = PAGED ? paged_length(a.s, blk.sequence) : blk.count;
+        const int32_t length = length_of(blk);
         const int32_t head = head0 + (wave & ((1 << heads_log2) - 1)), first = blk.first + 32 * (wave >> heads_log2), row = first + q;
         const bool mine = row < blk.end;
         char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
@@ -116,7 +129,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         }
 
         const auto sees = [&](int32_t r) { return keys_seen(a, blk, length, r); };
-        const BlockKeys line = block_keys<WINDOW>(a, blk, length, KT);
+        const BlockKeys line = block_keys<SEES>(a, blk, length, KT);
         int32_t block_most = line.length;
         if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
         const auto key_of = [&](int32_t place) { return WINDOW && place >= line.first ? place + line.skip : place; };
@@ -124,6 +137,21 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
         // the first key that the lane's row, and any row of the wavefront, sees through the window
         const int32_t low = WINDOW ? window_low(a.window, visible - 1) : 0, least = WINDOW && first < blk.end ? window_low(a.window, sees(first) - 1) : 0;
+
+        // keys before the tree; the lane's node; whether its chain has a wrong number.  Chains are needed where the tiles have nodes.
+        const int32_t before = length - blk.count, node = row - blk.begin;
+        const bool chains = TREE && a.parent && block_most > before;
+        bool wrong = false;
+        if (chains) {
+            for (int32_t i = thread; i < blk.count; i += P::THREADS) parent_s[i] = a.parent[blk.begin + i];
+            __syncthreads();
+            for (int32_t i = mine ? node : -1; __any(i >= 0);) {
+                const int32_t p = parent_s[i < 0 ? 0 : i];
+                const bool ok = i < 0 || parent_ok(i, p);
+                wrong |= !ok;
+                i = i < 0 || !ok ? -1 : p;
+            }
+        }
 
         u32x4 qf[DP / 16];
 #pragma unroll
@@ -191,7 +219,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             return any != 0;
         };
         // They are added to the rows that see them, from memory.
-        const auto add_special = [&](int32_t base) {
+        const auto add_special = [&](int32_t base, const uint32_t (&seen)[NT]) {
 #pragma unroll 1
             for (int32_t key = base; key < base + KT && key < most; ++key) {
                 const char *p = static_cast<const char *>(PAGED ? a.cache.values : a.v.data);
@@ -207,6 +235,12 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                     for (int r = 0; r < 16; ++r) {
                         const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
                         if (key >= visible || e >= a.head_dim || (WINDOW && key < low && key >= a.sinks)) continue;
+                        if (TREE) {
+                            uint32_t word = seen[0];
+#pragma unroll
+                            for (int t = 1; t < NT; ++t) word = (key - base) / 32 == t ? seen[t] : word;
+                            if (!(word >> (key - base) % 32 & 1)) continue;
+                        }
                         const typename TR::elem x = reinterpret_cast<const typename TR::elem *>(p)[e];
                         if ((__builtin_bit_cast(uint16_t, x) & TR::kExponent) == TR::kExponent) o[d][r] += (float)x;
                     }
@@ -224,7 +258,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             v_at[d] = P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, c) + lane % 2 * 8;
         }
         typedef __attribute__((address_space(3))) char *Lds;
-        const auto tile = [&](Lds buffer, int32_t base, auto masked) {
+        const auto tile = [&](Lds buffer, int32_t base, auto masked, const uint32_t (&seen)[NT]) {
             constexpr bool MASK = decltype(masked)::value;
             f32x16 s[NT];
 #pragma unroll
@@ -242,7 +276,8 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int n = 32 * t + 8 * (r / 4) + 4 * half + r % 4;   // number of the key in the tile
-                    if (MASK && !WINDOW) s[t][r] = n < visible - base ? s[t][r] : kMinusInf;
+                    if (MASK && TREE) s[t][r] = seen[t] >> (8 * (r / 4) + r % 4) & 1 ? s[t][r] : kMinusInf;   // (shifted by the lane's 4 half)
+                    if (MASK && SEES == kEverything) s[t][r] = n < visible - base ? s[t][r] : kMinusInf;
                     if (MASK && WINDOW) s[t][r] = n < visible - base && (n >= low - base || n < a.sinks - base) ? s[t][r] : kMinusInf;
                     top = fmaxf(top, s[t][r]);
                 }
@@ -300,7 +335,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         };
 
         if (block_most > 0) {
-            const int32_t block_all = sees(blk.first);   // keys that every row of the block sees
+            const int32_t block_all = TREE && a.parent ? before : sees(blk.first);   // keys that every row of the block sees
             // whether every row of the block sees the whole tile of keys from `key` on
             const auto whole = [&](int32_t key) { return key + KT <= block_all && (!WINDOW || key >= line.last_low || key + KT <= a.sinks); };
             int32_t place = SPLIT ? first_tile * KT : 0;
@@ -310,11 +345,28 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             const auto pass = [&](auto masked) {
                 constexpr bool MASK = decltype(masked)::value;
                 const int32_t base = key_of(place);
-                const bool more = place + KT < block_most, part = (MASK && !WINDOW) || !whole(key_of(place + KT));
+                const bool more = place + KT < block_most, part = (MASK && SEES == kEverything) || !whole(key_of(place + KT));
                 if (more) fetch(key_of(place + KT));
                 if (!MASK || (base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
-                    tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked);
-                    if (MASK && special) add_special(base);
+                    uint32_t seen[NT] = {}, mine_of[NT];
+                    if constexpr (MASK && TREE) {
+                        // bits of the keys before the tree (or, of rows in order, up to the row), then of the row's chain
+                        const int32_t n = (a.parent ? before : visible) - base;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) seen[t] = !mine || n <= 32 * t ? 0u : n >= 32 * t + 32 ? ~0u : (1u << (n - 32 * t)) - 1;
+                        const int32_t first_node = base - before;
+                        for (int32_t i = chains && mine && !wrong ? node : -1; __any(i >= 0 && i >= first_node);) {
+                            const int32_t bit = i - first_node, p = parent_s[i < 0 ? 0 : i];
+                            const uint32_t one = i >= 0 && bit >= 0 && bit < KT ? 1u << (bit & 31) : 0u;
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) seen[t] |= bit >> 5 == t ? one : 0u;
+                            i = i < 0 ? -1 : p;
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mine_of[t] = seen[t] >> 4 * half;
+                    }
+                    tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked, mine_of);
+                    if (MASK && special) add_special(base, seen);
                 }
                 buffer ^= 1;
                 bool any = false;
@@ -337,6 +389,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         }
         if (PAGED) bad = __syncthreads_or(bad);
         l += __shfl_xor(l, 32);
+        if (TREE && wrong) l = __builtin_nanf("");
         if (SPLIT && sums) {
             float *p = sums + wave * kPromptPiece<DP>;
 #pragma unroll
@@ -370,7 +423,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         // tiles of a block of rows; one that sees nothing has one too, since its rows are written
         const auto tiles_of = [&](const RowBlock &blk) {
             if (blk.sequence < 0) return 0;
-            const int32_t n = block_keys<WINDOW>(a, blk, PAGED ? paged_length(a.s, blk.sequence) : blk.count, KT).length;
+            const int32_t n = block_keys<SEES>(a, blk, length_of(blk), KT).length;
             return n <= KT ? 1 : (n - 1) / KT + 1;
         };
         // In the line a block's tiles lie behind kBegin places that stand for its start and end, which cost about as much as they.

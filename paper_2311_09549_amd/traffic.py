@@ -29,7 +29,7 @@ COPY_BYTES = 1 << 30  # size of the calibration copy bench.py queues (well beyon
 
 # Sources of the attention operators, which no contraction runs.
 ATTENTION = ("attention.cpp", "attention.h", "attention_device.h", "kernels_append.hip", "kernels_decode.hip", "kernels_pages.hip", "kernels_prompt.hip",
-             "kernels_prompt_window.hip", "kernels_tree.hip", "prompt_launch.h", "prompt_tile.h")
+             "kernels_prompt_tree.hip", "kernels_prompt_window.hip", "kernels_tree.hip", "prompt_launch.h", "prompt_tile.h")
 HEADER = os.path.join(HERE, "..", "include", "sparsecontract.h")
 ATTENTION_DECLARATIONS = " * Attention over packed rows and over a paged cache.\n"   # where they begin
 
