@@ -84,6 +84,7 @@ class Attention:
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
         self._few_rows = 4 * (32 if head_dim > 128 else 128)   # of a packed prompt: no more than four tiles of keys, which the library never splits
         self._own = {}   # workspaces, made by the first calls that need them
+        self._pages_bytes = {}   # of fork and compact, by the pages of a cache and the next power of two of sequences
         self._h = self.handle.handle
         (self._append, self._prompt, self._prompt_paged, self._decode, self._append_tree, self._tree, self._accept, self._fork, self._compact,
          self._copy) = sc.attention_calls()
@@ -194,8 +195,11 @@ class Attention:
         batch = lengths.shape[0]
         end = self._numbers("last", last, batch)
         if out is None:
-            out, = self._made(stream, (batch,))
-        status = self._accept(self._h, sequences, parent, end, cache, self._numbers("out", out, batch), _raw_stream(self._index) if stream is None else stream)
+            out, = self._made(stream, lambda: (_empty_like(lengths),))
+            result = out.data_ptr()
+        else:
+            result = self._numbers("out", out, batch)
+        status = self._accept(self._h, sequences, parent, end, cache, result, _raw_stream(self._index) if stream is None else stream)
         if status:
             raise sc.ScError(status, "sc_attention_accept")
         return out
@@ -209,12 +213,15 @@ class Attention:
             return self._there(self.fork, pages, lengths, holders, parents, wanted, out, workspace, stream)
         batch, columns, page, page_ld = self._table(pages, lengths)
         new, count = parents.shape[0], holders.shape[0]
-        shapes = (new, columns), (new,), (count,), (new, 3)
+        operands = (self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count), self._numbers("parents", parents, new),
+                    0 if wanted is None else self._numbers("wanted", wanted, new))
         if out is None:
-            out = self._made(stream, *shapes)
-        record = (batch, new, count, page, page_ld, columns, self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count),
-                  self._numbers("parents", parents, new), 0 if wanted is None else self._numbers("wanted", wanted, new), *self._results(out, shapes))
-        self._pages_call(self._fork, "sc_attention_fork", record, count, new, workspace, stream)
+            out = table, after, held, moves = self._made(stream, lambda: (_empty_like(pages) if new == batch else self._empty(new, columns), _empty_like(parents), _empty_like(holders),
+                                                                          self._empty(new, 3)))
+            results = table.data_ptr(), table.stride()[0], after.data_ptr(), held.data_ptr(), moves.data_ptr()
+        else:
+            results = self._results(out, ((new, columns), (new,), (count,), (new, 3)))
+        self._pages_call(self._fork, "sc_attention_fork", (batch, new, count, page, page_ld, columns, *operands, *results), count, new, workspace, stream)
         return tuple(out)
 
     def compact(self, pages, lengths, holders, out=None, workspace=None, stream=None):
@@ -224,13 +231,14 @@ class Attention:
             return self._there(self.compact, pages, lengths, holders, out, workspace, stream)
         batch, columns, page, page_ld = self._table(pages, lengths)
         count = holders.shape[0]
-        shapes = (batch, columns), (count,), (count // 2, 3)
+        length, held = self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count)
         if out is None:
-            out = self._made(stream, *shapes)
-        table, table_ld, after, moves = self._results(out, shapes)
-        record = (batch, 0, count, page, page_ld, columns, self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count), 0, 0,
-                  table, table_ld, 0, after, moves)
-        self._pages_call(self._compact, "sc_attention_compact", record, count, 0, workspace, stream)
+            out = table, after, moves = self._made(stream, lambda: (_empty_like(pages), _empty_like(holders), self._empty(count // 2, 3)))
+            table, table_ld, after, moves = table.data_ptr(), table.stride()[0], after.data_ptr(), moves.data_ptr()
+        else:
+            table, table_ld, after, moves = self._results(out, ((batch, columns), (count,), (count // 2, 3)))
+        self._pages_call(self._compact, "sc_attention_compact", (batch, 0, count, page, page_ld, columns, length, held, 0, 0, table, table_ld, 0, after, moves), count, 0,
+                         workspace, stream)
         return tuple(out)
 
     def copy(self, keys, values, moves, stream=None):
@@ -344,29 +352,29 @@ class Attention:
             self._refuse_table("out", " x ".join(str(n) for n in shapes[0]), first)
         return (first.data_ptr(), stride[0], *(self._numbers("out", x, *shape) for x, shape in zip(rest, shapes[1:])))
 
-    def _made(self, stream, *shapes):
+    def _empty(self, *shape):
+        return torch.empty(shape, dtype=_INT32, device=self.device)
+
+    def _made(self, stream, make):
         """Tables of the results, memory of the stream of the call."""
-        if stream is not None and stream != _raw_stream(self._index):
-            current = torch.cuda.current_stream(self.device)
-            with self._memory_of(stream):
-                tables = self._made(None, *shapes)
-            for x in tables:
-                x.record_stream(current)
-            return tables
-        return tuple(torch.empty(shape, dtype=_INT32, device=self.device) for shape in shapes)
+        if stream is None or stream == _raw_stream(self._index):
+            return make()
+        current = torch.cuda.current_stream(self.device)
+        with self._memory_of(stream):
+            tables = make()
+        for x in tables:
+            x.record_stream(current)
+        return tables
 
     def _pages_call(self, call, name, record, count, new, workspace, stream):
-        """The workspace of such a call goes back to its stream with it."""
         if stream is None:
             stream = _raw_stream(self._index)
-        if workspace is None:
-            size = sc.attention_pages_workspace_bytes(count, new)
-            if stream == _raw_stream(self._index):
-                workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
-            else:
-                with self._memory_of(stream):
-                    workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
-        address, size = self._workspace_of(stream, workspace, None)
+        key = None
+        if workspace is None:   # the handle's own, for as many pages and few sizes of batches
+            key = count, 1 << new.bit_length()
+            if key not in self._pages_bytes:
+                self._pages_bytes[key] = sc.attention_pages_workspace_bytes(count, min(key[1], 2 ** 20 - 1))
+        address, size = self._workspace_of(stream, workspace, key)
         status = call(self._h, _pack_pages(*record), address, size, stream)
         if status:
             raise sc.ScError(status, name)
@@ -389,7 +397,8 @@ class Attention:
         own = self._own.get(name)
         if own is None:
             with self._memory_of(stream):
-                own = self._own[name] = (torch.empty(getattr(self, name), dtype=torch.uint8, device=self.device), {stream})
+                size = self._pages_bytes[name] if name in self._pages_bytes else getattr(self, name)
+                own = self._own[name] = (torch.empty(size, dtype=torch.uint8, device=self.device), {stream})
         tensor, streams = own
         if stream not in streams:   # not given away before this stream is done with it either
             streams.add(stream)

@@ -100,6 +100,15 @@ __device__ __forceinline__ float finite_max(float m) { return m == kMinusInf ? 0
 // Of 16 bits those below x.
 __device__ __forceinline__ uint32_t below(int32_t x) { return x <= 0 ? 0u : x >= 16 ? 0xffffu : (1u << x) - 1; }
 
+// Page of key j of sequence b, as page_of, for a sequence and a key that all lanes have alike: read by the scalar unit, whose wait is not one for the vector loads on
+// their way.
+__device__ __forceinline__ int32_t page_of_all(const Sequences &s, int32_t b, int32_t j)
+{
+    const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(b) * s.page_ld + (__builtin_amdgcn_readfirstlane(j) >> s.page_shift);
+    const int32_t p = ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)s.page)[at];
+    return (uint32_t)p < (uint32_t)s.pages ? p : -1;
+}
+
 // Where 16 keys lie (wave-uniform): first rows of keys and values for the lane's head, and the last key of the tile that may be read (0..15).
 struct KeyTile {
     const char *k, *v;

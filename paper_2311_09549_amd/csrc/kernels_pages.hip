@@ -369,30 +369,48 @@ __global__ void __launch_bounds__(kWide) fork_take_kernel(ForkArgs a, int32_t bl
     else fork_finish(a, (blockIdx.x - blocks) * kWide, free_all);
 }
 
-// All of it by one workgroup.  Pages that are given up by sequences that found no room are not taken by others here either: what is free is settled in the third step.
+// All of it by one workgroup, tables of numbers of sequences and pages in LDS: few of the steps wait for memory.
+constexpr int32_t kSmallEntries = 32768, kSmallPages = 8192;   // of sequences kWide at most
+
 __global__ void __launch_bounds__(kWide) fork_kernel(ForkArgs a, int32_t blocks)
 {
-    for (int32_t p = threadIdx.x; p < a.pages; p += kWide) fork_begin(a, p);
-    __threadfence();
+    __shared__ int32_t holders_s[kSmallPages], keeper_s[kSmallPages], length_s[kWide], parent_s[kWide], wanted_s[kWide], free_s[kSmallPages / kPagesPerBlock];
+    __shared__ int64_t needed_s[kWide + 1];
+    __shared__ uint64_t bits_s[kSmallPages / 64];
+    int32_t *const holders_out = a.holders_out;
+    const int32_t t = threadIdx.x;
+    if (t < a.batch) length_s[t] = a.length[t];
+    if (t < a.new_batch) parent_s[t] = a.parent[t];
+    if (t < a.new_batch && a.wanted) wanted_s[t] = a.wanted[t];
+    a.length = length_s;
+    a.parent = parent_s;
+    a.wanted = a.wanted ? wanted_s : nullptr;
+    a.holders_out = holders_s;
+    a.keeper = keeper_s;
+    a.free_bits = bits_s;
+    a.free_before = free_s;
+    a.needed = needed_s;
+#pragma unroll
+    for (int32_t k = 0; k < kSmallPages; k += kWide)
+        if (k + t < a.pages) fork_begin(a, k + t);
     __syncthreads();
     // a wavefront for each row
-    for (int32_t row = threadIdx.x / 64; row < a.batch + a.new_batch; row += kWide / 64) fork_hold(a, row, threadIdx.x % 64, 64);
-    __threadfence();
+    for (int32_t row = t / 64; row < a.batch + a.new_batch; row += kWide / 64) fork_hold(a, row, t % 64, 64);
     __syncthreads();
     for (int32_t block = 0; block < blocks; ++block) fork_count(a, block);
     fork_need(a);
-    __threadfence();
     __syncthreads();
-    int32_t free_all, none;
-    sum_counts(a.free_before, blocks, 0, none, free_all);
-    for (int32_t i0 = 0; i0 < a.new_batch; i0 += kWide) fork_finish(a, i0, free_all);
-    __threadfence();
+    int32_t free_all = 0;
+    for (int32_t block = 0; block < blocks; ++block) free_all += free_s[block];
+    fork_finish(a, 0, free_all);
     __syncthreads();   // entries of pages that are copied were written in the second step, by others
     int32_t before = 0;
     for (int32_t block = 0; block < blocks; ++block) {
         fork_take(a, block, before, free_all);
-        before += fresh(a.free_before + block);
+        before += free_s[block];
     }
+    __syncthreads();
+    for (int32_t p = t; p < a.pages; p += kWide) holders_out[p] = holders_s[p];
 }
 
 // -- pages to the lowest numbers ---------------------------------------------------------------------------------------------------
@@ -468,26 +486,37 @@ __global__ void __launch_bounds__(kThreads) compact_to_kernel(CompactArgs a)
 
 __global__ void __launch_bounds__(kThreads) compact_tables_kernel(CompactArgs a) { compact_table(a, blockIdx.x, blockIdx.y * kThreads + threadIdx.x, gridDim.y * kThreads); }
 
-// All of it by one workgroup.
+// All of it by one workgroup, pages and moves in LDS.
 __global__ void __launch_bounds__(kWide) compact_kernel(CompactArgs a, int32_t blocks)
 {
-    for (int32_t block = 0; block < blocks; ++block) compact_count(a, block);
-    __threadfence();
+    __shared__ int32_t holders_s[kSmallPages], to_s[kSmallPages], moves_s[kSmallPages / 2 * 3], used_s[kSmallPages / kPagesPerBlock];
+    __shared__ uint64_t bits_s[kSmallPages / 64];
+    int32_t *const holders_out = a.holders_out, *const moves = a.moves;
+    const int32_t t = threadIdx.x;
+#pragma unroll
+    for (int32_t k = 0; k < kSmallPages; k += kWide)
+        if (k + t < a.pages) holders_s[k + t] = a.holders[k + t];
+    a.holders = a.holders_out = holders_s;
+    a.to = to_s;
+    a.moves = moves_s;
+    a.used_bits = bits_s;
+    a.used_before = used_s;
     __syncthreads();
-    int32_t none, count;
-    sum_counts(a.used_before, blocks, 0, none, count);
+    for (int32_t block = 0; block < blocks; ++block) compact_count(a, block);
+    __syncthreads();
+    int32_t count = 0, before = 0;
+    for (int32_t block = 0; block < blocks; ++block) count += used_s[block];
     const int32_t below_count = used_below(a, count);
-    int32_t before = 0;
     for (int32_t block = 0; block < blocks; ++block) {
         compact_moves(a, block, before, count, below_count);
-        before += fresh(a.used_before + block);
+        before += used_s[block];
     }
-    __threadfence();
     __syncthreads();
-    for (int32_t k = threadIdx.x; k < a.pages / 2; k += kWide) compact_to(a, k);
-    __threadfence();
+    for (int32_t k = t; k < a.pages / 2; k += kWide) compact_to(a, k);
     __syncthreads();
-    for (int32_t b = threadIdx.x / 64; b < a.batch; b += kWide / 64) compact_table(a, b, threadIdx.x % 64, 64);
+    for (int32_t b = t / 64; b < a.batch; b += kWide / 64) compact_table(a, b, t % 64, 64);
+    for (int32_t p = t; p < a.pages; p += kWide) holders_out[p] = holders_s[p];
+    for (int32_t k = t; k < a.pages / 2 * 3; k += kWide) moves[k] = moves_s[k];
 }
 
 }  // namespace
@@ -507,13 +536,10 @@ uint32_t page_blocks(int32_t pages) { return (uint32_t)(((int64_t)pages + kThrea
 
 }  // namespace
 
-// Tables and pages that one workgroup takes: as many as it does with in the time of the launches that it saves.
-constexpr int64_t kSmallEntries = 16384, kSmallPages = 16384;
-
 hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 {
     const int32_t blocks = blocks_of_pages(a.pages), rows = a.batch + a.new_batch;
-    if ((int64_t)rows * a.columns <= kSmallEntries && rows <= kSmallEntries && a.pages <= kSmallPages) {
+    if ((int64_t)rows * a.columns <= kSmallEntries && a.batch <= kWide && a.new_batch <= kWide && a.pages <= kSmallPages) {
         fork_kernel<<<1, kWide, 0, stream>>>(a, blocks);
         return hipGetLastError();
     }
@@ -527,7 +553,7 @@ hipError_t launch_fork(const ForkArgs &a, hipStream_t stream)
 hipError_t launch_compact(const CompactArgs &a, hipStream_t stream)
 {
     const int32_t blocks = blocks_of_pages(a.pages);
-    if ((int64_t)a.batch * a.columns <= kSmallEntries && a.batch <= kSmallEntries && a.pages <= kSmallPages) {
+    if ((int64_t)a.batch * a.columns <= kSmallEntries && a.batch <= kWide && a.pages <= kSmallPages) {
         compact_kernel<<<1, kWide, 0, stream>>>(a, blocks);
         return hipGetLastError();
     }

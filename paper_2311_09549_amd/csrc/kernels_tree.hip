@@ -10,6 +10,7 @@ namespace sck {
 namespace {
 
 constexpr int kWaves = 4;   // that Join takes
+constexpr int64_t kWholeKeys = 512;
 
 // Registers of a wavefront: queries and sums of RT tiles, keys and values of a step.
 template <typename W, int RT>
@@ -98,15 +99,80 @@ struct TreeLine {
     }
 };
 
+// What the rows of a tile of pairs see, in LDS: chains of their parents, and per row the nodes that it sees and its depth.
+template <int PAIRS>
+struct TreeSeen {
+    struct Space {
+        int32_t parent[kMaxNodes];
+        uint32_t seen[PAIRS][kMaxNodes / 32 + 1];
+        int32_t depth[PAIRS];
+    };
+    const AttendArgs &a;
+    Space &space;
+    bool chains;                  // whether `space` is needed, and filled
+    int32_t before;               // keys before the rows
+    int32_t row_first, row_last;  // of the tile
+    int32_t all, low;             // keys that all rows of the tile see: below `all`, and from `low` on or below `sinks`
+
+    // `tile`: of pairs; `end`: of the keys of the line that it takes here.
+    __device__ __forceinline__ TreeSeen(const AttendArgs &args, Space &s, const TreeSequence &q, int32_t tile, int32_t end) : a(args), space(s)
+    {
+        before = q.length - q.count;
+        row_first = same(tile * PAIRS / a.group);
+        row_last = same((tile * PAIRS + PAIRS - 1) / a.group);
+        row_last = row_last < q.count ? row_last : q.count - 1;
+        // chains, where keys are nodes or a window goes by depths
+        chains = a.parent && q.length >= 0 && (a.window || key_at(q.span, end - 1) >= before);
+        all = a.parent ? before : before + row_first + 1;
+        low = window_low(a.window, before + row_last);
+    }
+    // By all threads of a workgroup, which meet twice.
+    __device__ __forceinline__ void fill(const TreeSequence &q)
+    {
+        if (!chains) return;
+        for (int32_t i = threadIdx.x; i < q.count; i += blockDim.x) space.parent[i] = a.parent[q.begin + i];
+        __syncthreads();
+        const int32_t i = row_first + (int32_t)threadIdx.x;
+        if (i <= row_last) {
+            const int32_t depth = depth_of(space.parent, i);
+            uint32_t(&seen)[kMaxNodes / 32 + 1] = space.seen[threadIdx.x];
+            space.depth[threadIdx.x] = depth;
+            int32_t node = depth < 0 ? -1 : i, up = 0;
+            seen[(q.count + 31) / 32] = 0;
+            for (int32_t word = (q.count - 1) / 32; word >= 0; --word) {
+                uint32_t bits = 0;
+                for (; node >= 32 * word && node >= 0; node = space.parent[node], ++up)
+                    if (!a.window || up < a.window || before + depth - up < a.sinks) bits |= 1u << (node & 31);
+                seen[word] = bits;
+            }
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool whole(int32_t key) const { return key + 16 <= all && (key >= low || key + 16 <= a.sinks); }
+    // Of the 16 keys from `key` on, bits of those that row i sees.
+    __device__ __forceinline__ uint32_t of(int32_t key, int32_t i) const
+    {
+        const int32_t at = i - row_first, place = a.parent ? (chains ? before + space.depth[at] : 0) : before + i;
+        uint32_t bits = below((a.parent ? before : place + 1) - key);
+        if (a.window) bits &= ~below(window_low(a.window, place) - key) | below(a.sinks - key);
+        if (a.parent && key + 16 > before) {
+            const int32_t node = key - before;   // the first of them; nodes behind the last have no bits
+            const uint32_t *seen = space.seen[at];
+            if (node < 0) bits |= seen[0] << -node;
+            else bits |= (uint32_t)(((uint64_t)seen[node / 32 + 1] << 32 | seen[node / 32]) >> (node & 31));
+        }
+        return bits & 0xffffu;
+    }
+    __device__ __forceinline__ bool wrong(int32_t i) const { return chains && i >= 0 && space.depth[i - row_first] < 0; }
+};
+
 template <typename TR, int DP, bool EXACT, int RT>
 __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>, RT>)) tree_kernel(AttendArgs a, int32_t groups_log2)
 {
     using W = Wave<TR, DP, EXACT>;
     constexpr int B = TR::kBytes, TILES = W::TILES, EPL = W::EPL, PAIRS = 16 * RT;
     __shared__ typename Join<W>::Space join_s;
-    __shared__ int32_t parent_s[kMaxNodes];
-    __shared__ uint32_t seen_s[PAIRS][kMaxNodes / 32 + 1];   // per row of a tile of pairs, the nodes that it sees
-    __shared__ int32_t depth_s[PAIRS];
+    __shared__ typename TreeSeen<PAIRS>::Space seen_s;
     const int lane = threadIdx.x % 64, wave = same(threadIdx.x / 64);
     TreeLine<PAIRS> line = {a, lane};
     const int64_t units = line.all();   // in scalar registers, as what follows from it
@@ -149,7 +215,7 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
             for (int n = 0; n < TILES; ++n) {
                 const int32_t v = base + 16 * n, key = key_at(part.q.span, v < part.q.span.length ? v : base);   // behind the last key nothing is seen: any rows that are there
                 t[n].last = part.q.length - 1 - key;
-                int32_t page = page_of(a.s, part.b, key);
+                int32_t page = page_of_all(a.s, part.b, key);
                 bad |= page < 0;
                 if (page < 0) page = 0;
                 const int64_t off = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + part.kv * a.cache.head) * B;
@@ -173,46 +239,8 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
                 w[0].load_keys(keys, t, row_bytes);
                 w[0].load_values(values, t, row_bytes);
             }
-            const int32_t before = part.q.length - part.q.count;   // keys before the rows
-            const int32_t row_first = same(part.tile * PAIRS / a.group);
-            int32_t row_last = same((part.tile * PAIRS + PAIRS - 1) / a.group);
-            row_last = row_last < part.q.count ? row_last : part.q.count - 1;
-            // Chains of the tile's rows, where its keys are nodes or a window goes by depths.
-            const bool chains = a.parent && part.q.length >= 0 && (a.window || key_at(part.q.span, end - 1) >= before);
-            if (chains) {
-                for (int32_t i = threadIdx.x; i < part.q.count; i += 64 * kWaves) parent_s[i] = a.parent[part.q.begin + i];
-                __syncthreads();
-                const int32_t i = row_first + (int32_t)threadIdx.x;
-                if (i <= row_last) {
-                    const int32_t depth = depth_of(parent_s, i);
-                    uint32_t(&seen)[kMaxNodes / 32 + 1] = seen_s[threadIdx.x];
-                    depth_s[threadIdx.x] = depth;
-                    int32_t node = depth < 0 ? -1 : i, up = 0;
-                    seen[(part.q.count + 31) / 32] = 0;
-                    for (int32_t word = (part.q.count - 1) / 32; word >= 0; --word) {
-                        uint32_t bits = 0;
-                        for (; node >= 32 * word && node >= 0; node = parent_s[node], ++up)
-                            if (!a.window || up < a.window || before + depth - up < a.sinks) bits |= 1u << (node & 31);
-                        seen[word] = bits;
-                    }
-                }
-                __syncthreads();
-            }
-            // keys that all rows of the tile see: below `all`, and from `low` on or below `sinks`
-            const int32_t all = a.parent ? before : before + row_first + 1, low = window_low(a.window, before + row_last);
-            // of the 16 keys from `key` on, bits of those that the lane's row i sees
-            const auto seen_of = [&](int32_t key, int32_t i) {
-                const int32_t at_s = i - row_first, place = a.parent ? (chains ? before + depth_s[at_s] : 0) : before + i;
-                uint32_t bits = below((a.parent ? before : place + 1) - key);
-                if (a.window) bits &= ~below(window_low(a.window, place) - key) | below(a.sinks - key);
-                if (a.parent && key + 16 > before) {
-                    const int32_t node = key - before;   // the first of them; nodes behind the last have no bits
-                    const uint32_t *seen = seen_s[at_s];
-                    if (node < 0) bits |= seen[0] << -node;
-                    else bits |= (uint32_t)(((uint64_t)seen[node / 32 + 1] << 32 | seen[node / 32]) >> (node & 31));
-                }
-                return bits & 0xffffu;
-            };
+            TreeSeen<PAIRS> rows(a, seen_s, part.q, part.tile, end);
+            rows.fill(part.q);
             for (int32_t base = base0; base < end; base += STEP) {
                 const bool more = base + STEP < end;
                 typename W::Scores scores[RT];
@@ -228,7 +256,7 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
 #pragma unroll
                 for (int n = 0; n < TILES; ++n) {
                     key[n] = key_at(part.q.span, base + 16 * n);
-                    whole &= base + 16 * n < part.q.span.length && key[n] + 16 <= all && (key[n] >= low || key[n] + 16 <= a.sinks);
+                    whole &= base + 16 * n < part.q.span.length && rows.whole(key[n]);
                 }
                 if (!whole) {
 #pragma unroll
@@ -238,7 +266,7 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
                         seen[r] = 0;
 #pragma unroll
                         for (int n = 0; n < TILES; ++n)
-                            if (base + 16 * n < part.q.span.length) seen[r] |= seen_of(key[n], row[r] < 0 ? row_first : row[r]) << 16 * n;
+                            if (base + 16 * n < part.q.span.length) seen[r] |= rows.of(key[n], row[r] < 0 ? rows.row_first : row[r]) << 16 * n;
                         W::mask(scores[r], seen[r] >> 4 * w[0].g);
                     }
                     special = W::any_special(values);
@@ -268,7 +296,7 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
             float *piece = a.pieces + (int64_t)piece_slot(first, share0, blockIdx.x) * RT * piece_floats(DP);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const bool wrong = bad || (chains && row[r] >= 0 && depth_s[row[r] - row_first] < 0);
+                const bool wrong = bad || rows.wrong(row[r]);
                 const float l = over_groups_sum(w[r].l);
                 float x[EPL], top, sum;
                 Join<W>::run(w[r], join_s, wave, lane, wrong ? __builtin_nanf("") : l, a.scale_log2, x, top, sum);
@@ -367,6 +395,138 @@ __global__ void __launch_bounds__(256) tree_join_kernel(AttendArgs a, int32_t gr
     else *reinterpret_cast<f32x4 *>(out) = sum;
 }
 
+// Few keys: a workgroup for each tile of 16 pairs, whose wavefronts take a few steps each; no shares to find, no pieces to join.
+template <int DP>
+constexpr int kWholeWaves = DP == 256 ? 4 : 8;
+
+// Tiles of pairs of all sequences, without a table of them: sequence b has the numbers from row_begin(b) * group / 16 + b up to that of b + 1, never fewer than it has tiles;
+// numbers left over have no pairs.
+__device__ __forceinline__ int32_t first_tile_of(const AttendArgs &a, int32_t b) { return (int32_t)((int64_t)row_begin(a.s, b) * a.group / kHeadTile) + b; }
+
+template <typename TR, int DP, bool EXACT>
+__global__ void __launch_bounds__(64 * kWholeWaves<DP>, kWholeWaves<DP> / 4) tree_whole_kernel(AttendArgs a)
+{
+    using W = Wave<TR, DP, EXACT>;
+    constexpr int B = TR::kBytes, TILES = W::TILES, EPL = W::EPL, WAVES = kWholeWaves<DP>, LD = DP + 4, PAIRS = kHeadTile;   // rows of sums begin in different banks
+    // chains are done with before sums are stored
+    __shared__ union {
+        typename TreeSeen<PAIRS>::Space seen;
+        __attribute__((aligned(16))) float sum[WAVES][PAIRS][LD];
+    } space_s;
+    __shared__ float top_s[WAVES][PAIRS], weight_s[WAVES][PAIRS];
+    const int lane = threadIdx.x % 64, wave = same(threadIdx.x / 64);
+    const int32_t kv = blockIdx.x % a.kv_heads, number = blockIdx.x / a.kv_heads;
+    // the last sequence that begins at this number or before, 64 at a time
+    int32_t b = 0;
+    for (int32_t end = a.s.batch;;) {
+        const int32_t step = (end - b + 63) / 64;
+        const int64_t at = b + (int64_t)lane * step;
+        const uint64_t bits = __ballot(at < end && first_tile_of(a, (int32_t)at) <= number);
+        if (bits == 0) return;
+        b += (63 - __builtin_clzll(bits)) * step;
+        if (step == 1) break;
+        end = end - b < step ? end : b + step;
+    }
+    TreeSequence q = tree_sequence(a, b);
+    q = {same(q.begin), same(q.count), same(q.length), {same(q.span.first), same(q.span.skip), same(q.span.length)}};
+    const int32_t tile = same(number - first_tile_of(a, b));
+    if (q.count <= 0 || (int64_t)tile * PAIRS >= (int64_t)q.count * a.group) return;
+    constexpr int32_t STEP = WAVES * W::KEYS;
+    W w;
+    w.init(lane, a.head_dim);
+    const int32_t pair = tile * PAIRS + w.col, i = pair / a.group, row = i < q.count ? i : -1;
+    const int32_t head = row < 0 ? 0 : kv * a.group + (pair - i * a.group);
+    w.load_q(static_cast<const char *>(a.q.data) + ((int64_t)(q.begin + (row < 0 ? 0 : row)) * a.q.row + head * a.q.head) * B, row >= 0);
+    const char *k0 = static_cast<const char *>(a.cache.keys) + kv * a.cache.head * B, *v0 = static_cast<const char *>(a.cache.values) + kv * a.cache.head * B;
+    const int64_t row_bytes = a.cache.row * B;
+    const int32_t end = q.span.length;
+    bool bad = q.length < 0;
+    TreeSeen<PAIRS> rows(a, space_s.seen, q, tile, end);
+    bool filled = false;
+    for (int32_t base0 = 0; base0 < end || !filled; base0 += STEP) {
+        const int32_t base = base0 + wave * W::KEYS;
+        typename W::Keys keys;
+        typename W::Values values;
+        typename W::Scores scores;
+        KeyTile t[TILES];
+        int32_t key[TILES];
+        if (base < end) {
+#pragma unroll
+            for (int n = 0; n < TILES; ++n) {
+                key[n] = key_at(q.span, base + 16 * n < end ? base + 16 * n : base);   // behind the last key nothing is seen: any rows that are there
+                t[n].last = q.length - 1 - key[n];
+                int32_t page = page_of_all(a.s, b, key[n]);
+                bad |= page < 0;
+                if (page < 0) page = 0;
+                const int64_t off = (page * a.cache.page + (key[n] & ((1 << a.s.page_shift) - 1)) * a.cache.row) * B;
+                t[n].k = k0 + off;
+                t[n].v = v0 + off;
+            }
+            w.load_keys(keys, t, row_bytes);
+            w.load_values(values, t, row_bytes);
+        }
+        if (!filled) rows.fill(q);   // keys and values are on their way
+        filled = true;
+        if (base < end) {
+            w.scores(scores, keys);
+            uint32_t seen = 0;
+#pragma unroll
+            for (int n = 0; n < TILES; ++n)
+                if (base + 16 * n < end) seen |= rows.of(key[n], row < 0 ? rows.row_first : row) << 16 * n;
+            W::mask(scores, seen >> 4 * w.g);
+            const bool special = W::any_special(values);
+            if (special) W::without_infinities(values);
+            w.add_seen(scores, values, a.scale_log2);
+            if (special) {
+                // infinities and NaN that the product would have spread to rows that do not see them are added to those that do, from memory
+#pragma unroll 1
+                for (int n = 0; n < W::KEYS; ++n) {
+                    const KeyTile &x = n < 16 ? t[0] : t[TILES - 1];
+                    if (n % 16 <= x.last && (seen >> n & 1)) w.add_special(x.v + n % 16 * row_bytes);
+                }
+            }
+        }
+    }
+    const int parts = end <= 0 ? 0 : end > STEP - W::KEYS ? WAVES : (end - 1) / W::KEYS + 1;   // wavefronts that have had keys
+    const float l = bad || rows.wrong(row) ? __builtin_nanf("") : over_groups_sum(w.l);
+    __syncthreads();
+    if (wave < parts) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int u = 0; u < EPL; u += 4)
+                *reinterpret_cast<f32x4 *>(&space_s.sum[wave][w.col][(4 * w.g + k) * EPL + u]) = f32x4{w.o[u][k], w.o[u + 1][k], w.o[u + 2][k], w.o[u + 3][k]};
+        if (w.g == 0) {
+            top_s[wave][w.col] = w.m;
+            weight_s[wave][w.col] = l;
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < PAIRS * (DP / 4); x += 64 * WAVES) {
+        const int c = x / (DP / 4), e = x % (DP / 4) * 4;
+        const int32_t p = tile * PAIRS + c, r = p / a.group;
+        if (r >= q.count || (!EXACT && e >= a.head_dim)) continue;
+        float m[WAVES], top = kMinusInf, weight = 0.0f;
+        f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) {
+            m[n] = n < parts ? top_s[n][c] : kMinusInf;
+            top = fmaxf(top, m[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < WAVES; ++n) {
+            if (n >= parts) continue;
+            const float factor = __builtin_amdgcn_exp2f((m[n] - finite_max(top)) * a.scale_log2);
+            sum += *reinterpret_cast<const f32x4 *>(&space_s.sum[n][c][e]) * factor;
+            weight += weight_s[n][c] * factor;
+        }
+        sum *= q.length < 0 ? __builtin_nanf("") : weight == 0.0f ? 0.0f : 1.0f / weight;
+        char *out = static_cast<char *>(a.out.data) + ((int64_t)(q.begin + r) * a.out.row + (kv * a.group + p - r * a.group) * a.out.head + e) * B;
+        if constexpr (B == 2) *reinterpret_cast<u32x2 *>(out) = u32x2{TR::pack(sum.x, sum.y), TR::pack(sum.z, sum.w)};
+        else *reinterpret_cast<f32x4 *>(out) = sum;
+    }
+}
+
 template <typename TR, int DP, bool EXACT, int RT>
 void launch_pairs(const AttendArgs &a, hipStream_t stream)
 {
@@ -378,6 +538,14 @@ void launch_pairs(const AttendArgs &a, hipStream_t stream)
 template <typename TR, int DP, bool EXACT>
 void launch_exact(const AttendArgs &a, hipStream_t stream)
 {
+    // Few keys: all that the table has room for, or that a window has (and the rows of a tree behind it).
+    int64_t room = table_room(a.s);
+    if (a.window && room > (int64_t)a.window + a.sinks + 32 + a.s.rows) room = (int64_t)a.window + a.sinks + 32 + a.s.rows;
+    const int64_t tiles = (int64_t)a.s.rows * a.group / kHeadTile + a.s.batch;
+    if (room <= kWholeKeys && tiles * a.kv_heads < 1 << 22) {
+        tree_whole_kernel<TR, DP, EXACT><<<(uint32_t)(tiles * a.kv_heads), 64 * kWholeWaves<DP>, 0, stream>>>(a);
+        return;
+    }
     // Tiles of a workgroup: as many as a sequence has pairs for on average, and as its registers hold.
     constexpr int kMost = kTreeTiles<TR, DP>;
     const int64_t pairs = a.tree ? (int64_t)a.s.rows * a.group / a.s.batch : 1;

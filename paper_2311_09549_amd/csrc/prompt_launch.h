@@ -165,7 +165,7 @@ template <typename TR, int DP, bool PAGED, Sees SEES>
 void launch_padded(AttendArgs a, hipStream_t stream)
 {
     if constexpr (TR::kBytes == 2) {
-        constexpr int NW = kPromptWaves<DP>, KT = DP == 256 ? 32 : 128;
+        constexpr int NW = kPromptWaves<DP>, KT = DP == 256 ? 32 : SEES == kTree ? 64 : 128;
         int heads_log2 = 0;
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;

@@ -133,22 +133,23 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         int32_t block_most = line.length;
         if (SPLIT && last_tile < (block_most + KT - 1) / KT) block_most = last_tile * KT;
         const auto key_of = [&](int32_t place) { return WINDOW && place >= line.first ? place + line.skip : place; };
-        const int32_t visible = mine ? sees(row) : 0;
+        const int32_t visible = mine && !TREE ? sees(row) : 0;
         const int32_t most = first < blk.end ? sees((first + 32 < blk.end ? first + 32 : blk.end) - 1) : 0;
         // the first key that the lane's row, and any row of the wavefront, sees through the window
         const int32_t low = WINDOW ? window_low(a.window, visible - 1) : 0, least = WINDOW && first < blk.end ? window_low(a.window, sees(first) - 1) : 0;
 
         // keys before the tree; the lane's node; whether its chain has a wrong number.  Chains are needed where the tiles have nodes.
-        const int32_t before = length - blk.count, node = row - blk.begin;
+        const int32_t before = length - blk.count;
         const bool chains = TREE && a.parent && block_most > before;
-        bool wrong = false;
+        constexpr int32_t kWrong = -2;
+        int32_t node = mine ? row - blk.begin : -1;
         if (chains) {
             for (int32_t i = thread; i < blk.count; i += P::THREADS) parent_s[i] = a.parent[blk.begin + i];
             __syncthreads();
-            for (int32_t i = mine ? node : -1; __any(i >= 0);) {
+            for (int32_t i = node; __any(i >= 0);) {
                 const int32_t p = parent_s[i < 0 ? 0 : i];
                 const bool ok = i < 0 || parent_ok(i, p);
-                wrong |= !ok;
+                node = ok ? node : kWrong;
                 i = i < 0 || !ok ? -1 : p;
             }
         }
@@ -180,6 +181,17 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         u32x4 ks[LOADS], vs[LOADS];
         // In pages a row's keys and values wait for its page number, within every tile: chunks of four prompts behind up to 8,191 keys take 5.0 us a tile
         // without a split, packed keys 4.1.
+        // Windows and trees: the rows of a load of a wavefront are in one page, whose number is read by the scalar unit a tile ahead.
+        constexpr bool AHEAD = PAGED && SEES != kEverything;
+        static_assert(64 / CHUNKS <= 16, "in one page");
+        int32_t page_next[LOADS];
+        const auto find_pages = [&](int32_t base) {
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                const int32_t key = base + wave * (64 / CHUNKS) + n * P::ROWS_PER_LOAD;
+                if (AHEAD) page_next[n] = page_of_all(a.s, blk.sequence, key < length ? key : length - 1);
+            }
+        };
         const auto fetch = [&](int32_t base) {
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) {
@@ -187,7 +199,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 key = key < length ? key : length - 1;   // rows behind the last key are seen by none: any that are there
                 int64_t k_at = key * k_row, v_at = key * v_row;
                 if (PAGED) {
-                    int32_t page = page_of(a.s, blk.sequence, key);
+                    int32_t page = AHEAD ? page_next[n] : page_of(a.s, blk.sequence, key);
                     bad |= page < 0 && (!WINDOW || key >= line.low || key < a.sinks);   // pages behind every row's window may be gone
                     if (page < 0) page = 0;
                     k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
@@ -234,7 +246,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int e = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-                        if (key >= visible || e >= a.head_dim || (WINDOW && key < low && key >= a.sinks)) continue;
+                        if ((!TREE && key >= visible) || e >= a.head_dim || (WINDOW && key < low && key >= a.sinks)) continue;
                         if (TREE) {
                             uint32_t word = seen[0];
 #pragma unroll
@@ -339,23 +351,28 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             // whether every row of the block sees the whole tile of keys from `key` on
             const auto whole = [&](int32_t key) { return key + KT <= block_all && (!WINDOW || key >= line.last_low || key + KT <= a.sinks); };
             int32_t place = SPLIT ? first_tile * KT : 0;
+            find_pages(key_of(place));
             fetch(key_of(place));
+            find_pages(key_of(place + KT));
             bool special = __syncthreads_or(put(tile_s, !whole(key_of(place))));
             int buffer = 0;
             const auto pass = [&](auto masked) {
                 constexpr bool MASK = decltype(masked)::value;
                 const int32_t base = key_of(place);
                 const bool more = place + KT < block_most, part = (MASK && SEES == kEverything) || !whole(key_of(place + KT));
-                if (more) fetch(key_of(place + KT));
-                if (!MASK || (base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
+                if (more) {
+                    fetch(key_of(place + KT));
+                    find_pages(key_of(place + 2 * KT));
+                }
+                if ((!MASK && (!TREE || first < blk.end)) || (MASK && base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
                     uint32_t seen[NT] = {}, mine_of[NT];
                     if constexpr (MASK && TREE) {
                         // bits of the keys before the tree (or, of rows in order, up to the row), then of the row's chain
-                        const int32_t n = (a.parent ? before : visible) - base;
+                        const int32_t n = (a.parent ? before : before + node + 1) - base;
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) seen[t] = !mine || n <= 32 * t ? 0u : n >= 32 * t + 32 ? ~0u : (1u << (n - 32 * t)) - 1;
+                        for (int t = 0; t < NT; ++t) seen[t] = node < 0 || n <= 32 * t ? 0u : n >= 32 * t + 32 ? ~0u : (1u << (n - 32 * t)) - 1;
                         const int32_t first_node = base - before;
-                        for (int32_t i = chains && mine && !wrong ? node : -1; __any(i >= 0 && i >= first_node);) {
+                        for (int32_t i = chains ? node : -1; __any(i >= 0 && i >= first_node);) {
                             const int32_t bit = i - first_node, p = parent_s[i < 0 ? 0 : i];
                             const uint32_t one = i >= 0 && bit >= 0 && bit < KT ? 1u << (bit & 31) : 0u;
 #pragma unroll
@@ -389,8 +406,9 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         }
         if (PAGED) bad = __syncthreads_or(bad);
         l += __shfl_xor(l, 32);
-        if (TREE && wrong) l = __builtin_nanf("");
+        if (TREE && node == kWrong) l = __builtin_nanf("");
         if (SPLIT && sums) {
+            if (first >= blk.end) return;   // nobody joins it
             float *p = sums + wave * kPromptPiece<DP>;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -520,6 +538,7 @@ __global__ void __launch_bounds__(64) prompt_join_kernel(AttendArgs a, int heads
     }
     const RowBlock blk = row_block_of<32 * NW>(a.s, id % a.blocks, heads_log2);
     const int32_t head = (id / a.blocks << heads_log2) + (wave & ((1 << heads_log2) - 1)), row = blk.first + 32 * (wave >> heads_log2) + lane % 32;
+    if (blk.sequence < 0 || blk.first + 32 * (wave >> heads_log2) >= blk.end) return;
     const auto piece = [&](int32_t n) { return a.pieces + (n == 0 ? 2 * (int64_t)w + 1 : 2 * ((int64_t)w + n)) * NW * kPromptPiece<DP> + wave * kPromptPiece<DP>; };
     float top = kMinusInf;
     for (int32_t n = 0; n <= more; ++n) top = fmaxf(top, piece(n)[32 * DP + lane]);
@@ -537,7 +556,7 @@ __global__ void __launch_bounds__(64) prompt_join_kernel(AttendArgs a, int heads
         for (int i = 0; i < 4 * DT; ++i) o[i] += reinterpret_cast<const f32x4 *>(p)[i * 64 + lane] * factor;
     }
     const float factor = l == 0.0f ? 0.0f : 1.0f / l;
-    if (blk.sequence < 0 || row >= blk.end) return;
+    if (row >= blk.end) return;
     char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
 #pragma unroll
     for (int i = 0; i < 4 * DT; ++i) {

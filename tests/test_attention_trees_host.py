@@ -333,10 +333,15 @@ def test_results_and_workspaces_belong_to_the_stream_of_their_call(monkeypatch):
     calls(attention)["tree"](stream=STREAM, out=OUT["tree"], workspace=None)       # the handle's own: it stays
     calls(attention)["tree"](stream=STREAM, out=OUT["tree"], workspace=None)
     assert [(on, x.numel()) for on, x in memory.made] == [(STREAM, attention.tree_ws_bytes)]
-    for op in ("fork", "compact"):
+    for op, new in (("fork", 4), ("compact", 1)):
         memory = Memory(monkeypatch, 7)
-        calls(attention)[op](stream=STREAM, out=OUT[op], workspace=None)
-        assert [(on, x.numel()) for on, x in memory.made] == [(STREAM, sc.attention_pages_workspace_bytes(40, 3 if op == "fork" else 0))] and not memory.told
+        for _ in range(2):
+            calls(attention)[op](stream=STREAM, out=OUT[op], workspace=None)
+        made, = memory.made
+        assert made[0] == STREAM and made[1].numel() == sc.attention_pages_workspace_bytes(40, new) and not memory.told
+        assert [call[-3:] for call in recorder.calls[-2:]] == [(made[1].data_ptr(), made[1].numel(), STREAM)] * 2
+        calls(attention)[op](out=OUT[op], workspace=None)          # the current stream: not given away before that is done with it
+        assert len(memory.made) == 1 and memory.told == {made[1].data_ptr(): [7]}
 
 
 def test_calls_are_made_on_the_device_of_the_handle(monkeypatch):
