@@ -87,9 +87,6 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(CopyArgs a, int32_t elem
 // Fork and compact are a few steps over tables, each of which needs the one before it whole.  Small tables: one workgroup takes all steps; others: a kernel for each.
 constexpr int kWide = 1024;   // threads of a workgroup of theirs
 
-// What another workgroup, or an atomic operation of this one, has written.
-__device__ __forceinline__ int32_t fresh(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
 // Sum over the threads of a workgroup, and of those before each.
 template <typename T>
 __device__ __forceinline__ T sum_before(T x, T &all)
@@ -144,7 +141,7 @@ __device__ __forceinline__ void sum_counts(const int32_t *count, int32_t blocks,
 {
     before = all = 0;
     for (int32_t k0 = 0; k0 < blocks; k0 += kWide) {
-        const int32_t k = k0 + (int32_t)threadIdx.x, n = k < blocks ? fresh(count + k) : 0;
+        const int32_t k = k0 + (int32_t)threadIdx.x, n = k < blocks ? count[k] : 0;
         int32_t sum;
         sum_before(k < block ? n : 0, sum);
         before += sum;
@@ -159,7 +156,7 @@ __device__ __forceinline__ void each_page(int32_t block, int32_t pages, const ui
 {
     static_assert(kPagesPerBlock == 64 * 64, "a word for each lane");
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint64_t word = __hip_atomic_load(bits + (int64_t)block * 64 + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint64_t word = bits[(int64_t)block * 64 + lane];
     int32_t upto = __popcll(word);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -262,7 +259,7 @@ __device__ __forceinline__ void fork_hold(const ForkArgs &a, int32_t row, int32_
 // it whole.
 __device__ __forceinline__ void fork_count(const ForkArgs &a, int32_t block)
 {
-    count_block(block, a.pages, a.free_bits, a.free_before, [&](int32_t p) { return fresh(a.holders_out + p) == 0 && fresh(a.keeper + p) == kNone; });
+    count_block(block, a.pages, a.free_bits, a.free_before, [&](int32_t p) { return a.holders_out[p] == 0 && a.keeper[p] == kNone; });
 }
 
 __device__ __forceinline__ void fork_need(const ForkArgs &a)
@@ -274,7 +271,7 @@ __device__ __forceinline__ void fork_need(const ForkArgs &a)
         if (i < a.new_batch) {
             const Branch r = branch_of(a, i);
             const int32_t part = page_in_part(a, r);
-            const bool copied = part >= 0 && !(fresh(a.keeper + part) == i && fresh(a.holders_out + part) == 0);
+            const bool copied = part >= 0 && !(a.keeper[part] == i && a.holders_out[part] == 0);
             if (r.wanted >= 0) mine = (copied ? 1 : 0) + columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
         }
         const int64_t mine_before = sum_before(mine, all);
@@ -284,11 +281,10 @@ __device__ __forceinline__ void fork_need(const ForkArgs &a)
     if (threadIdx.x == 0) a.needed[a.new_batch] = before;
 }
 
-__device__ __forceinline__ int64_t needed(const ForkArgs &a, int32_t i) { return __hip_atomic_load(a.needed + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool served(const ForkArgs &a, int32_t i, int32_t free_all)
 {
-    const int64_t upto = needed(a, i + 1);
-    return upto == needed(a, i) || upto <= free_all;
+    const int64_t upto = a.needed[i + 1];
+    return upto == a.needed[i] || upto <= free_all;
 }
 
 // Fourth step, for kWide sequences from i0 on: lengths, moves, and holders of pages that are kept in part.
@@ -301,7 +297,7 @@ __device__ __forceinline__ void fork_finish(const ForkArgs &a, int32_t i0, int32
         const Branch r = branch_of(a, i);
         const bool is = r.wanted >= 0 && served(a, i, free_all);
         const int32_t part = page_in_part(a, r);
-        const bool copied = is && part >= 0 && needed(a, i + 1) - needed(a, i) > columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
+        const bool copied = is && part >= 0 && a.needed[i + 1] - a.needed[i] > columns_of(r.wanted, a.page_shift) - columns_of(r.kept, a.page_shift);
         a.length_out[i] = is ? r.wanted : -1;
         a.moves[3 * (int64_t)i] = copied ? part : -1;
         if (!copied) a.moves[3 * (int64_t)i + 1] = -1;
@@ -326,7 +322,7 @@ __device__ __forceinline__ void fork_finish(const ForkArgs &a, int32_t i0, int32
 // And for the pages of a block: the n-th free page goes to the sequence that takes it.
 __device__ __forceinline__ void fork_take(const ForkArgs &a, int32_t block, int32_t before, int32_t free_all)
 {
-    const int64_t taken_all = needed(a, a.new_batch);
+    const int64_t taken_all = a.needed[a.new_batch];
     if (before >= taken_all) return;
     each_page(block, a.pages, a.free_bits, before, [&](int32_t p, bool is, int32_t rank) {
         if (!is || rank >= taken_all) return;
@@ -334,13 +330,13 @@ __device__ __forceinline__ void fork_take(const ForkArgs &a, int32_t block, int3
         int32_t lo = 0, hi = a.new_batch;
         while (hi - lo > 1) {
             const int32_t mid = (lo + hi) / 2;
-            if (needed(a, mid) <= rank) lo = mid; else hi = mid;
+            if (a.needed[mid] <= rank) lo = mid; else hi = mid;
         }
         if (!served(a, lo, free_all)) return;
         const Branch r = branch_of(a, lo);
         const int32_t first = columns_of(r.kept, a.page_shift), grown = columns_of(r.wanted, a.page_shift) - first;
-        const int64_t mine = needed(a, lo);
-        const int32_t copied = (int32_t)(needed(a, lo + 1) - mine) - grown, n = (int32_t)(rank - mine);
+        const int64_t mine = a.needed[lo];
+        const int32_t copied = (int32_t)(a.needed[lo + 1] - mine) - grown, n = (int32_t)(rank - mine);
         if (n < copied) a.moves[3 * (int64_t)lo + 1] = p;
         a.page_out[lo * a.page_out_ld + (n < copied ? r.kept >> a.page_shift : first + n - copied)] = p;
         a.holders_out[p] = 1;
@@ -424,9 +420,9 @@ __device__ __forceinline__ int32_t used_below(const CompactArgs &a, int32_t coun
 {
     const int32_t edge = count / kPagesPerBlock, words = count / 64, rest = count % 64;
     int32_t n = 0, all;
-    for (int32_t k = threadIdx.x; k < edge; k += kWide) n += fresh(a.used_before + k);
+    for (int32_t k = threadIdx.x; k < edge; k += kWide) n += a.used_before[k];
     for (int32_t w = edge * 64 + (int32_t)threadIdx.x; w <= words && w * 64 < count; w += kWide) {
-        const uint64_t word = __hip_atomic_load(a.used_bits + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint64_t word = a.used_bits[w];
         n += __popcll(w < words ? word : word & (((uint64_t)1 << rest) - 1));
     }
     sum_before(n, all);
@@ -453,10 +449,10 @@ __device__ __forceinline__ void compact_moves(const CompactArgs &a, int32_t bloc
 // Where page number k of the moves went, and its holders.
 __device__ __forceinline__ void compact_to(const CompactArgs &a, int64_t k)
 {
-    const int32_t from = fresh(a.moves + 3 * k), to = fresh(a.moves + 3 * k + 1);
+    const int32_t from = a.moves[3 * k], to = a.moves[3 * k + 1];
     if (from < 0) return;
     a.to[from] = to;
-    a.holders_out[to] = fresh(a.holders_out + from);
+    a.holders_out[to] = a.holders_out[from];
     a.holders_out[from] = 0;
 }
 
@@ -465,7 +461,7 @@ __device__ __forceinline__ void compact_table(const CompactArgs &a, int32_t b, i
     const int32_t n = a.length[b], used = n > (int64_t)a.columns << a.page_shift ? 0 : columns_of(n, a.page_shift);
     for (int32_t c = c0; c < a.columns; c += step) {
         const int32_t p = a.page[b * a.page_ld + c];
-        a.page_out[b * a.page_out_ld + c] = c < used && (uint32_t)p < (uint32_t)a.pages ? fresh(a.to + p) : p;
+        a.page_out[b * a.page_out_ld + c] = c < used && (uint32_t)p < (uint32_t)a.pages ? a.to[p] : p;
     }
 }
 

@@ -165,7 +165,7 @@ template <typename TR, int DP, bool PAGED, Sees SEES>
 void launch_padded(AttendArgs a, hipStream_t stream)
 {
     if constexpr (TR::kBytes == 2) {
-        constexpr int NW = kPromptWaves<DP>, KT = DP == 256 ? 32 : SEES == kTree ? 64 : 128;
+        constexpr int NW = kPromptWaves<DP>, KT = DP == 256 ? 32 : DP == 128 && SEES != kEverything ? 64 : 128;   // straight to LDS: four buffers of 32 KB
         int heads_log2 = 0;
         while (heads_log2 < 3 && a.group % (2 << heads_log2) == 0 && (2 << heads_log2) <= NW) ++heads_log2;
         const int64_t blocks = a.s.rows / (32 * NW >> heads_log2) + a.s.batch, groups = a.heads >> heads_log2;
@@ -177,12 +177,20 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         // behind up to 8,191 keys, 32, 8, 128: 264 and 320; but 32, 8, 128, 2,048 rows 90 and 73, 4,000 rows 196 and 172, 600 rows 50 and 29.
         int64_t longest = PAGED ? table_room(a.s) : a.s.batch > 1 ? 2 * (int64_t)a.s.rows / a.s.batch : a.s.rows;
         if (SEES == kWindow && longest > (int64_t)a.window + a.sinks + (32 * NW >> heads_log2)) longest = (int64_t)a.window + a.sinks + (32 * NW >> heads_log2);
-        const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / KT;
+        const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / (DP == 256 ? 32 : 128);
         const int shares = prompt_shares(a.n_cu);
-        if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && tiles * shares > kSplitTiles<DP> * shares + 13 * blocks * groups * tiles / 20) {
+        // windows and trees: blocks that have rows, of sequences that are alike
+        int64_t filled = blocks, longest_alone = tiles * shares;
+        if (SEES != kEverything) {
+            const int64_t rows = 32 * NW >> heads_log2;
+            filled = a.s.batch * (((a.s.rows - 1) / a.s.batch) / rows + 1);
+            if (filled * groups > shares) longest_alone = filled * groups < 2 * shares ? 2 * longest_alone : 0;   // a second one on some compute units; more share them out by themselves
+        }
+        if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && longest_alone > kSplitTiles<DP> * shares + 13 * filled * groups * tiles / 20) {
             a.blocks = (int32_t)blocks;
             prompt_tile_kernel<TR, DP, PAGED, true, SEES, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
-            prompt_join_kernel<TR, DP, NW><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
+            if (SEES == kEverything) prompt_join_kernel<TR, DP, NW, DP / 32><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
+            else prompt_join_kernel<TR, DP, NW, 1><<<dim3(shares, NW, DP / 32), 64, 0, stream>>>(a, heads_log2, shares);
             return;
         }
         const auto kernel = prompt_tile_kernel<TR, DP, PAGED, false, SEES, NW, KT>;

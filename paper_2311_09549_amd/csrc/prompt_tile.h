@@ -28,7 +28,7 @@ template <typename TR, int DP, int NW, int KT>
 struct PromptTile {
     static constexpr int THREADS = 64 * NW, CHUNKS = DP / 8, DT = DP / 32, NT = KT / 32;   // pieces of a row, tiles of the head, tiles of keys
     static constexpr int LOADS = KT * CHUNKS / THREADS, ROWS_PER_LOAD = THREADS / CHUNKS;
-    static constexpr int ROW_BYTES = DP * 2, TILE_BYTES = KT * ROW_BYTES, LDS_BYTES = 4 * TILE_BYTES;
+    static constexpr int ROW_BYTES = DP * 2, TILE_BYTES = KT * ROW_BYTES;
     static constexpr float kRaise = 8.0f;
     // A weight's exponent is s scale_log2 - m scale_log2 in one operation, off by roundings of the second product: less than 2^-14 of the weight where that
     // is at most 2^8.  Beyond it, up to products that pass fp32, the difference of the scores is taken first, which is exact where it matters.
@@ -58,6 +58,39 @@ template <int R>
 __device__ __forceinline__ RowBlock row_block_of(const Sequences &s, int32_t number, int heads_log2)
 {
     return heads_log2 == 0 ? row_block<R>(s, number) : heads_log2 == 1 ? row_block<R / 2>(s, number) : heads_log2 == 2 ? row_block<R / 4>(s, number) : row_block<R / 8>(s, number);
+}
+
+// Block number k of those that have rows, of `rows` (a power of two) each: 64 sequences at a time, a lane each.  Numbers without rows in between would leave compute units idle:
+// workgroups go to the shader engines in turn, and of 24 sequences of 63 rows every other number has rows, on every other engine (530 us instead of 290 behind 8,192 keys).
+constexpr int32_t kCountedBatch = 1024;   // more sequences take as many reads one after the other as that is 64s
+
+__device__ __forceinline__ RowBlock row_block_at(const Sequences &s, int32_t k, int32_t rows_log2)
+{
+    for (int32_t c = 0; 64 * c < s.batch; ++c) {
+        const int32_t b = 64 * c + (int32_t)(threadIdx.x % 64);
+        const int32_t begin = b < s.batch ? row_begin(s, b) : 0, end = b < s.batch ? row_begin(s, b + 1) : 0;
+        const int32_t n = end > begin ? ((end - begin - 1) >> rows_log2) + 1 : 0;
+        int32_t upto = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t y = __shfl_up(upto, d);
+            upto += (int32_t)(threadIdx.x % 64) >= d ? y : 0;
+        }
+        const int32_t all = __builtin_amdgcn_readlane(upto, 63);
+        if (k < all) {
+            const int at = __ffsll((unsigned long long)__ballot(upto > k)) - 1;
+            RowBlock r;
+            r.sequence = 64 * c + at;
+            r.begin = __builtin_amdgcn_readlane(begin, at);
+            const int32_t last = __builtin_amdgcn_readlane(end, at);
+            r.count = last - r.begin;
+            r.first = r.begin + ((k - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(n, at)) << rows_log2);
+            r.end = r.first + (1 << rows_log2) < last ? r.first + (1 << rows_log2) : last;
+            return r;
+        }
+        k -= all;
+    }
+    return {-1, 0, 0, 0, 0};
 }
 
 // Keys that row r of a block sees: none but those up to its own position.
@@ -107,7 +140,10 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
     using P = PromptTile<TR, DP, NW, KT>;
     constexpr int CHUNKS = P::CHUNKS, DT = P::DT, NT = P::NT, LOADS = P::LOADS, R = 32 * NW;
     constexpr bool WINDOW = SEES == kWindow, TREE = SEES == kTree;
-    __shared__ __attribute__((aligned(16))) char tile_s[P::LDS_BYTES];   // [buffer][keys, values]
+    // Windows and trees: keys and values go straight to LDS, three tiles ahead, in four buffers.
+    constexpr bool DIRECT = SEES != kEverything;
+    constexpr int BUFFERS = DIRECT ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) char tile_s[BUFFERS * 2 * P::TILE_BYTES];   // [buffer][keys, values]
     __shared__ int32_t parent_s[TREE ? kMaxNodes : 1];
     const int32_t head_groups = a.heads >> heads_log2;
     const auto length_of = [&](const RowBlock &blk) { return TREE ? tree_length(a, blk.sequence, blk.count) : PAGED ? paged_length(a.s, blk.sequence) : blk.count; };
@@ -181,17 +217,6 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         u32x4 ks[LOADS], vs[LOADS];
         // In pages a row's keys and values wait for its page number, within every tile: chunks of four prompts behind up to 8,191 keys take 5.0 us a tile
         // without a split, packed keys 4.1.
-        // Windows and trees: the rows of a load of a wavefront are in one page, whose number is read by the scalar unit a tile ahead.
-        constexpr bool AHEAD = PAGED && SEES != kEverything;
-        static_assert(64 / CHUNKS <= 16, "in one page");
-        int32_t page_next[LOADS];
-        const auto find_pages = [&](int32_t base) {
-#pragma unroll
-            for (int n = 0; n < LOADS; ++n) {
-                const int32_t key = base + wave * (64 / CHUNKS) + n * P::ROWS_PER_LOAD;
-                if (AHEAD) page_next[n] = page_of_all(a.s, blk.sequence, key < length ? key : length - 1);
-            }
-        };
         const auto fetch = [&](int32_t base) {
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) {
@@ -199,8 +224,8 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 key = key < length ? key : length - 1;   // rows behind the last key are seen by none: any that are there
                 int64_t k_at = key * k_row, v_at = key * v_row;
                 if (PAGED) {
-                    int32_t page = AHEAD ? page_next[n] : page_of(a.s, blk.sequence, key);
-                    bad |= page < 0 && (!WINDOW || key >= line.low || key < a.sinks);   // pages behind every row's window may be gone
+                    int32_t page = page_of(a.s, blk.sequence, key);
+                    bad |= page < 0;
                     if (page < 0) page = 0;
                     k_at = v_at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row) * 2;
                 }
@@ -227,6 +252,65 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
                 }
                 *reinterpret_cast<u32x4 *>(buffer + r * P::ROW_BYTES + 16 * P::key_piece(r, piece)) = ks[n];
                 *reinterpret_cast<u32x4 *>(buffer + P::TILE_BYTES + r * P::ROW_BYTES + 16 * P::value_piece(r, piece)) = vs[n];
+            }
+            return any != 0;
+        };
+        // Straight to LDS: a load of a wavefront fills 64 pieces in a row, whole rows, and its lanes ask for the pieces that belong there.  The rows of a load are in one page, whose
+        // number is read by the scalar unit a tile ahead.  Pieces behind the head are 0 from the start and stay so.
+        constexpr int LOAD_ROWS = 64 / CHUNKS;
+        static_assert(LOAD_ROWS <= 16, "in one page");
+        const uint32_t tile_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile_s;
+        int32_t page_next[LOADS];
+        const auto find_pages = [&](int32_t base) {
+            if constexpr (PAGED && DIRECT) {
+#pragma unroll
+                for (int n = 0; n < LOADS; ++n) {
+                    const int32_t key = base + wave * LOAD_ROWS + n * P::ROWS_PER_LOAD;
+                    page_next[n] = page_of_all(a.s, blk.sequence, key < length ? key : length - 1);
+                }
+            }
+        };
+        const auto to_lds = [](uint32_t at, const char *p) {
+            // nothing else in these kernels uses m0
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
+        };
+        const auto load_tile = [&](int32_t base, int buffer) {
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                const int r = wave * LOAD_ROWS + n * P::ROWS_PER_LOAD + lane / CHUNKS;
+                const int32_t key = base + r < length ? base + r : length - 1;   // rows behind the last key are seen by none: any that are there
+                const char *k, *v;
+                if constexpr (PAGED) {
+                    const int32_t page = page_next[n] < 0 ? 0 : page_next[n];
+                    bad |= page_next[n] < 0 && (!WINDOW || key >= line.low || key < a.sinks);   // pages behind every row's window may be gone
+                    const int64_t at = (page * a.cache.page + (key & ((1 << a.s.page_shift) - 1)) * a.cache.row + kv * a.cache.head) * 2;
+                    k = static_cast<const char *>(a.cache.keys) + at;
+                    v = static_cast<const char *>(a.cache.values) + at;
+                } else {
+                    k = static_cast<const char *>(a.k.data) + ((blk.begin + key) * a.k.row + kv * a.k.head) * 2;
+                    v = static_cast<const char *>(a.v.data) + ((blk.begin + key) * a.v.row + kv * a.v.head) * 2;
+                }
+                const uint32_t at = tile_at + buffer * 2 * P::TILE_BYTES + (wave * LOAD_ROWS + n * P::ROWS_PER_LOAD) * P::ROW_BYTES;
+                const int kc = P::key_piece(r, lane % CHUNKS), vc = P::value_piece(r, lane % CHUNKS);   // exchanges are their own inverse
+                if (kc * 8 < a.head_dim) to_lds(at, k + 16 * kc);
+                if (vc * 8 < a.head_dim) to_lds(at + P::TILE_BYTES, v + 16 * vc);
+            }
+        };
+        // Of a tile that some rows see in part: infinities and NaN among the values that this lane has loaded become 0; whether there were any.
+        const auto clean = [&](int buffer) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                u32x4 *p = reinterpret_cast<u32x4 *>(tile_s + (2 * buffer + 1) * P::TILE_BYTES + (wave * LOAD_ROWS + n * P::ROWS_PER_LOAD) * P::ROW_BYTES + 16 * lane);
+                u32x4 x = *p;
+                uint32_t here = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    here |= Special<TR>::infinite_or_nan(x[i]);
+                    x[i] = Special<TR>::without(x[i]);
+                }
+                if (here) *p = x;
+                any |= here;
             }
             return any != 0;
         };
@@ -351,54 +435,91 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             // whether every row of the block sees the whole tile of keys from `key` on
             const auto whole = [&](int32_t key) { return key + KT <= block_all && (!WINDOW || key >= line.last_low || key + KT <= a.sinks); };
             int32_t place = SPLIT ? first_tile * KT : 0;
-            find_pages(key_of(place));
-            fetch(key_of(place));
-            find_pages(key_of(place + KT));
-            bool special = __syncthreads_or(put(tile_s, !whole(key_of(place))));
-            int buffer = 0;
-            const auto pass = [&](auto masked) {
-                constexpr bool MASK = decltype(masked)::value;
-                const int32_t base = key_of(place);
-                const bool more = place + KT < block_most, part = (MASK && SEES == kEverything) || !whole(key_of(place + KT));
-                if (more) {
-                    fetch(key_of(place + KT));
-                    find_pages(key_of(place + 2 * KT));
+            // Keys of the row's chain among those of a tile: bits of the keys before the tree (or, of rows in order, up to the row), then of nodes.
+            const auto chain = [&](int32_t base, uint32_t (&seen)[NT]) {
+                const int32_t n = (a.parent ? before : before + node + 1) - base;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) seen[t] = node < 0 || n <= 32 * t ? 0u : n >= 32 * t + 32 ? ~0u : (1u << (n - 32 * t)) - 1;
+                const int32_t first_node = base - before;
+                for (int32_t i = chains ? node : -1; __any(i >= 0 && i >= first_node);) {
+                    const int32_t bit = i - first_node, p = parent_s[i < 0 ? 0 : i];
+                    const uint32_t one = i >= 0 && bit >= 0 && bit < KT ? 1u << (bit & 31) : 0u;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) seen[t] |= bit >> 5 == t ? one : 0u;
+                    i = i < 0 ? -1 : p;
                 }
-                if ((!MASK && (!TREE || first < blk.end)) || (MASK && base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
-                    uint32_t seen[NT] = {}, mine_of[NT];
-                    if constexpr (MASK && TREE) {
-                        // bits of the keys before the tree (or, of rows in order, up to the row), then of the row's chain
-                        const int32_t n = (a.parent ? before : before + node + 1) - base;
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) seen[t] = node < 0 || n <= 32 * t ? 0u : n >= 32 * t + 32 ? ~0u : (1u << (n - 32 * t)) - 1;
-                        const int32_t first_node = base - before;
-                        for (int32_t i = chains ? node : -1; __any(i >= 0 && i >= first_node);) {
-                            const int32_t bit = i - first_node, p = parent_s[i < 0 ? 0 : i];
-                            const uint32_t one = i >= 0 && bit >= 0 && bit < KT ? 1u << (bit & 31) : 0u;
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) seen[t] |= bit >> 5 == t ? one : 0u;
-                            i = i < 0 ? -1 : p;
-                        }
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mine_of[t] = seen[t] >> 4 * half;
-                    }
-                    tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked, mine_of);
-                    if (MASK && special) add_special(base, seen);
-                }
-                buffer ^= 1;
-                bool any = false;
-                if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
-                if (part) special = __syncthreads_or(any);
-                else __syncthreads();
-                place += KT;
             };
-            if constexpr (WINDOW) {
-                // edges of the window and of the first keys, and what every row of the block sees whole, in turn
-                while (place < block_most) {
-                    while (place < block_most && !whole(key_of(place))) pass(std::true_type());
-                    while (place < block_most && whole(key_of(place))) pass(std::false_type());
+            if constexpr (DIRECT) {
+                constexpr int PER = 2 * LOADS;   // loads of a wavefront for a tile
+                int32_t ahead = place;           // what has been asked for
+                int buffer = 0;
+                // queries have arrived: a wait for them within the loop would be one for the loads on their way
+#pragma unroll
+                for (int c = 0; c < DP / 16; ++c) asm volatile("" : "+v"(qf[c]));
+                __syncthreads();   // the buffers are done with
+                find_pages(key_of(ahead));
+                const auto more = [&](int to) {
+                    if (ahead >= block_most) return;
+                    load_tile(key_of(ahead), to);
+                    ahead += KT;
+                    find_pages(key_of(ahead));
+                };
+#pragma unroll
+                for (int n = 0; n < BUFFERS - 1; ++n) more(n);
+                const auto pass = [&](auto masked) {
+                    constexpr bool MASK = decltype(masked)::value;
+                    const int32_t base = key_of(place);
+                    // this tile has arrived, the two behind it may be on their way
+                    if (ahead - place > 2 * KT) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * PER) : "memory");
+                    else if (ahead - place > KT) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    bool special = false;
+                    if (MASK) special = __syncthreads_or(clean(buffer));
+                    else __syncthreads();
+                    more((buffer + BUFFERS - 1) % BUFFERS);   // every wavefront is done with the tile before this one
+                    if ((!MASK && (!TREE || first < blk.end)) || (MASK && base < most && (!WINDOW || base + KT > least || base < a.sinks))) {
+                        uint32_t seen[NT] = {}, mine_of[NT];
+                        if constexpr (MASK && TREE) {
+                            chain(base, seen);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mine_of[t] = seen[t] >> 4 * half;
+                        }
+                        tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, base, masked, mine_of);
+                        if (MASK && special) add_special(base, seen);
+                    }
+                    buffer = (buffer + 1) % BUFFERS;
+                    place += KT;
+                };
+                // edges of windows and first keys, and what every row of the block sees whole, in turn; of trees first what is before them
+                if constexpr (WINDOW) {
+                    while (place < block_most) {
+                        while (place < block_most && !whole(key_of(place))) pass(std::true_type());
+                        while (place < block_most && whole(key_of(place))) pass(std::false_type());
+                    }
+                } else {
+                    while (place < block_most && whole(place)) pass(std::false_type());
+                    while (place < block_most) pass(std::true_type());
                 }
             } else {
+                fetch(place);
+                bool special = __syncthreads_or(put(tile_s, place + KT > block_all));
+                int buffer = 0;
+                const auto pass = [&](auto masked) {
+                    constexpr bool MASK = decltype(masked)::value;
+                    const bool more = place + KT < block_most, part = MASK || place + 2 * KT > block_all;
+                    if (more) fetch(place + KT);
+                    if (!MASK || place < most) {
+                        const uint32_t seen[NT] = {};
+                        tile((Lds)tile_s + buffer * 2 * P::TILE_BYTES, place, masked, seen);
+                        if (MASK && special) add_special(place, seen);
+                    }
+                    buffer ^= 1;
+                    bool any = false;
+                    if (more) any = put(tile_s + buffer * 2 * P::TILE_BYTES, part);
+                    if (part) special = __syncthreads_or(any);
+                    else __syncthreads();
+                    place += KT;
+                };
                 // tiles that every row of the block sees whole, then the others
                 while (place + KT <= block_all && (!SPLIT || place < block_most)) pass(std::false_type());
                 while (place < block_most) pass(std::true_type());
@@ -431,10 +552,16 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
         }
     };
 
+    if (DIRECT && a.head_dim < DP)
+        for (int x = threadIdx.x; x < (int)sizeof(tile_s) / 16; x += P::THREADS) reinterpret_cast<u32x4 *>(tile_s)[x] = u32x4{0, 0, 0, 0};
+
     if constexpr (!SPLIT) {
         // Blocks of a key head follow each other at a distance that is a multiple of the number of its XCD, where that is one, and share that
         // one's L2; the last rows of a sequence, which see most keys, come first.
-        const RowBlock blk = row_block_of<R>(a.s, a.blocks - 1 - (int32_t)(blockIdx.x / head_groups), heads_log2);
+        const int32_t number = a.blocks - 1 - (int32_t)(blockIdx.x / head_groups);
+        RowBlock blk;
+        if (DIRECT && a.s.batch <= kCountedBatch) blk = row_block_at(a.s, number, (R == 256 ? 8 : 7) - heads_log2);
+        else blk = row_block_of<R>(a.s, number, heads_log2);
         if (blk.sequence >= 0) work(blk, blockIdx.x % head_groups, 0, 0, nullptr);
     } else {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -445,7 +572,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             return n <= KT ? 1 : (n - 1) / KT + 1;
         };
         // In the line a block's tiles lie behind kBegin places that stand for its start and end, which cost about as much as they.
-        constexpr int kBegin = 2;
+        constexpr int kBegin = DP == 128 && DIRECT ? 4 : 2;
         __shared__ int64_t upto_s[kSplitBlocks + 1], wave_s[NW];
         constexpr int EACH = kSplitBlocks / (64 * NW);
         int32_t places[EACH];
@@ -518,12 +645,13 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
     }
 }
 
-// Joins the pieces of the block that begins in share blockIdx.x and goes on behind it, in the order of the shares; a wavefront has the 32 rows of one of the first kernel's.
-template <typename TR, int DP, int NW>
+// Joins the pieces of the block that begins in share blockIdx.x and goes on behind it, in the order of the shares; a wavefront has the 32 rows of one of the first kernel's, and DT tiles
+// of 32 elements of their head: one of them, where one long sequence has many pieces (33 of them 80 us with four, 35 with one).
+template <typename TR, int DP, int NW, int DT>
 __global__ void __launch_bounds__(64) prompt_join_kernel(AttendArgs a, int heads_log2, int32_t shares)
 {
-    constexpr int DT = DP / 32;
-    const int32_t w = blockIdx.x, wave = blockIdx.y;
+    constexpr int UNROLL = DT == 1 ? 4 : 1;
+    const int32_t w = blockIdx.x, wave = blockIdx.y, tile0 = blockIdx.z * DT;
     const int lane = threadIdx.x;
     const int32_t id = a.cut[2 * w + 1];
     if (id < 0 || a.cut[2 * w] == id) return;
@@ -547,20 +675,21 @@ __global__ void __launch_bounds__(64) prompt_join_kernel(AttendArgs a, int heads
     float l = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4 * DT; ++i) o[i] = f32x4{0, 0, 0, 0};
+#pragma unroll UNROLL
     for (int32_t n = 0; n <= more; ++n) {
         const float *p = piece(n);
         const float m = p[32 * DP + lane], part = p[32 * DP + 64 + lane];
         const float factor = __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
         l += part * factor;
 #pragma unroll
-        for (int i = 0; i < 4 * DT; ++i) o[i] += reinterpret_cast<const f32x4 *>(p)[i * 64 + lane] * factor;
+        for (int i = 0; i < 4 * DT; ++i) o[i] += reinterpret_cast<const f32x4 *>(p)[(4 * tile0 + i) * 64 + lane] * factor;
     }
     const float factor = l == 0.0f ? 0.0f : 1.0f / l;
     if (row >= blk.end) return;
     char *out = static_cast<char *>(a.out.data) + (row * a.out.row + head * a.out.head) * 2;
 #pragma unroll
     for (int i = 0; i < 4 * DT; ++i) {
-        const int e = 8 * i + 4 * (lane / 32);
+        const int e = 32 * tile0 + 8 * i + 4 * (lane / 32);
         if (e < a.head_dim) *reinterpret_cast<u32x2 *>(out + 2 * e) = u32x2{TR::pack(o[i].x * factor, o[i].y * factor), TR::pack(o[i].z * factor, o[i].w * factor)};
     }
 }
