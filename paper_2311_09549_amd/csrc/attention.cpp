@@ -103,6 +103,7 @@ AttendArgs attend_args(const sc_attention *at)
     a.causal = at->causal;
     a.scale_log2 = at->scale_log2;
     a.groups_log2 = at->groups_log2;
+    a.n_cu = at->n_cu;
     a.window = at->window;
     a.sinks = at->sinks;
     return a;
@@ -110,7 +111,6 @@ AttendArgs attend_args(const sc_attention *at)
 
 sc_status prompt_workspace_of(const sc_attention *at, void *workspace, size_t bytes, AttendArgs &a)
 {
-    a.n_cu = at->n_cu;
     if (!workspace || !at->prompt_ws_bytes) return SC_OK;
     if (bytes < at->prompt_ws_bytes) return SC_ERR_WORKSPACE_SMALL;
     if ((uintptr_t)workspace % 256) return SC_ERR_SHAPE_MISMATCH;
@@ -406,7 +406,6 @@ extern "C" sc_status sc_attention_tree(const sc_attention *at, const sc_sequence
     a.tree = 1;
     a.parent = parent;
     a.causal = 1;
-    a.n_cu = at->n_cu;
     if (!tree_line_ok(a)) return SC_ERR_BAD_DIMS;
     if (!at->has_device) return SC_ERR_DEVICE;
     a.pieces = static_cast<float *>(workspace);

@@ -535,14 +535,32 @@ void launch_pairs(const AttendArgs &a, hipStream_t stream)
     tree_join_kernel<TR, DP, RT><<<dim3(1 << groups_log2, 4 * RT), 256, 0, stream>>>(a, groups_log2);
 }
 
+// Keys that a sequence may have to read: all that the table has room for, or that a window has (and the rows of a tree behind it).
+int64_t room_of(const AttendArgs &a)
+{
+    const int64_t room = table_room(a.s), through = (int64_t)a.window + a.sinks + 32 + a.s.rows;
+    return a.window && through < room ? through : room;
+}
+
+int64_t whole_tiles(const AttendArgs &a) { return (int64_t)a.s.rows * a.group / kHeadTile + a.s.batch; }
+
+// Whether the keys of a tile are shared by the wavefronts of a workgroup, through LDS (prompt_tile.h), by the pairs of a sequence and a key head on average.  bf16, 32 heads of 128 on 8,
+// us there and here: 24 sequences of 640 keys, 4 rows 24.5 and 26.3, 8 rows 24 and 39, 16 rows 25 and 46; of 2,560 keys 64, 64 and 66 beside 54, 63 and 77; of 8,192
+// keys 207, 207 and 213 beside 172, 189 and 185; 24 rows 216 there.  One sequence of 32,768 keys, 16 rows: 81 and 60.  320 keys, by tree_whole_kernel: 8 sequences of 16 rows 17 and
+// 13, 24 of 8 rows 16 and 21.
+bool through_lds(const AttendArgs &a, sc_dtype dtype)
+{
+    if (!a.tree || a.window || dtype == SC_F32) return false;
+    const int64_t pairs = (int64_t)a.s.rows * a.group / a.s.batch, room = room_of(a);
+    if (room <= kWholeKeys) return pairs >= 16 && whole_tiles(a) * a.kv_heads > a.n_cu;
+    return pairs >= 96 || (pairs > 16 && room <= 4096 && (int64_t)a.s.batch * a.kv_heads >= a.n_cu / 2);
+}
+
 template <typename TR, int DP, bool EXACT>
 void launch_exact(const AttendArgs &a, hipStream_t stream)
 {
-    // Few keys: all that the table has room for, or that a window has (and the rows of a tree behind it).
-    int64_t room = table_room(a.s);
-    if (a.window && room > (int64_t)a.window + a.sinks + 32 + a.s.rows) room = (int64_t)a.window + a.sinks + 32 + a.s.rows;
-    const int64_t tiles = (int64_t)a.s.rows * a.group / kHeadTile + a.s.batch;
-    if (room <= kWholeKeys && tiles * a.kv_heads < 1 << 22) {
+    const int64_t tiles = whole_tiles(a);
+    if (room_of(a) <= kWholeKeys && tiles * a.kv_heads < 1 << 22) {
         tree_whole_kernel<TR, DP, EXACT><<<(uint32_t)(tiles * a.kv_heads), 64 * kWholeWaves<DP>, 0, stream>>>(a);
         return;
     }
@@ -576,9 +594,6 @@ void launch_typed(const AttendArgs &a, hipStream_t stream)
 
 }  // namespace
 
-// Pairs of a sequence and a key head, on average, from which on the keys of a tile are shared by the wavefronts of a workgroup, through LDS (prompt_tile.h).
-constexpr int64_t kManyPairs = 96;
-
 size_t row_pieces(int head_dim, int groups_log2) { return sizeof(float) * 2 * ((size_t)1 << groups_log2) * piece_floats(padded_dim(head_dim)); }
 
 // Four tiles of pairs: of heads of 128 for half as many workgroups.
@@ -590,7 +605,7 @@ size_t tree_pieces(int head_dim, int groups_log2)
 
 hipError_t launch_tree(const AttendArgs &a, sc_dtype dtype, hipStream_t stream)
 {
-    if (a.tree && !a.window && dtype != SC_F32 && (int64_t)a.s.rows * a.group >= kManyPairs * a.s.batch) return launch_prompt_tree(a, dtype, stream);
+    if (through_lds(a, dtype)) return launch_prompt_tree(a, dtype, stream);
     if (dtype == SC_BF16) launch_typed<Bf16>(a, stream);
     else if (dtype == SC_F16) launch_typed<F16>(a, stream);
     else launch_typed<F32>(a, stream);

@@ -186,7 +186,9 @@ void launch_padded(AttendArgs a, hipStream_t stream)
             filled = a.s.batch * (((a.s.rows - 1) / a.s.batch) / rows + 1);
             if (filled * groups > shares) longest_alone = filled * groups < 2 * shares ? 2 * longest_alone : 0;   // a second one on some compute units; more share them out by themselves
         }
-        if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && longest_alone > kSplitTiles<DP> * shares + 13 * filled * groups * tiles / 20) {
+        // (their mean is taken as three quarters of the longest)
+        const int64_t shared = SEES == kEverything ? 13 * filled * groups * tiles / 20 : filled * groups * tiles;
+        if (a.pieces && blocks <= kSplitBlocks && tiles > 4 && longest_alone > kSplitTiles<DP> * shares + shared) {
             a.blocks = (int32_t)blocks;
             prompt_tile_kernel<TR, DP, PAGED, true, SEES, NW, KT><<<shares, 64 * NW, 0, stream>>>(a, heads_log2);
             if (SEES == kEverything) prompt_join_kernel<TR, DP, NW, DP / 32><<<dim3(shares, NW), 64, 0, stream>>>(a, heads_log2, shares);
