@@ -55,12 +55,13 @@ SHAPES = [
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("heads,kv_heads,head_dim,page_rows,lengths,nodes,spread,heads_first", SHAPES)
 @pytest.mark.parametrize("window,sinks", [(None, 0), (19, 3)])
-def test_tree(dtype, heads, kv_heads, head_dim, page_rows, lengths, nodes, spread, heads_first, window, sinks):
+@pytest.mark.parametrize("more_columns", [1, 2000])      # a table with room for many more keys takes other kernels
+def test_tree(dtype, heads, kv_heads, head_dim, page_rows, lengths, nodes, spread, heads_first, window, sinks, more_columns):
     gen = torch.Generator().manual_seed(sum(lengths) + head_dim)
     keys, values = ([normal(gen, n, kv_heads, head_dim, dtype=dtype) for n in lengths] for _ in range(2))
     q = normal(gen, sum(nodes), heads, head_dim, dtype=dtype)
     trees = [random_tree(n, spread, gen) for n in nodes]
-    columns = -(-max(lengths) // page_rows) + 1
+    columns = -(-max(lengths) // page_rows) + more_columns
     kc, vc, table = cache_of(keys, values, page_rows, columns, gen, heads_first)
     attention = Attention(heads, kv_heads, head_dim, dtype, page_rows, window=window, sinks=sinks)
     workspace = torch.full((attention.tree_ws_bytes // 4,), NAN, device="cuda")   # its contents do not matter
@@ -72,6 +73,67 @@ def test_tree(dtype, heads, kv_heads, head_dim, page_rows, lengths, nodes, sprea
         want, bound = attend_seen(q[at:at + n], keys[b], values[b], tree_mask(trees[b], lengths[b], window, sinks)[0], 1 / math.sqrt(head_dim), dtype)
         assert_within(got[at:at + n], want, bound, f"tree {b}")
         at += n
+
+
+LONG = [
+    # heads, kv_heads, head_dim, lengths, nodes, window, sinks
+    (4, 2, 128, [3000, 700, 1, 513], [5, 4, 1, 6], None, 0),          # one tile of pairs
+    (4, 2, 128, [3000, 700, 12, 513], [12, 9, 12, 16], None, 0),      # two
+    (8, 2, 128, [3000, 700, 12, 513], [12, 9, 12, 16], None, 0),      # four
+    (8, 2, 64, [3000, 700, 12, 513], [12, 9, 12, 16], None, 0),
+    (4, 4, 104, [2000, 900], [40, 33], None, 0),
+    (3, 1, 256, [2000, 900], [7, 30], None, 0),
+    (8, 1, 128, [6000], [64], None, 0),                               # tiles through LDS, keys split
+    (8, 1, 64, [6000], [70], None, 0),
+    (2, 1, 256, [2500, 1000], [100, 70], None, 0),
+    (16, 2, 72, [4000, 900, 50], [130, 20, 50], None, 0),
+    (4, 2, 128, [3000, 700, 12, 513], [12, 9, 12, 16], 600, 40),      # a window whose edge is far from the tree
+    (8, 2, 64, [3000, 700, 12, 513], [12, 9, 12, 16], 640, 0),
+    (8, 1, 128, [6000], [64], 2000, 130),
+    (3, 1, 256, [2000, 900], [7, 30], 555, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv_heads,head_dim,lengths,nodes,window,sinks", LONG)
+def test_tree_behind_many_keys(dtype, heads, kv_heads, head_dim, lengths, nodes, window, sinks):
+    gen = torch.Generator().manual_seed(sum(lengths) + head_dim)
+    keys, values = ([normal(gen, n, kv_heads, head_dim, dtype=dtype) for n in lengths] for _ in range(2))
+    q = normal(gen, sum(nodes), heads, head_dim, dtype=dtype)
+    trees = [random_tree(n, 5, gen) for n in nodes]
+    kc, vc, table = cache_of(keys, values, 32, -(-max(lengths) // 32), gen)
+    for b, n in enumerate(lengths):        # pages that no node sees are given back
+        for c in range(table.shape[1]):
+            if window is not None and c * 32 >= sinks and (c + 1) * 32 <= n - nodes[b] - window + 1:
+                table[b, c] = -1
+    attention = Attention(heads, kv_heads, head_dim, dtype, 32, window=window, sinks=sinks)
+    args = (q.cuda(), kc, vc, table, int32(lengths), int32(starts(nodes)), int32(flat(trees)))
+    got = attention.tree(*args)
+    assert torch.equal(got, attention.tree(*args))
+    got, at = got.cpu(), 0
+    for b, n in enumerate(nodes):
+        want, bound = attend_seen(q[at:at + n], keys[b], values[b], tree_mask(trees[b], lengths[b], window, sinks)[0], 1 / math.sqrt(head_dim), dtype)
+        assert_within(got[at:at + n], want, bound, f"tree {b}")
+        at += n
+
+
+def test_blocks_of_many_sequences():
+    """More sequences than are counted to find a block, with and without rows; blocks of one sequence one behind the other."""
+    gen = torch.Generator().manual_seed(6)
+    lengths = [int(x) for x in torch.randint(1, 90, (1100,), generator=gen)]
+    nodes = [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 60, (1100,), generator=gen))]
+    for count in (1100, 130):
+        keys, values = ([normal(gen, n, 1, 64, dtype=BF16) for n in lengths[:count]] for _ in range(2))
+        q = normal(gen, sum(nodes[:count]), 8, 64, dtype=BF16)
+        trees = [random_tree(n, 3, gen) for n in nodes[:count]]
+        kc, vc, table = cache_of(keys, values, 16, 40, gen)
+        got = Attention(8, 1, 64, BF16, 16).tree(q.cuda(), kc, vc, table, int32(lengths[:count]), int32(starts(nodes[:count])), int32(flat(trees))).cpu()
+        at = 0
+        for b, n in enumerate(nodes[:count]):
+            if n and (b % 7 == 0 or n > 50):
+                want, bound = attend_seen(q[at:at + n], keys[b], values[b], tree_mask(trees[b], lengths[b])[0], 1 / 8, BF16)
+                assert_within(got[at:at + n], want, bound, f"tree {b}")
+            at += n
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -117,18 +179,19 @@ def test_many_sequences(dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("head_dim", [64, 128, 256])
 @pytest.mark.parametrize("bad", [NAN, INF, -INF])
-def test_other_branches_reach_nothing(dtype, head_dim, bad):
+@pytest.mark.parametrize("heads,columns", [(2, 3), (1, 100), (2, 100), (8, 100)])      # by each kind of kernel
+def test_other_branches_reach_nothing(dtype, head_dim, bad, heads, columns):
     """Two branches: what one of them holds reaches its own nodes alone; rows behind the length hold the same."""
     gen = torch.Generator().manual_seed(head_dim)
     n, nodes = 75, 40
-    k, v, q = normal(gen, n, 1, head_dim, dtype=dtype), normal(gen, n, 1, head_dim, dtype=dtype), normal(gen, nodes, 2, head_dim, dtype=dtype)
+    k, v, q = normal(gen, n, 1, head_dim, dtype=dtype), normal(gen, n, 1, head_dim, dtype=dtype), normal(gen, nodes, heads, head_dim, dtype=dtype)
     tree = [-1, -1] + [i - 2 for i in range(2, nodes)]       # even nodes one branch, odd nodes the other
     seen, _ = tree_mask(tree, n)
     bad_k, bad_v = k.clone(), v.clone()
     for x in (bad_k, bad_v):
         x[n - nodes + 1::2] = bad
-    kc, vc, table = cache_of([bad_k], [bad_v], 64, 3, gen, fill=bad)
-    got = Attention(2, 1, head_dim, dtype, 64).tree(q.cuda(), kc, vc, table, int32([n]), int32([0, nodes]), int32(tree)).cpu()
+    kc, vc, table = cache_of([bad_k], [bad_v], 64, columns, gen, fill=bad)
+    got = Attention(heads, 1, head_dim, dtype, 64).tree(q.cuda(), kc, vc, table, int32([n]), int32([0, nodes]), int32(tree)).cpu()
     want, bound = attend_seen(q, k, v, seen, 1 / math.sqrt(head_dim), dtype)
     assert_within(got[::2], want[::2], bound[::2])
     if math.isnan(bad):
@@ -138,37 +201,39 @@ def test_other_branches_reach_nothing(dtype, head_dim, bad):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_lowest_scores(dtype):
+@pytest.mark.parametrize("heads,columns", [(1, 2), (1, 100), (32, 100)])
+def test_lowest_scores(dtype, heads, columns):
     """Scores of the type's lowest value are scores like others; nodes whose scores are all -infinity give +0."""
     d, n = 64, 20
-    q, k, v = torch.zeros(4, 1, d, dtype=dtype), torch.zeros(n, 1, d, dtype=dtype), torch.ones(n, 1, d, dtype=dtype)
+    q, k, v = torch.zeros(4, heads, d, dtype=dtype), torch.zeros(n, 1, d, dtype=dtype), torch.ones(n, 1, d, dtype=dtype)
     q[..., 0] = 1.0
     gen = torch.Generator().manual_seed(1)
     for low, value in ((torch.finfo(dtype).min, 1.0), (-INF, 0.0)):
         k[:, 0, 0] = low
-        kc, vc, table = cache_of([k], [v], 16, 2, gen)
-        got = Attention(1, 1, d, dtype, 16, scale=1.0).tree(q.cuda(), kc, vc, table, int32([n]), int32([0, 4]), int32([-1, 0, 0, -1])).cpu()
+        kc, vc, table = cache_of([k], [v], 16, columns, gen)
+        got = Attention(heads, 1, d, dtype, 16, scale=1.0).tree(q.cuda(), kc, vc, table, int32([n]), int32([0, 4]), int32([-1, 0, 0, -1])).cpu()
         assert bool((got == value).all()) and not bool(torch.signbit(got).any())
 
 
-def test_wrong_tables():
+@pytest.mark.parametrize("heads,columns", [(4, 7), (4, 100), (64, 100)])
+def test_wrong_tables(heads, columns):
     """Wrong lengths, pages and parents make NaN of the rows that they concern and leave the others as they are."""
     gen = torch.Generator().manual_seed(7)
     n, nodes = 100, 6
     count = 9
     keys, values = ([normal(gen, n, 2, 64, dtype=BF16) for _ in range(count)] for _ in range(2))
-    q = normal(gen, count * nodes, 4, 64, dtype=BF16)
+    q = normal(gen, count * nodes, heads, 64, dtype=BF16)
     tree = [-1, 0, 0, 1, 1, 4]
     trees = [list(tree) for _ in range(count)]
     trees[5][2] = 2          # itself: node 2 alone, which nobody follows
     trees[6][1] = -2         # nodes 1, 3, 4, 5
     trees[7][4] = 5          # a later one: nodes 4 and 5
     trees[8][5] = 2 ** 31 - 1
-    kc, vc, table = cache_of(keys, values, 16, 7, gen)
+    kc, vc, table = cache_of(keys, values, 16, columns, gen)
     table[1, 3] = -1
     table[2, 6] = kc.shape[0]
     lengths = int32([n, n, n, -1, nodes - 1, n, n, n, n])
-    got = Attention(4, 2, 64, BF16, 16).tree(q.cuda(), kc, vc, table, lengths, int32(starts([nodes] * count)), int32(flat(trees))).cpu()
+    got = Attention(heads, 2, 64, BF16, 16).tree(q.cuda(), kc, vc, table, lengths, int32(starts([nodes] * count)), int32(flat(trees))).cpu()
     wrong = {0: [], 1: range(6), 2: range(2, 6), 3: range(6), 4: range(6), 5: [2], 6: [1, 3, 4, 5], 7: [4, 5], 8: [5]}
     for b in range(count):
         want, bound = attend_seen(q[b * nodes:(b + 1) * nodes], keys[b], values[b], tree_mask(tree, n)[0], 1 / 8, BF16)
@@ -200,13 +265,16 @@ def test_wrong_row_starts():
     gen = torch.Generator().manual_seed(12)
     k, v, q = normal(gen, 100, 1, 64, dtype=BF16), normal(gen, 100, 1, 64, dtype=BF16), normal(gen, 40, 1, 64, dtype=BF16)
     kc, vc, table = cache_of([k] * 3, [v] * 3, 16, 7, gen)
-    attention = Attention(1, 1, 64, BF16, 16)
     tree = random_tree(40, 4, gen)
     want, bound = attend_seen(q[:10], k, v, tree_mask(tree[:10], 100)[0], 1 / 8, BF16)
+    wide = torch.full((3, 200), -1, dtype=torch.int32, device="cuda")
+    wide[:, :7] = table
+    many = q.repeat(1, 16, 1)
     for row_start in ([0, 10, -7, 40], [0, 10, 500, 2 ** 31 - 1], [-9, 10, 10, 8], [40, 0, 0, 0]):
-        out = attention.tree(q.cuda(), kc, vc, table, int32([100] * 3), int32(row_start), int32(tree), out=torch.zeros(40, 1, 64, dtype=BF16, device="cuda")).cpu()
-        if row_start[0] <= 0 and row_start[2] != -7:
-            assert_within(out[:8], want[:8], bound[:8])
+        for heads, pages, rows in ((1, table, q), (1, wide, q), (16, wide, many)):      # by each kind of kernel
+            out = Attention(heads, 1, 64, BF16, 16).tree(rows.cuda(), kc, vc, pages, int32([100] * 3), int32(row_start), int32(tree), out=torch.zeros_like(rows).cuda()).cpu()
+            if row_start[0] <= 0 and row_start[2] != -7:
+                assert_within(out[:8], want[:8].expand(8, heads, 64), bound[:8].expand(8, heads, 64))
 
 
 def test_cache_beyond_32_bits():

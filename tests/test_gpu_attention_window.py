@@ -132,6 +132,8 @@ def test_prompt_paged(dtype, heads, kv_heads, head_dim, page_rows, lengths, rows
     (2, 2, 136, 16, [90, 900], 700, 0, False),
     (2, 1, 8, 16, [140], 10, 3, False),
     (4, 1, 128, 128, [9000], 4000, 4, False),            # one long sequence, split over many workgroups
+    (20, 1, 64, 64, [3000, 40, 0, 1500], 1000, 100, False),
+    (2, 1, 256, 16, [2000, 5], 900, 33, True),
     (4, 1, 128, 16, [9000], 2 ** 30, 2 ** 30, False),
 ])
 def test_decode(dtype, heads, kv_heads, head_dim, page_rows, lengths, window, sinks, heads_first):
@@ -175,6 +177,21 @@ def test_hidden_keys_reach_nothing(dtype, head_dim, bad):
             x[int(table[0, j // 16]), j % 16] = bad
     last = attention.decode(q[n - 1:].cuda(), kc, vc, table, int32([n])).cpu()
     check(last, q[n - 1:], k, v, position[-1:], window, sinks, dtype, "decode")
+    # a window of more keys than one workgroup takes
+    n, window, sinks = 1500, 700, 50
+    q, k, v = normal(gen, 9, 2, head_dim, dtype=dtype), normal(gen, n, 1, head_dim, dtype=dtype), normal(gen, n, 1, head_dim, dtype=dtype)
+    bad_k, bad_v = k.clone(), v.clone()
+    for x in (bad_k, bad_v):
+        x[sinks:n - window] = bad
+    kc, vc, table = cache_of([bad_k], [bad_v], 16, n // 16 + 1, gen, fill=bad)
+    attention = Attention(2, 1, head_dim, dtype, 16, window=window, sinks=sinks)
+    last = attention.decode(q[8:].cuda(), kc, vc, table, int32([n])).cpu()
+    check(last, q[8:], k, v, torch.tensor([n - 1]), window, sinks, dtype, "decode of many keys")
+    for x in (kc, vc):
+        for j in range(n - window - 8, n - window):
+            x[int(table[0, j // 16]), j % 16] = (k if x is kc else v)[j].cuda()
+    chain = attention.tree(q.cuda(), kc, vc, table, int32([n]), int32([0, 9])).cpu()
+    check(chain, q, k, v, torch.arange(n - 9, n), window, sinks, dtype, "chain behind many keys")
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
