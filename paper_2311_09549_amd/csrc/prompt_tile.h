@@ -18,6 +18,12 @@
 // vector ALUs 0.49 (a maximum, a power of two, a sum and a conversion per score), and LDS reads, 256 rows' worth for every 32 that use them,
 // about as long again.  Twelve packed prompts up to 2,048 rows, 32 heads on 8: 146 us, 0.59 PFLOP/s, matrix pipes 0.34: the start and end
 // of blocks, with nothing beside them on the compute unit.
+//
+// Windows and trees: tiles of 32 KB for keys and values go straight to LDS (global_load_lds), in the order of the exchange, three ahead of the one that is worked on, and page
+// numbers come a tile ahead of those; the registers that this frees keep queries from being spilled.  The waits are by counts of loads, so nothing else of a
+// wavefront may load in the main loop.  bf16, heads of 128: 16,384 rows through a window of 4,096 and four first keys, 16 heads on 4, in 600 us (0.80 PFLOP/s; its 66 tiles of 64 keys a block take 2.2 us each,
+// products, powers and LDS reads as above); chunks of four sequences up to 509 rows through a window of 1,000 in 54 us; 24 trees of up to 63 rows behind 8,191 keys in 112 us and
+// 18 for the join, 170 with tiles through registers.
 #pragma once
 
 #include "attention_device.h"
