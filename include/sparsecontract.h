@@ -439,7 +439,8 @@ sc_status sc_attention_append_tree(const sc_attention *attention, const sc_seque
 sc_status sc_attention_tree_workspace_bytes(const sc_attention *attention, size_t *bytes);
 
 /* Attention of nodes over keys and values in the cache.  parent = NULL: each row follows the one before it, as in prompts, for few rows a sequence (no limit to
- * their number).  Wrong lengths, page numbers and parents make NaN of the rows that they concern.  Queues two kernels, as decode does. */
+ * their number).  Wrong lengths, page numbers and parents make NaN of the rows that they concern.  At most 2^30 rows times heads of a key head (SC_ERR_BAD_DIMS).  Queues two kernels, as
+ * decode does, or one, where the table or the window has room for few keys. */
 sc_status sc_attention_tree(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const sc_rows_view *q, const sc_cache_view *cache,
                             const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 

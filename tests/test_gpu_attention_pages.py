@@ -67,7 +67,37 @@ CASES = [
     (300, 70, 300, 16, 20000, 0),  # several blocks of pages, wide tables
     (5, 0, 4, 16, 3, 0),           # all are given up
     (0, 6, 4, 32, 9, 2),           # all are new
+    (40, 1500, 6, 16, 12000, 0),   # more sequences than a workgroup has threads
+    (1500, 40, 6, 16, 0, 0),
 ]
+
+
+def test_tables_of_millions_of_pages():
+    """More blocks of pages than a workgroup has threads: the free ones are far behind the first, and pages in use are spread over all of it."""
+    count, columns = 4_300_000, 40
+    attention = Attention(2, 1, 64, BF16, 16)
+    rng = random.Random(1)
+    pages = [[rng.randrange(count - 4_250_000, count) for _ in range(columns)] for _ in range(5)]
+    lengths = [640, 633, 0, 17, 320]
+    free = sorted(rng.sample(range(4_100_000, count), 500))
+    holders = [1] * count
+    for p in free:
+        holders[p] = 0
+    for row, n in zip(pages, lengths):
+        for p in row[:reference.columns_of(n, 16)]:
+            holders[p] = holders[p] or 1      # never below what the table holds
+    parents, wanted = [1, 1, 4, -1, 3, 0], [633, 640, 600, 500, 16, 640]
+    expect = reference.fork(pages, lengths, holders, parents, wanted, 16)
+    got = attention.fork(int32(pages), int32(lengths), int32(holders), int32(parents), int32(wanted))
+    for x, y in zip(got, expect):
+        assert torch.equal(x, int32(y))
+    sparse = [0] * count
+    for p in rng.sample(range(count), 70_000):
+        sparse[p] = rng.randint(1, 4)
+    expect = reference.compact(pages, lengths, sparse, 16)
+    got = attention.compact(int32(pages), int32(lengths), int32(sparse))
+    for x, y in zip(got, expect):
+        assert torch.equal(x, int32(y))
 
 
 @pytest.mark.parametrize("sequences,new,columns,page_rows,spare,outside", CASES)

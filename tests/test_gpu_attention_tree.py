@@ -401,3 +401,84 @@ def test_accept_wrong_tables():
             x[int(table[7, 2]), at] = rows[32 + i].cuda()
     for x, y in zip((kc, vc), expect):
         assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+# -- streams, strides, captures ---------------------------------------------------------------------------------------------------------
+def operands(gen, heads=8, n=1500, nodes=40, d=64):
+    k, v, q = normal(gen, n, 1, d, dtype=BF16), normal(gen, n, 1, d, dtype=BF16), normal(gen, nodes, heads, d, dtype=BF16)
+    tree = random_tree(nodes, 4, gen)
+    kc, vc, table = cache_of([k], [v], 64, 30, gen, fill=0.0)
+    return q, k, v, tree, (kc, vc, table, int32([n]), int32([0, nodes]), int32(tree))
+
+
+@pytest.mark.parametrize("heads", [1, 8])
+def test_strides(heads):
+    """Queries and results in a wider array, and heads before rows."""
+    gen = torch.Generator().manual_seed(heads)
+    q, k, v, tree, args = operands(gen, heads)
+    want, bound = attend_seen(q, k, v, tree_mask(tree, 1500)[0], 1 / 8, BF16)
+    attention = Attention(heads, 1, 64, BF16, 64)
+    wide = torch.full((2, 40, heads + 3, 80), NAN, dtype=BF16, device="cuda")
+    wide[0, :, 1:-2, 8:-8] = q.cuda()
+    out = wide[1, :, 1:-2, 8:-8]
+    assert attention.tree(wide[0, :, 1:-2, 8:-8], *args, out=out) is out
+    assert_within(out, want, bound)
+    assert bool(torch.isnan(wide[1, :, 0].float()).all()) and bool(torch.isnan(wide[1, :, :, :8].float()).all()) and bool(torch.isnan(wide[1, :, :, 72:].float()).all())
+    turned = q.cuda().transpose(0, 1).contiguous().transpose(0, 1)
+    assert_within(attention.tree(turned, *args), want, bound)
+
+
+@pytest.mark.parametrize("heads", [1, 8])
+@pytest.mark.parametrize("named", [False, True])
+def test_first_call_in_a_capture(heads, named):
+    """A handle whose first calls are captured: replays and eager calls beside them are right."""
+    gen = torch.Generator().manual_seed(5)
+    q, _, _, tree, args = operands(gen, heads)
+    q, last = q.cuda(), int32([-1])
+    want = Attention(heads, 1, 64, BF16, 64).tree(q, *args).clone()
+    holders = torch.zeros(args[0].shape[0], dtype=torch.int32, device="cuda")
+    holders[args[2][0, :24].long()] = 1
+    tables = args[2], args[3], holders, int32([0, 0, -1])
+    expect = [x.clone() for x in Attention(heads, 1, 64, BF16, 64).fork(*tables)]
+    torch.cuda.synchronize()
+    attention, side, graph = Attention(heads, 1, 64, BF16, 64), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    kw = dict(stream=side.cuda_stream) if named else {}
+    with torch.cuda.graph(graph, stream=side):
+        got = [attention.tree(q, *args, **kw), attention.accept(*args, last, **kw), *attention.fork(*tables, **kw)]
+    for _ in range(3):
+        for x in got:
+            x.fill_(-9)
+        others = [torch.full((1 << 22,), 3.0, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want) and got[1].tolist() == [1460]
+        assert all(torch.equal(x, y) for x, y in zip(got[2:], expect))
+        assert torch.equal(attention.tree(q, *args), want)
+        torch.cuda.synchronize()
+        assert all(bool((x == 3.0).all()) for x in others)
+
+
+def test_calls_on_another_stream():
+    """Results and workspaces are made while the current stream still reads memory that was freed on it, of their sizes."""
+    gen = torch.Generator().manual_seed(1)
+    q, _, _, tree, args = operands(gen)
+    q = q.cuda()
+    attention = Attention(8, 1, 64, BF16, 64)
+    want = Attention(8, 1, 64, BF16, 64).tree(q, *args).clone()
+    gate = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    side, ready, done = torch.cuda.Stream(), torch.cuda.Event(), torch.cuda.Event()
+    ready.record()
+    side.wait_event(ready)
+    old = [torch.full((attention.tree_ws_bytes // 4,), 3.0, device="cuda"), torch.full_like(want, 3.0)]
+    for _ in range(20):
+        gate = (gate @ gate).clamp_(-1.0, 1.0)
+    read = [x.clone() for x in old]     # queued behind that
+    del old
+    got = attention.tree(q, *args, stream=side.cuda_stream)
+    done.record(side)
+    torch.cuda.current_stream().wait_event(done)
+    kept = got.clone()
+    torch.cuda.synchronize()
+    assert all(bool((x == 3.0).all()) for x in read) and torch.equal(kept, want)

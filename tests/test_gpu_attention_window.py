@@ -251,3 +251,65 @@ def test_a_window_of_everything_is_none():
     got = wide.prompt(q, k, v, int32([0, n])).cpu()
     check(got, q.cpu(), k.cpu(), v.cpu(), torch.arange(n), None, 0, F32, "wide")
     check(plain.prompt(q, k, v, int32([0, n])).cpu(), q.cpu(), k.cpu(), v.cpu(), torch.arange(n), n, 0, F32, "none")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 72, 128, 200])
+def test_strides_and_rows_of_no_sequence(dtype, head_dim):
+    """Rows in a wider array and heads before rows; rows before the first sequence and behind the last are not written, and what they hold does not matter."""
+    gen = torch.Generator().manual_seed(head_dim)
+    rows, window, sinks = [150, 0, 333], 90, 5
+    total = 7 + sum(rows) + 9
+    attention = Attention(4, 2, head_dim, dtype, window=window, sinks=sinks)
+    q, k, v = (normal(gen, total, h, head_dim, dtype=dtype) for h in (4, 2, 2))
+    for x in (q, k, v):
+        x[:7], x[-9:] = NAN, NAN
+    for how in ("wide", "heads"):
+        if how == "wide":
+            views = []
+            for x in (q, k, v, torch.full_like(q, 7.0)):
+                wide = torch.full((total, x.shape[1] + 3, head_dim + 16), NAN, dtype=dtype, device="cuda")
+                wide[:, 1:-2, 8:-8] = x.cuda()
+                views.append(wide[:, 1:-2, 8:-8])
+        else:
+            views = [x.cuda().transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, torch.full_like(q, 7.0))]
+        got = attention.prompt(*views[:3], int32([7, 157, 157, 490]), out=views[3]).cpu()
+        assert bool((got[:7] == 7.0).all()) and bool((got[490:] == 7.0).all())
+        for at, n in ((7, 150), (157, 333)):
+            check(got[at:at + n], q[at:at + n], k[at:at + n], v[at:at + n], torch.arange(n), window, sinks, dtype, f"{how}, sequence of {n}")
+
+
+def test_shared_heads_of_stride_zero():
+    """Keys and values of a head that all share, by a stride of 0."""
+    gen = torch.Generator().manual_seed(3)
+    q, k, v = normal(gen, 200, 4, 64, dtype=BF16), normal(gen, 200, 1, 64, dtype=BF16), normal(gen, 200, 1, 64, dtype=BF16)
+    got = Attention(4, 2, 64, BF16, window=30).prompt(q.cuda(), k.cuda().expand(200, 2, 64), v.cuda().expand(200, 2, 64), int32([0, 200])).cpu()
+    check(got, q, k, v, torch.arange(200), 30, 0, BF16, "shared")
+
+
+def test_more_sequences_than_are_counted():
+    """Packed prompts of more sequences than a block is counted among."""
+    gen = torch.Generator().manual_seed(9)
+    rows = [int(x) for x in torch.randint(0, 6, (1500,), generator=gen)]
+    rows[700] = 300
+    total = sum(rows)
+    q, k, v = (normal(gen, total, h, 64, dtype=BF16) for h in (2, 1, 1))
+    got = Attention(2, 1, 64, BF16, window=20, sinks=1).prompt(q.cuda(), k.cuda(), v.cuda(), int32(starts(rows))).cpu()
+    at = 0
+    for b, n in enumerate(rows):
+        if n and (b % 50 == 0 or n > 5 or b > 1490):
+            check(got[at:at + n], q[at:at + n], k[at:at + n], v[at:at + n], torch.arange(n), 20, 1, BF16, f"sequence {b}")
+        at += n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_decode_many_sequences(dtype):
+    """More sequences than a wavefront has lanes, and more units than workgroups: shares that begin and end anywhere."""
+    gen = torch.Generator().manual_seed(5)
+    lengths = [int(x) for x in torch.randint(0, 1500, (300,), generator=gen)]
+    keys, values = ([normal(gen, n, 2, 64, dtype=dtype) for n in lengths] for _ in range(2))
+    q = normal(gen, 300, 4, 64, dtype=dtype)
+    kc, vc, table = cache_of(keys, values, 64, 24, gen)
+    got = Attention(4, 2, 64, dtype, 64, window=700, sinks=3).decode(q.cuda(), kc, vc, table, int32(lengths)).cpu()
+    for b, n in enumerate(lengths):
+        check(got[b:b + 1], q[b:b + 1], keys[b], values[b], torch.tensor([n - 1]), 700, 3, dtype, f"sequence {b} of length {n}")
