@@ -479,12 +479,13 @@ sc_status sc_attention_pages_workspace_bytes(int64_t pages, int32_t new_batch, s
  *   - length_out[i] is wanted[i], -1 for a wrong parent, length or wanted number (outside 0 .. page_count * page_rows), and for a sequence that does not get the pages it
  *     takes because those before it (such ones among them) and it take more than are free.  Such a sequence holds nothing; its entries are -1, as are all that hold no page.
  *   - Entries whose number is no page stay out of it: -1 in the next batch as well.
- * Sequences that are not in the call keep their pages by `holders`.  The results do not depend on the order in which the GPU works.  Four kernels. */
+ * Sequences that are not in the call keep their pages by `holders`.  The results do not depend on the order in which the GPU works.  Four kernels; one for small tables. */
 sc_status sc_attention_fork(const sc_attention *attention, const sc_pages_view *tables, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Pages in use (holders not 0) move to the lowest numbers: with n of them, the k-th one from number n on goes to the k-th free one below n.  moves[3 k ..] (pages / 2 triples) is
  * (page, where it goes, page_rows), -1, -1, 0 behind the last move; sc_attention_copy makes them.  Entries that lengths reach follow their pages, others stay as they are, and
- * `page_out` may be `page`.  Tables of sequences that are not in the call have to follow by the moves.  new_batch is 0, and parent, wanted and length_out are NULL.  Four kernels. */
+ * `page_out` may be `page`.  Tables of sequences that are not in the call have to follow by the moves.  new_batch is 0, and parent, wanted and length_out are NULL.  Four kernels; one for small
+ * tables. */
 sc_status sc_attention_compact(const sc_attention *attention, const sc_pages_view *tables, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Copies rows 0 .. moves[3 k + 2] - 1 of the keys and values of page moves[3 k] to page moves[3 k + 1], for `count` triples in device memory; a triple with a number outside 0..pages-1

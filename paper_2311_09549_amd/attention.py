@@ -216,7 +216,7 @@ class Attention:
         operands = (self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count), self._numbers("parents", parents, new),
                     0 if wanted is None else self._numbers("wanted", wanted, new))
         if out is None:
-            out = table, after, held, moves = self._made(stream, lambda: (_empty_like(pages) if new == batch else self._empty(new, columns), _empty_like(parents), _empty_like(holders),
+            out = table, after, held, moves = self._made(stream, lambda: (_empty_like(pages) if new == batch and page_ld >= columns else self._empty(new, columns), _empty_like(parents), _empty_like(holders),
                                                                           self._empty(new, 3)))
             results = table.data_ptr(), table.stride()[0], after.data_ptr(), held.data_ptr(), moves.data_ptr()
         else:
@@ -233,7 +233,7 @@ class Attention:
         count = holders.shape[0]
         length, held = self._numbers("lengths", lengths, batch), self._numbers("holders", holders, count)
         if out is None:
-            out = table, after, moves = self._made(stream, lambda: (_empty_like(pages), _empty_like(holders), self._empty(count // 2, 3)))
+            out = table, after, moves = self._made(stream, lambda: (_empty_like(pages) if page_ld >= columns else self._empty(batch, columns), _empty_like(holders), self._empty(count // 2, 3)))
             table, table_ld, after, moves = table.data_ptr(), table.stride()[0], after.data_ptr(), moves.data_ptr()
         else:
             table, table_ld, after, moves = self._results(out, ((batch, columns), (count,), (count // 2, 3)))

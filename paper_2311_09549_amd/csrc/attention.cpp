@@ -326,7 +326,7 @@ extern "C" sc_status sc_attention_append(const sc_attention *at, const sc_sequen
 extern "C" sc_status sc_attention_append_tree(const sc_attention *at, const sc_sequence_view *sequences, const int32_t *parent, const sc_rows_view *q,
                                               const sc_rows_view *k, const sc_rows_view *v, const sc_rows_view *q_out, const sc_cache_view *cache, void *hip_stream)
 {
-    if (!parent) return SC_ERR_NULL;
+    if (!parent && !(sequences && sequences->rows == 0)) return SC_ERR_NULL;
     return append(at, sequences, parent, q, k, v, q_out, cache, hip_stream);
 }
 

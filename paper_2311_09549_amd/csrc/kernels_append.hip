@@ -114,9 +114,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a)
     // a node of a tree is at the position of its depth, wherever it is stored
     int64_t position = place;
     if (a.parent) {
-        const int32_t depth = depth_of(a.parent + begin, row - begin);
-        position = (int64_t)a.s.length[b] - count + (depth < 0 ? row - begin : depth);
-        if (depth < 0 || a.s.length[b] < count) page = -1;
+        const int32_t depth = count > kMaxNodes ? -1 : depth_of(a.parent + begin, row - begin);
+        if (depth < 0 || paged_length(a.s, b) < count) page = -1;   // rotated as if each row followed the one before it
+        else position = place - (row - begin) + depth;
     }
     for (int t = threadIdx.x; t < a.pairs; t += kAppendThreads) {
         const double x = (double)position * a.turns[t];

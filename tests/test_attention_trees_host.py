@@ -128,7 +128,8 @@ def test_append_tree_refusals():
     assert call(parent=0) == "SC_ERR_NULL" and call(q=None) == "SC_ERR_NULL" and call(key=None) == "SC_ERR_NULL"
     for change, status in BAD_SEQUENCES:
         assert call(sequences=_sequences(**change)) == status, change
-    assert call(sequences=_sequences(rows=0)) == "SC_OK"
+    assert call(sequences=_sequences(rows=0)) == "SC_OK" and call(sequences=_sequences(rows=0), parent=0) == "SC_OK"
+    assert call(sequences=None, parent=0) == "SC_ERR_NULL"
 
 
 def test_accept_refusals():

@@ -164,6 +164,25 @@ def test_compact(sequences, columns, page_rows, spare):
         assert torch.equal(in_place[0], got[0]) and torch.equal(in_place[1], got[1]) and torch.equal(moves, got[2])
 
 
+@pytest.mark.parametrize("step", [0, 1, 3, 9])
+def test_tables_whose_rows_share_memory(step):
+    """Rows of a table that is only read may overlap or be the same; the tables that are made of it are whole."""
+    columns, batch = 5, 4
+    numbers = torch.arange(40, dtype=torch.int32, device="cuda") % 30
+    pages = numbers.as_strided((batch, columns), (step, 1))
+    lengths = int32([80, 64, 17, 33])
+    holders = torch.zeros(37, dtype=torch.int32)
+    for b, n in enumerate((5, 4, 2, 3)):
+        for p in pages[b, :n].tolist():
+            holders[p] += 1
+    attention, holders = Attention(1, 1, 64, BF16, 16), holders.cuda()
+    for a, b in zip(attention.compact(pages, lengths, holders), attention.compact(pages.contiguous(), lengths, holders)):
+        assert torch.equal(a, b)
+    parents = int32([3, 0, 1, 2])
+    for a, b in zip(attention.fork(pages, lengths, holders, parents), attention.fork(pages.contiguous(), lengths, holders, parents)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("kv_heads,head_dim,page_rows,heads_first", [(1, 64, 16, False), (8, 128, 64, True), (3, 72, 32, False), (2, 8, 16, True), (16, 256, 128, False)])
 def test_copy(dtype, kv_heads, head_dim, page_rows, heads_first):

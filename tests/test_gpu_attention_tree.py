@@ -353,6 +353,36 @@ def test_append_wrong_tables():
         assert torch.equal(cache, x)
 
 
+def test_append_of_wrong_lengths():
+    """More nodes than a tree may have, and a length that the table has no room for: nothing is stored, also of the rows whose places it has."""
+    gen = torch.Generator().manual_seed(14)
+    attention = Attention(1, 1, 64, BF16, 16)
+    for nodes, length, columns in ((1025, 1030, 65), (1024, 1030, 65), (5, 33, 2), (5, 32, 2)):
+        k = normal(gen, nodes, 1, 64, dtype=BF16).cuda()
+        kc, vc = (torch.full((columns, 16, 1, 64), 5.0, dtype=BF16, device="cuda") for _ in range(2))
+        attention.append(None, k, k, kc, vc, torch.arange(columns, dtype=torch.int32, device="cuda")[None], int32([length]), int32([0, nodes]), parents=int32(range(-1, nodes - 1)))
+        expect = torch.full((columns * 16, 1, 64), 5.0, dtype=BF16, device="cuda")
+        if nodes <= 1024 and length <= 16 * columns:
+            expect[length - nodes:length] = k
+        for cache in (kc, vc):
+            assert torch.equal(cache.view(-1, 1, 64), expect), (nodes, length)
+
+
+def test_no_rows():
+    """Sequences without rows: nothing is stored, and paths of no nodes leave what is before them."""
+    gen = torch.Generator().manual_seed(15)
+    k, v = normal(gen, 20, 1, 64, dtype=BF16), normal(gen, 20, 1, 64, dtype=BF16)
+    kc, vc, table = cache_of([k, k], [v, v], 16, 2, gen, fill=0.0)
+    before = kc.clone(), vc.clone()
+    attention, lengths, row_start, none = Attention(2, 1, 64, BF16, 16), int32([20, 11]), int32([0, 0, 0]), int32([])
+    q, new = torch.empty(0, 2, 64, dtype=BF16, device="cuda"), torch.empty(0, 1, 64, dtype=BF16, device="cuda")
+    assert attention.append(q, new, new, kc, vc, table, lengths, row_start, parents=none).shape == q.shape
+    assert attention.tree(q, kc, vc, table, lengths, row_start, none).shape == q.shape
+    assert attention.accept(kc, vc, table, lengths, row_start, none, int32([-1, -1])).tolist() == [20, 11]
+    assert attention.accept(kc, vc, table, lengths, row_start, none, int32([0, -1])).tolist() == [-1, 11]
+    assert torch.equal(kc, before[0]) and torch.equal(vc, before[1])
+
+
 # -- the accepted path ----------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("heads_first", [False, True])
