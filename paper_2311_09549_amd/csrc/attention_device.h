@@ -320,6 +320,8 @@ struct Wave {
 
     struct Scores { f32x4 s[TILES]; };
 
+    // TRIM: without the products of pieces behind the head, by a branch that all lanes take alike.
+    template <bool TRIM = false>
     __device__ __forceinline__ void scores(Scores &x, const Keys &k) const
     {
 #pragma unroll
@@ -327,6 +329,7 @@ struct Wave {
             x.s[n] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < QC; ++c) {
+                if (TRIM && !EXACT && c >= QC / 2 && c * (64 / B) >= head_dim) continue;   // more than half of DP is head
                 if constexpr (B == 2) {
                     x.s[n] = TR::mfma(k.k[n][c], q[c], x.s[n]);
                 } else {

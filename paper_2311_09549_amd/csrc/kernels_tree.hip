@@ -7,7 +7,7 @@
 //
 // Single rows, 64 sequences up to 32,767 keys through a window of 4,096, bf16, 32 heads of 128 on 8: 152 us, 5.0 TB/s (a large copy reaches 4.7), of which the join is 5.  Trees
 // behind 24 sequences of 8,192 keys: of 4 rows 171 us (4.7 TB/s), of 16 rows, 64 pairs, 186 (4.3).  fp32, 16 heads of 80 with keys of their own, trees of up to 21 rows behind
-// 12 sequences up to 1,500: 29 us and 7 for the join, matrix pipes, with pairs padded to 16 or 32 and heads to 128, busy half of the time; two tiles of pairs at a time, with one workgroup on
+// 12 sequences up to 1,500: 28 us (29 with the products of pieces behind the head) and 7 for the join, matrix pipes, with pairs padded to 16 or 32, busy half of the time; two tiles of pairs at a time, with one workgroup on
 // a compute unit instead of two, take 50.  Behind few keys, tree_whole_kernel: 8 sequences of 320 keys and 8 rows 10.6 us, a chain of reads.
 #include "attention_device.h"
 
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(64 * kWaves, (kTreeGroups<Wave<TR, DP, EXACT>,
                 const bool more = base + STEP < end;
                 typename W::Scores scores[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) w[r].scores(scores[r], keys);
+                for (int r = 0; r < RT; ++r) w[r].template scores<B == 4>(scores[r], keys);
                 if (more) {
                     find(base + STEP);
                     w[0].load_keys(keys, t, row_bytes);
@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(64 * kWholeWaves<DP>, kWholeWaves<DP> / 4) tre
         if (!filled) rows.fill(q);   // keys and values are on their way
         filled = true;
         if (base < end) {
-            w.scores(scores, keys);
+            w.template scores<B == 4>(scores, keys);
             uint32_t seen = 0;
 #pragma unroll
             for (int n = 0; n < TILES; ++n)
