@@ -446,12 +446,15 @@ sc_status sc_attention_tree(const sc_attention *attention, const sc_sequence_vie
 
 /* The sequences go on from node last[b] of their trees (-1: from the keys before the tree): the keys and values of the path to it move to the places behind those keys, in
  * order, and length_out[b] (NULL: not wanted) becomes their number with the path's, -1 where the length, the path or last[b] is wrong: nothing moves there.
- * What rows behind the new length hold is not specified.  A row whose old or new place is in no page of the cache does not move.  Other layers of a model
+ * What rows behind the new length hold is not specified; their pages stay with the sequence until sc_attention_fork is called with the lengths of before and wants the new ones.  A row whose
+ * old or new place is in no page of the cache does not move.  Other layers of a model
  * take the same call with their caches and the same (old) lengths; `length_out` is apart from them.  One kernel. */
 sc_status sc_attention_accept(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const int32_t *last, const sc_cache_view *cache,
                               int32_t *length_out, void *hip_stream);
 
 /* Tables of pages, lengths, and holders: holders[p] is the number of entries that hold page p, of those that the length of their sequence reaches, 0 for a free page.
+ * Lengths are those that the entries were given out for.  After sc_attention_accept these are still the ones that it was given, not the ones that it made: with shorter ones, pages of entries
+ * that they no longer reach would stay held by nobody who could give them up, and would be moved without their entries.  Its lengths are what is wanted of the fork that comes next.
  * All of it device memory.  `page_out` has page_count entries a sequence as well. */
 typedef struct {
     int32_t batch, new_batch;
@@ -475,7 +478,8 @@ sc_status sc_attention_pages_workspace_bytes(int64_t pages, int32_t new_batch, s
  *   - Whole pages are shared.  A page that new sequences keep in part, and are going to write to, stays with the first of them, if no entry holds it whole; the others get a copy: moves[3 i ..]
  *     is (page, copy, rows to copy), -1, -1, 0 for a sequence without one (new_batch triples).  sc_attention_copy makes them, in the cache of each layer.
  *   - Pages that are taken are the free ones (0 holders when the present batch is given up) of the lowest numbers, in the order of the sequences.
- *   - With a window, pages that are wholly behind the window of the last kept row, and hold none of the first `sinks`, are let go (entry -1).
+ *   - With a window, pages that are wholly behind the window of the last kept row, and hold none of the first `sinks`, are let go (entry -1).  A sequence that is to lose rows and then to gain
+ *     others takes two calls there, the first for the rows that stay: of one call for both, rows that are to be written over count as kept.
  *   - length_out[i] is wanted[i], -1 for a wrong parent, length or wanted number (outside 0 .. page_count * page_rows), and for a sequence that does not get the pages it
  *     takes because those before it (such ones among them) and it take more than are free.  Such a sequence holds nothing; its entries are -1, as are all that hold no page.
  *   - Entries whose number is no page stay out of it: -1 in the next batch as well.

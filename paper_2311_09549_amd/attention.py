@@ -10,13 +10,19 @@ Drafted tokens, nodes of a tree behind each sequence (`parents`: one number per 
 
     q = attention.append(q, k, v, keys, values, pages, lengths, row_start, parents=parents)      # rotated by their depths
     y = attention.tree(q, keys, values, pages, lengths, row_start, parents)                      # each sees its ancestors
-    lengths = attention.accept(keys, values, pages, lengths, row_start, parents, last)           # the path to node last[b] becomes the sequence
+    accepted = attention.accept(keys, values, pages, lengths, row_start, parents, last)          # the path to node last[b] becomes the sequence
 
 Sequences that branch, end, shrink and grow share pages (`holders`: how many entries hold each page, 0 for a free one):
 
-    pages, lengths, holders, moves = attention.fork(pages, lengths, holders, parents, wanted)    # sequence i goes on from sequence parents[i]
+    pages, lengths, holders, moves = attention.fork(pages, lengths, holders, order, wanted)      # sequence i goes on from sequence order[i]
     pages, holders, moves = attention.compact(pages, lengths, holders)                           # pages in use to the lowest numbers
     attention.copy(keys, values, moves)                                                          # in every layer's cache, after either
+
+Both take the lengths that the table's pages were given out for.  After `accept` those are the ones of before, and its own are what is wanted, of a fork before any other call on the pages:
+
+    pages, lengths, holders, moves = attention.fork(pages, lengths, holders, order, accepted[order])     # pages of nodes that were not accepted are free again
+    attention.copy(keys, values, moves)
+    pages, lengths, holders, moves = attention.fork(pages, lengths, holders, same, lengths + new)        # then room for new rows (same: 0, 1, 2, ..)
 
 `q` is (rows, heads, head_dim), `k` and `v` (rows, kv_heads, head_dim), `keys` and `values` (pages, page_rows, kv_heads, head_dim); any strides
 that are multiples of 16 bytes, head_dim contiguous.  `pages` (batch, columns), `lengths` (batch) and `row_start` (batch + 1) are int32.
@@ -187,7 +193,7 @@ class Attention:
     def accept(self, keys, values, pages, lengths, row_start, parents, last, out=None, stream=None):
         """Sequence b goes on from node last[b] of its tree (-1: from what is before it): the rows of the path move to the places behind what is before the
         tree.  Returns the lengths after that (in `out`, apart from the operands), -1 where a length, a path or its end is wrong.  Every layer's
-        cache takes the call, with the lengths of before."""
+        cache takes the call, with the lengths of before, and so does the `fork` that gives up the pages of the other nodes, with the new lengths as `wanted`."""
         if _current_device() != self._index:
             return self._there(self.accept, keys, values, pages, lengths, row_start, parents, last, out, stream)
         rows = parents.shape[0]
@@ -206,7 +212,7 @@ class Attention:
 
     def fork(self, pages, lengths, holders, parents, wanted=None, out=None, workspace=None, stream=None):
         """The next batch of sequences: number i has the first rows of sequence parents[i] (-1: none), up to wanted[i] of them (all unless given), and pages for
-        the rest of wanted[i] rows.  Returns its pages and lengths (-1 for a sequence that is wrong or finds no free page), holders, and the copies of pages that
+        the rest of wanted[i] rows.  `lengths`: what the pages were given out for (after `accept`, those of before it).  Returns its pages and lengths (-1 for a sequence that is wrong or finds no free page), holders, and the copies of pages that
         `copy` has to make in every layer's cache before anything is written there (rows of `moves`: page, copy, rows).  `out`: those four, apart from the
         operands, but for holders, which may stay where they are.  `workspace`: device bytes of the caller's (binding.attention_pages_workspace_bytes)."""
         if _current_device() != self._index:
@@ -225,7 +231,7 @@ class Attention:
         return tuple(out)
 
     def compact(self, pages, lengths, holders, out=None, workspace=None, stream=None):
-        """Moves the pages in use to the lowest numbers.  Returns pages, holders and the moves that `copy` has to make in every layer's cache before anything
+        """Moves the pages in use to the lowest numbers.  `lengths`: what the pages were given out for; entries behind them stay as they are.  Returns pages, holders and the moves that `copy` has to make in every layer's cache before anything
         is written there (rows: page, where it goes, rows).  `out`: those three; the first two may be the operands themselves."""
         if _current_device() != self._index:
             return self._there(self.compact, pages, lengths, holders, out, workspace, stream)

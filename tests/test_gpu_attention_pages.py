@@ -285,6 +285,38 @@ def test_a_search_with_drafts(dtype, window, sinks):
         assert m.holders.tolist() == held(m.pages.tolist(), m.lengths.tolist(), 16, len(m.holders))
 
 
+@pytest.mark.parametrize("window,sinks", [(None, 0), (37, 5)])
+def test_pages_of_drafts_are_free_again(window, sinks):
+    """Trees of many more nodes than are accepted, in the order of calls that the module gives: every page is held by the entries that lengths reach, and by nothing else."""
+    rng, gen = random.Random(2), torch.Generator().manual_seed(2)
+    attention = Attention(4, 2, 64, BF16, 16, window=window, sinks=sinks)
+    caches = [torch.zeros(90, 16, 2, 64, dtype=BF16, device="cuda") for _ in range(2)]
+    holders = torch.zeros(90, dtype=torch.int32, device="cuda")
+
+    def fork(pages, lengths, holders, parents, wanted):
+        pages, lengths, holders, moves = attention.fork(pages, lengths, holders, parents, wanted)
+        attention.copy(*caches, moves)
+        assert lengths.tolist() == wanted.tolist() and holders.tolist() == held(pages.tolist(), lengths.tolist(), 16, 90)
+        return pages, lengths, holders
+
+    pages, lengths, holders = fork(int32([], 0, 20), int32([], 0), holders, int32([-1] * 3), int32([15, 40, 1]))
+    for step in range(5):
+        nodes = [63, rng.randint(1, 63), 17]
+        pages, lengths, holders = fork(pages, lengths, holders, int32([0, 1, 2]), lengths + int32(nodes))
+        parents = int32([p for n in nodes for p in random_tree(n, 3, gen)])
+        row_start, last = int32([0, nodes[0], nodes[0] + nodes[1], sum(nodes)]), int32([0, rng.randrange(-1, nodes[1]), 16])
+        k = torch.randn(sum(nodes), 2, 64, generator=gen).to(BF16).cuda()
+        attention.append(None, k, k, *caches, pages, lengths, row_start, parents=parents)
+        accepted = attention.accept(*caches, pages, lengths, row_start, parents, last)
+        order = [rng.randrange(3) for _ in range(3)]
+        pages, lengths, holders = fork(pages, lengths, holders, int32(order), accepted[order])
+        if step % 2:
+            pages, holders, moves = attention.compact(pages, lengths, holders)
+            attention.copy(*caches, moves)
+            used = int((holders != 0).sum())
+            assert holders.tolist() == held(pages.tolist(), lengths.tolist(), 16, 90) and not bool(holders[used:].any())
+
+
 def test_a_step_in_a_graph():
     """Branching, drafting, attention, acceptance, captured once and replayed on other tables: each replay as the eager calls, bit for bit."""
     gen, rng = torch.Generator().manual_seed(10), random.Random(10)
