@@ -128,6 +128,52 @@ def test_fork(sequences, new, columns, page_rows, spare, outside, window, sinks)
                 assert got[2].tolist() == held(expect[0], expect[1], page_rows, len(holders))
 
 
+def short_of_pages(seed, sequences, new, columns, page_rows, spare, outside):
+    """A batch of which every sequence goes on, most of them by pages, with fewer of those than they take."""
+    rng = random.Random(seed)
+    pages, lengths, holders = batch_of(rng, sequences, columns, page_rows, spare, share=0.7, outside=outside)
+    parents = list(range(sequences)) + [rng.randrange(sequences) for _ in range(new - sequences)]
+    rng.shuffle(parents)
+    wanted = [min(columns * page_rows, lengths[p] + rng.choice((0, 0, 1, page_rows, 3 * page_rows))) for p in parents]
+    wanted = [rng.randint(0, n) if rng.random() < 0.2 else n for n in wanted]
+    return pages, lengths, holders, parents, wanted
+
+
+SHORT = [
+    # sequences, new ones, columns, page_rows, spare pages, outside
+    (8, 14, 8, 16, 1, 0),
+    (40, 160, 12, 32, 10, 7),            # by one workgroup
+    (300, 1300, 4, 16, 700, 0),          # more sequences than a workgroup has threads
+    (60, 400, 15, 16, 20, 9000),         # more pages than it has room for
+]
+
+
+@pytest.mark.parametrize("sequences,new,columns,page_rows,spare,outside", SHORT)
+@pytest.mark.parametrize("window,sinks", [(None, 0), (90, 17)])
+def test_fork_without_pages_enough(sequences, new, columns, page_rows, spare, outside, window, sinks):
+    """Sequences that find no free page hold nothing: with sequences before and behind them that are served, of kinds that share whole pages and that a page would have been left to."""
+    attention = Attention(2, 1, 64, BF16, page_rows, window=window, sinks=sinks)
+    short, between, sharing, keeping = 0, False, False, False
+    for seed in range(6):
+        pages, lengths, holders, parents, wanted = short_of_pages(seed, sequences, new, columns, page_rows, spare, outside)
+        expect = reference.fork(pages, lengths, holders, parents, wanted, page_rows, window, sinks)
+        refused = [i for i, n in enumerate(expect[1]) if n < 0]
+        short += bool(refused)
+        between |= bool(refused) and any(n >= 0 for n in expect[1][:refused[0]]) and any(n >= 0 for n in expect[1][refused[0]:])
+        kept = [min(lengths[p], n) for p, n in zip(parents, wanted)]
+        sharing |= any(kept[i] >= page_rows and any(parents[i] == parents[j] and kept[j] >= page_rows for j in range(new) if j not in refused) for i in refused)
+        keeping |= any(kept[i] % page_rows and not any(pages[parents[i]][kept[i] // page_rows] in row[:reference.columns_of(max(n, 0), page_rows)] for row, n in zip(*expect[:2])) for i in refused)
+        args = int32(pages), int32(lengths), int32(holders), int32(parents), int32(wanted)
+        got = attention.fork(*args)
+        for name, x, y in zip(("pages", "lengths", "holders", "moves"), got, expect):
+            assert torch.equal(x, int32(y)), f"{name}, seed {seed}"
+        if not outside:
+            assert got[2].tolist() == held(expect[0], expect[1], page_rows, len(holders))
+        again = attention.fork(*args, out=(*(torch.empty_like(x) for x in got[:2]), args[2], torch.empty_like(got[3])))     # holders in place
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+    assert short >= 3 and between and sharing and keeping
+
+
 def test_fork_in_place_on_views_and_with_a_workspace():
     """Holders changed in place, tables with rows of a wider one, a workspace of the caller's whose contents do not matter."""
     rng = random.Random(4)
