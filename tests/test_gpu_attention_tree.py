@@ -512,3 +512,39 @@ def test_calls_on_another_stream():
     kept = got.clone()
     torch.cuda.synchronize()
     assert all(bool((x == 3.0).all()) for x in read) and torch.equal(kept, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("head_dim", [64, 40, 128, 72, 256, 200])
+def test_many_trees_in_tiles(dtype, head_dim):
+    """As many sequences as give every workgroup a block of rows and all of its keys, in tiles through LDS.  Rows behind the lengths hold NaN, and one branch of a tree infinities, which
+    the other one does not see."""
+    gen = torch.Generator().manual_seed(head_dim)
+    count, nodes, bad = 40, 20, 7
+    lengths = [max(nodes, int(x)) for x in torch.randint(1, 700, (count,), generator=gen)]
+    lengths[bad] = 300
+    keys, values = ([normal(gen, n, 4, head_dim, dtype=dtype) for n in lengths] for _ in range(2))
+    q = normal(gen, count * nodes, 8, head_dim, dtype=dtype)
+    trees = [random_tree(nodes, 4, gen) for _ in range(count)]
+    trees[bad] = [-1, -1] + [i - 2 for i in range(2, nodes)]       # even nodes one branch, odd nodes the other
+    trees[11][5] = 9                                               # a later one
+    hidden = [x.clone() for x in values]
+    hidden[bad][300 - nodes + 1::2] = INF
+    kc, vc, table = cache_of(keys, hidden, 16, 44, gen, fill=NAN)
+    args = (q.cuda(), kc, vc, table, int32(lengths), int32(starts([nodes] * count)), int32(flat(trees)))
+    attention = Attention(8, 4, head_dim, dtype, 16)
+    got = attention.tree(*args)
+    assert torch.equal(got.nan_to_num(7.0), attention.tree(*args).nan_to_num(7.0))
+    got = got.cpu()
+    for b in range(count):
+        rows = got[b * nodes:(b + 1) * nodes]
+        if b == 11:
+            wrong = [i for i in range(nodes) if i >= 5 and (i == 5 or 5 in path_of(trees[b][:5] + [-1] + trees[b][6:], i))]
+            assert bool(torch.isnan(rows[wrong]).all()) and bool(torch.isfinite(rows[[i for i in range(nodes) if i not in wrong]]).all())
+            continue
+        want, bound = attend_seen(q[b * nodes:(b + 1) * nodes], keys[b], values[b], tree_mask(trees[b], lengths[b])[0], 1 / math.sqrt(head_dim), dtype)
+        if b == bad:
+            assert_within(rows[::2], want[::2], bound[::2], "the branch without infinities")
+            assert not bool(torch.isfinite(rows[1::2]).any())
+        else:
+            assert_within(rows, want, bound, f"tree {b}")

@@ -313,3 +313,74 @@ def test_decode_many_sequences(dtype):
     got = Attention(4, 2, 64, dtype, 64, window=700, sinks=3).decode(q.cuda(), kc, vc, table, int32(lengths)).cpu()
     for b, n in enumerate(lengths):
         check(got[b:b + 1], q[b:b + 1], keys[b], values[b], torch.tensor([n - 1]), 700, 3, dtype, f"sequence {b} of length {n}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("heads,head_dim", [(8, 64), (8, 40), (4, 128), (8, 104), (4, 256), (2, 200)])
+def test_prompt_in_pages_split_over_the_gpu(dtype, heads, head_dim):
+    """Few rows behind many keys in pages: shares that cut blocks of rows, on both sides of the gap.  Pages behind every row's window are given back; what no row sees of the others holds
+    NaN; a wrong page among those that are seen makes NaN of its sequence alone."""
+    gen = torch.Generator().manual_seed(head_dim)
+    lengths, rows, window, sinks = [6001, 5500, 5800], [40, 33, 7], 3000, 100
+    keys, values = ([normal(gen, n, 1, head_dim, dtype=dtype) for n in lengths] for _ in range(2))
+    q = normal(gen, sum(rows), heads, head_dim, dtype=dtype)
+    hidden = [[x.clone() for x in side] for side in (keys, values)]
+    for side in hidden:
+        for x, n, r in zip(side, lengths, rows):
+            x[sinks:n - r - window + 1] = NAN
+    kc, vc, table = cache_of(*hidden, 16, -(-max(lengths) // 16), gen, fill=NAN)
+    give_back(table, 16, lengths, rows, window, sinks)
+    table[2, 5700 // 16] = -1
+    attention = Attention(heads, 1, head_dim, dtype, 16, window=window, sinks=sinks)
+    workspace = torch.full((attention.prompt_ws_bytes // 4,), NAN, device="cuda")   # its contents do not matter
+    args = (q.cuda(), kc, vc, table, int32(lengths), int32(starts(rows)))
+    got = attention.prompt_paged(*args, workspace=workspace).cpu()
+    at = 0
+    for b, n in enumerate(rows):
+        if b == 2:
+            assert bool(torch.isnan(got[at:at + n]).all())
+        else:
+            check(got[at:at + n], q[at:at + n], keys[b], values[b], torch.arange(lengths[b] - n, lengths[b]), window, sinks, dtype, f"sequence {b}")
+        at += n
+    again = attention.prompt_paged(*args).cpu()
+    assert torch.equal(got[:73], again[:73]) and bool(torch.isnan(again[73:]).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("heads,head_dim", [(4, 64), (4, 56), (4, 72), (4, 256), (2, 200)])
+def test_prompts_of_other_heads_split_over_the_gpu(dtype, heads, head_dim):
+    """As test_prompt_split_over_the_gpu, in tiles of other sizes; keys in the middle hold NaN, which the rows that are looked at do not see."""
+    gen = torch.Generator().manual_seed(head_dim)
+    n, window, sinks = 4000, 2001, 200
+    q, k, v = (normal(gen, n, h, head_dim, dtype=dtype) for h in (heads, 1, 1))
+    bad_k, bad_v = k.clone(), v.clone()
+    for x in (bad_k, bad_v):
+        x[1000:1400] = NAN
+    attention = Attention(heads, 1, head_dim, dtype, window=window, sinks=sinks)
+    got = attention.prompt(q.cuda(), bad_k.cuda(), bad_v.cuda(), int32([0, n])).cpu()
+    for lo, hi in ((0, 100), (900, 1000), (1400 + window - 1, 3500), (3900, 4000)):
+        check(got[lo:hi], q[lo:hi], k, v, torch.arange(lo, hi), window, sinks, dtype, f"rows from {lo}")
+    assert bool(torch.isnan(got[1000:1400 + window - 1]).all())
+
+
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(16, 4, 64), (16, 4, 72), (16, 2, 256)])
+def test_many_rows_in_fp32(heads, kv_heads, head_dim):
+    """As many rows and heads as make a wavefront take 16 rows and all their keys by itself, packed and in pages; infinities where nobody looked at sees them."""
+    gen = torch.Generator().manual_seed(head_dim)
+    rows, window, sinks = [4050, 0, 33], 130, 5
+    total = sum(rows)
+    q, k, v = (normal(gen, total, h, head_dim) for h in (heads, kv_heads, kv_heads))
+    bad_k, bad_v = k.clone(), v.clone()
+    bad_k[1000:1050], bad_v[1000:1050] = NAN, INF
+    attention = Attention(heads, kv_heads, head_dim, F32, 32, window=window, sinks=sinks)
+    places = [(0, 0, 40), (0, 960, 1000), (0, 1050 + window - 1, 1230), (0, 3990, 4050), (4050, 0, 33)]
+
+    def look(got):
+        for begin, lo, hi in places:
+            n = rows[0] if begin == 0 else rows[2]
+            check(got[begin + lo:begin + hi], q[begin + lo:begin + hi], k[begin:begin + n], v[begin:begin + n], torch.arange(lo, hi), window, sinks, F32, f"rows from {begin + lo}")
+
+    look(attention.prompt(q.cuda(), bad_k.cuda(), bad_v.cuda(), int32(starts(rows))).cpu())
+    caches = [[x[:4050], x[:0], x[4050:]] for x in (bad_k, bad_v)]
+    kc, vc, table = cache_of(*caches, 32, 128, gen, fill=NAN)
+    look(attention.prompt_paged(q.cuda(), kc, vc, table, int32(rows), int32(starts(rows))).cpu())
