@@ -277,8 +277,11 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             }
         };
         const auto to_lds = [](uint32_t at, const char *p) {
-            // nothing else in these kernels uses m0
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory");
+            // m0 is no register that the compiler gives away, which it warns of; it writes it itself before each instruction of its own that reads it
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(p) : "memory", "m0");
+#pragma clang diagnostic pop
         };
         const auto load_tile = [&](int32_t base, int buffer) {
 #pragma unroll
