@@ -420,7 +420,9 @@ sc_status sc_attention_decode(const sc_attention *attention, const sc_sequence_v
                               const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* A handle whose rows see a window: a row at position p sees keys p - window + 1 .. p, and of the keys before those the first `sinks` (0: none).  Prompts, decode and trees go by
- * it; desc->causal has to be 1.  Keys that no row of a call sees are not read, nor the entries of pages that hold none that one sees: those may be anything.
+ * it; desc->causal has to be 1.  Keys that no row of a call sees, and entries of pages that hold none that one sees, have no effect on its results, whatever they are; some beside the edges of the
+ * window and of the first keys may be read, so that a number of a page of the cache stands for memory that can be.  (fork and compact go by every entry that lengths reach: one whose page was given
+ * back has to be -1 for them, or still to be counted in `holders`.)
  * `window` 1..2^30, `sinks` 0..2^30.  The decoding workspace of such a handle is larger. */
 sc_status sc_attention_create_window(sc_attention **out, const sc_attention_desc *desc, int32_t window, int32_t sinks);
 
@@ -439,7 +441,8 @@ sc_status sc_attention_append_tree(const sc_attention *attention, const sc_seque
 sc_status sc_attention_tree_workspace_bytes(const sc_attention *attention, size_t *bytes);
 
 /* Attention of nodes over keys and values in the cache.  parent = NULL: each row follows the one before it, as in prompts, for few rows a sequence (no limit to
- * their number).  Wrong lengths, page numbers and parents make NaN of the rows that they concern.  At most 2^30 rows times heads of a key head (SC_ERR_BAD_DIMS).  Queues two kernels, as
+ * their number).  Wrong lengths and parents make NaN of the rows that they concern; a page number outside 0..pages-1 of the rows whose keys reach it, and it may make NaN of other rows of
+ * the sequence.  At most 2^30 rows times heads of a key head (SC_ERR_BAD_DIMS).  Queues two kernels, as
  * decode does, or one, where the table or the window has room for few keys. */
 sc_status sc_attention_tree(const sc_attention *attention, const sc_sequence_view *sequences, const int32_t *parent, const sc_rows_view *q, const sc_cache_view *cache,
                             const sc_rows_view *out, void *workspace, size_t workspace_bytes, void *hip_stream);
@@ -483,7 +486,7 @@ sc_status sc_attention_pages_workspace_bytes(int64_t pages, int32_t new_batch, s
  *   - length_out[i] is wanted[i], -1 for a wrong parent, length or wanted number (outside 0 .. page_count * page_rows), and for a sequence that does not get the pages it
  *     takes because those before it (such ones among them) and it take more than are free.  Such a sequence holds nothing; its entries are -1, as are all that hold no page.
  *   - Entries whose number is no page stay out of it: -1 in the next batch as well.
- * Sequences that are not in the call keep their pages by `holders`.  The results do not depend on the order in which the GPU works.  Four kernels; one for small tables. */
+ * Sequences that are not in the call keep their pages by `holders`.  A caller that may run out of pages keeps the present tables, `holders` among them, until it has seen the lengths.  The results do not depend on the order in which the GPU works.  Four kernels; one for small tables. */
 sc_status sc_attention_fork(const sc_attention *attention, const sc_pages_view *tables, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Pages in use (holders not 0) move to the lowest numbers: with n of them, the k-th one from number n on goes to the k-th free one below n.  moves[3 k ..] (pages / 2 triples) is
