@@ -90,7 +90,7 @@ class Attention:
         self.prompt_ws_bytes = sc.attention_prompt_workspace_bytes(self.handle)
         self._few_rows = 4 * (32 if head_dim > 128 else 128)   # of a packed prompt: no more than four tiles of keys, which the library never splits
         self._own = {}   # workspaces, made by the first calls that need them
-        self._pages_bytes = {}   # of fork and compact, by the pages of a cache and the next power of two of sequences
+        self._pages_bytes = {}   # of fork and compact, by the pages of a cache and sequences
         self._h = self.handle.handle
         (self._append, self._prompt, self._prompt_paged, self._decode, self._append_tree, self._tree, self._accept, self._fork, self._compact,
          self._copy) = sc.attention_calls()
@@ -376,10 +376,10 @@ class Attention:
         if stream is None:
             stream = _raw_stream(self._index)
         key = None
-        if workspace is None:   # the handle's own, for as many pages and few sizes of batches
-            key = count, 1 << new.bit_length()
+        if workspace is None:   # the handle's own, for as many pages and the next of a few sizes of batches: all of them stay, and most of a workspace goes by the pages
+            key = count, 0 if new == 0 else 31 if new <= 31 else 2047 if new <= 2047 else 2 ** 17 - 1 if new < 2 ** 17 else 2 ** 20 - 1
             if key not in self._pages_bytes:
-                self._pages_bytes[key] = sc.attention_pages_workspace_bytes(count, min(key[1], 2 ** 20 - 1))
+                self._pages_bytes[key] = sc.attention_pages_workspace_bytes(*key)
         address, size = self._workspace_of(stream, workspace, key)
         status = call(self._h, _pack_pages(*record), address, size, stream)
         if status:

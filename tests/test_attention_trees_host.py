@@ -345,6 +345,19 @@ def test_results_and_workspaces_belong_to_the_stream_of_their_call(monkeypatch):
         assert len(memory.made) == 1 and memory.told == {made[1].data_ptr(): [7]}
 
 
+def test_workspaces_of_many_batches(monkeypatch):
+    """Batches of any sizes share a few workspaces of the handle's, which stay as long as it does; each has room for its batch."""
+    attention, recorder = handle()
+    memory, holders = Memory(monkeypatch, 7), numbers(5000)
+    for new in (1, 2, 3, 5, 9, 17, 31, 32, 33, 100, 500, 2047, 2048, 5000, 70_000, 2 ** 17 - 1, 2 ** 17, 2 ** 20 - 1):
+        out = numbers(new, 5, address=2 * A), numbers(new, address=3 * A), holders, numbers(new, 3, address=4 * A)
+        attention.fork(numbers(2, 5), numbers(2), holders, numbers(new), None, out=out, stream=STREAM)
+        assert recorder.calls[-1][-2] >= sc.attention_pages_workspace_bytes(5000, new)
+    attention.compact(numbers(2, 5), numbers(2), holders, out=(numbers(2, 5), holders, numbers(2500, 3, address=4 * A)), stream=STREAM)
+    assert recorder.calls[-1][-2] >= sc.attention_pages_workspace_bytes(5000, 0)
+    assert len(memory.made) <= 5
+
+
 def test_calls_are_made_on_the_device_of_the_handle(monkeypatch):
     attention, _ = handle()
     devices, at = Devices(monkeypatch, 2), []
