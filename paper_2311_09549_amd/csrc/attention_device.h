@@ -228,7 +228,8 @@ struct Wave {
         return a;
     }
 
-    // o += V^T P^T for the weights p of the lane's keys.
+    // o += V^T P^T for the weights p of the lane's keys.  16-bit types: the product takes both operands in the type of the values, so weights are rounded to it here, by half a step of
+    // each at most; their sums are of the fp32 ones.
     __device__ __forceinline__ void add_values(const Values &x, const float (&p)[TILES * 4])
     {
         if constexpr (B == 2) {

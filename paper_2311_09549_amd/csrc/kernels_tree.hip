@@ -5,10 +5,10 @@
 // workgroup takes an equal share of it.  A step's keys and values are read into registers once for RT products of 16 pairs each: with few pairs everything is bound by memory.
 // Steps that all rows see whole are taken without a mask; the others by bits, one for each key and row, from chains of parents that are gone up once, in LDS.
 //
-// Single rows, 64 sequences up to 32,767 keys through a window of 4,096, bf16, 32 heads of 128 on 8: 152 us, 5.0 TB/s (a large copy reaches 4.7), of which the join is 5.  Trees
+// Single rows, 64 sequences up to 32,767 keys through a window of 4,096, bf16, 32 heads of 128 on 8: 154 us a call, 5.0 TB/s (a large copy reaches 4.7), of which the join is 5.  Trees
 // behind 24 sequences of 8,192 keys: of 4 rows 171 us (4.7 TB/s), of 16 rows, 64 pairs, 186 (4.3).  fp32, 16 heads of 80 with keys of their own, trees of up to 21 rows behind
-// 12 sequences up to 1,500: 28 us (29 with the products of pieces behind the head) and 7 for the join, matrix pipes, with pairs padded to 16 or 32, busy half of the time; two tiles of pairs at a time, with one workgroup on
-// a compute unit instead of two, take 50.  Behind few keys, tree_whole_kernel: 8 sequences of 320 keys and 8 rows 10.6 us, a chain of reads.
+// 12 sequences up to 1,500: 28 us (29 with the products of pieces behind the head) and 7 for the join, matrix pipes (with pairs padded to 16 or 32) busy a quarter of the time, 2.9 TB/s, waits 0.4: what a step of keys
+// ahead does not cover; two tiles of pairs at a time, with one workgroup on a compute unit instead of two, take 50.  Behind few keys, tree_whole_kernel: 8 sequences of 320 keys and 8 rows 10.6 us, a chain of reads.
 #include "attention_device.h"
 
 namespace sck {
@@ -541,7 +541,9 @@ void launch_pairs(const AttendArgs &a, hipStream_t stream)
     tree_join_kernel<TR, DP, RT><<<dim3(1 << groups_log2, 4 * RT), 256, 0, stream>>>(a, groups_log2);
 }
 
-// Keys that a sequence may have to read: all that the table has room for, or that a window has (and the rows of a tree behind it).
+// Keys that a sequence may have to read: all that the table has room for, or that a window has, where every row of the call counts as a key.  What the first kernel reads once for all pairs of a sequence,
+// tree_whole_kernel reads for each 16, which pays where few rows leave the GPU to them.  bf16, 32 heads of 128 on 8, window of 256 and four first keys, us there and here: single rows of 256 sequences 79 and 56, of 384
+// 123 and 91, 24 trees of 63 rows 137 and 74, 64 of 8 rows 48 and 26, 24 of 20 rows 50 and 51 (of heads of 64, 24 and 43; 16 heads of 256 on 2, 38 and 46); fp32, 16 heads of 128 on 4, 384 single rows 103 and 86.
 int64_t room_of(const AttendArgs &a)
 {
     const int64_t room = table_room(a.s), through = (int64_t)a.window + a.sinks + 32 + a.s.rows;
@@ -551,9 +553,10 @@ int64_t room_of(const AttendArgs &a)
 int64_t whole_tiles(const AttendArgs &a) { return (int64_t)a.s.rows * a.group / kHeadTile + a.s.batch; }
 
 // Whether the keys of a tile are shared by the wavefronts of a workgroup, through LDS (prompt_tile.h), by the pairs of a sequence and a key head on average.  bf16, 32 heads of 128 on 8,
-// us there and here: 24 sequences of 640 keys, 4 rows 24.5 and 26.3, 8 rows 24 and 39, 16 rows 25 and 46; of 2,560 keys 64, 64 and 66 beside 54, 63 and 77; of 8,192
-// keys 207, 207 and 213 beside 172, 189 and 185; 24 rows 216 there.  One sequence of 32,768 keys, 16 rows: 81 and 60.  320 keys, by tree_whole_kernel: 8 sequences of 16 rows 17 and
-// 13, 24 of 8 rows 16 and 21.
+// us there and here: 24 sequences of 640 keys, 4 rows 24 and 26, 8 rows 24 and 38, 16 rows 25 and 46; of 2,560 keys 64, 64 and 66 beside 51, 62 and 77; of 8,192
+// keys, 8 rows 209 and 181, 16 rows 210 and 180, 24 rows 211 and 320, 63 rows 295 and 596.  One sequence of 32,768 keys, 16 rows 82 and 61, 24 rows 82 and 73, 63 rows 113 and 109.  320 keys, by tree_whole_kernel: 8 sequences
+// of 16 rows 16 and 13, 24 of 8 rows 16 and 21.  Heads of 64 and 256 go by the same numbers, which suit them less: of 64, 24 sequences of 8 rows behind 320 keys 23 and 12, behind 640 27 and 28, 16 rows behind 2,560
+// 52 and 55, behind 8,192 144 and 114, 24 rows 144 and 172; of 256, 8 rows behind 320 keys 34 and 38, behind 640 55 and 53, 16 rows behind 2,560 190 and 300, behind 8,192 494 and 929, 63 rows 947 and 3,759.
 bool through_lds(const AttendArgs &a, sc_dtype dtype)
 {
     if (!a.tree || a.window || dtype == SC_F32) return false;

@@ -179,8 +179,10 @@ void launch_padded(AttendArgs a, hipStream_t stream)
         if (SEES == kWindow && longest > (int64_t)a.window + a.sinks + (32 * NW >> heads_log2)) longest = (int64_t)a.window + a.sinks + (32 * NW >> heads_log2);
         const int64_t tiles = (longest < kMaxKeys ? longest : kMaxKeys) / (DP == 256 ? 32 : 128);
         const int shares = prompt_shares(a.n_cu);
-        // Windows and trees: blocks that have rows, of sequences that are alike.  24 trees of 63 rows, 32, 8, 128: behind 2,560 keys 116 us with and 98 without, 5,120 keys 205 and about 180,
-        // lengths up to 8,191 125 and 200; one behind 32,768 keys 112 with.
+        // Windows and trees: blocks that have rows, of sequences that are alike.  Trees of 63 rows, 32, 8, 128: 24 behind 2,560 keys 112 us with and 97 without, behind 5,120 191 and 183, behind 8,192 296 and 285, lengths up to
+        // 8,191 125 and 200; 12 behind 4,096 95 and 125, 4 behind 8,192 83 and 235, one behind 32,768 117 and 890.  32, 8, 64: 86 and 69, 130 and 114, 184 and 173; 76 and 89, 69 and 155, 90 and 578; 32, 8, 256: 340 and
+        // 379, 618 and 721, 951 and 1,131; 278 and 295, 197 and 564, 222 and 2,181.  Windows, 32, 8, 128: 2,048 rows through 1,000 keys 68 and 51, 4,096 through 2,000 156 and 158 (8, 1, 128: 60 and 78; 8, 1, 256: 172 and
+        // 144), chunks of 4 times 509 rows through 1,000 keys 84 and 61, of 100 rows through 8,000 73 and 269 (of 64: 52 and 172, of 256: 129 and 556).
         int64_t filled = blocks, longest_alone = tiles * shares;
         if (SEES != kEverything) {
             const int64_t rows = 32 * NW >> heads_log2;

@@ -21,8 +21,8 @@
 //
 // Windows and trees: tiles of 32 KB for keys and values go straight to LDS (global_load_lds), in the order of the exchange, three ahead of the one that is worked on, and page
 // numbers come a tile ahead of those; the registers that this frees keep queries from being spilled.  The waits are by counts of loads, so nothing else of a
-// wavefront may load in the main loop.  bf16, heads of 128: 16,384 rows through a window of 4,096 and four first keys, 16 heads on 4, in 600 us (0.80 PFLOP/s; its 66 tiles of 64 keys a block take 2.2 us each,
-// products, powers and LDS reads as above); chunks of four sequences up to 509 rows through a window of 1,000 in 54 us; 24 trees of up to 63 rows behind 8,191 keys in 112 us and
+// wavefront may load in the main loop.  bf16, heads of 128: 16,384 rows through a window of 4,096 and four first keys, 16 heads on 4, in 590 us (0.81 PFLOP/s; its 66 tiles of 64 keys a block take 2.2 us each,
+// products, powers and LDS reads as above); chunks of four sequences up to 509 rows through a window of 1,000 in 53 us, 16 of them before the first and behind the last of 18 tiles; 24 trees of up to 63 rows behind 8,191 keys in 112 us and
 // 18 for the join, 170 with tiles through registers.
 #pragma once
 
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) prompt_tile_kernel(AttendArgs
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; r += 2) {
-                    l += s[t][r] + s[t][r + 1];
+                    l += s[t][r] + s[t][r + 1];   // in fp32; weights are rounded once, to the type of the values, for the product that takes both in it
                     w[t][r / 8][r / 2 % 4] = TR::pack(s[t][r], s[t][r + 1]);
                 }
 
