@@ -23,6 +23,7 @@ Both take the lengths that the table's pages were given out for.  After `accept`
     pages, lengths, holders, moves = attention.fork(pages, lengths, holders, order, accepted[order])     # pages of nodes that were not accepted are free again
     attention.copy(keys, values, moves)
     pages, lengths, holders, moves = attention.fork(pages, lengths, holders, same, lengths + new)        # then room for new rows (same: 0, 1, 2, ..)
+    attention.copy(keys, values, moves)
 
 `q` is (rows, heads, head_dim), `k` and `v` (rows, kv_heads, head_dim), `keys` and `values` (pages, page_rows, kv_heads, head_dim); any strides
 that are multiples of 16 bytes, head_dim contiguous.  `pages` (batch, columns), `lengths` (batch) and `row_start` (batch + 1) are int32.
